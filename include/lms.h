@@ -431,6 +431,86 @@ lms_status lms_swap_decode_staged(void* dst, const void* src_host, uint64_t nume
                                   const void* stage, int32_t w, void* stream);
 
 
+/* ------------------------------------------------------------------ language-model layers
+ * Stand-alone like the convolutions above: raw device pointers, a hipStream_t as void*, a workspace the caller owns, nothing allocated,
+ * nothing waited for.  Matrices are row-major; weights lie as (inputs, outputs) like a 1x1 filter (C, K).  dtype is LMS_BF16 or LMS_F32 and is the
+ * type of every activation and weight; sums are fp32; biases and their gradients are fp32.  A row pitch (ld*, in elements) of 0 means dense rows,
+ * else it is at least the row's length.  bf16 matrices may start at any even address and have any pitch; those whose addresses are multiples of 16
+ * bytes and whose lengths and pitches are multiples of 8 elements are faster.  fp32 pointers are 4-byte aligned.  Outputs must not
+ * overlap inputs, unless said so.  The elements between the end of a row and the next one are neither read into a result nor written.
+ * Calls with m = 0 write what does not depend on rows (weight and bias gradients: zeros).
+ * workspace: device memory of at least the bytes that *_workspace_bytes says, 256-byte aligned, may be NULL for 0; what it holds before and after means nothing.
+ * LMS_EINVAL with a message for bad arguments, before anything is launched. */
+typedef enum { LMS_ACT_NONE = 0, LMS_ACT_RELU = 1, LMS_ACT_SILU = 2, LMS_ACT_GELU = 3 /* by erf */, LMS_ACT_GELU_TANH = 4 } lms_act;
+
+/* Linear layer of m rows, k inputs, n outputs: y = act(x w + bias) + res. */
+typedef struct {
+  int64_t m;                /* rows (tokens), >= 0 */
+  int32_t n, k;             /* outputs, inputs, >= 1 */
+  int32_t act;              /* lms_act */
+  int32_t dtype;            /* lms_dtype: LMS_BF16 or LMS_F32 */
+  int32_t wgrad_dtype;      /* type of dw: LMS_F32, or LMS_BF16 with dtype LMS_BF16 */
+  int64_t ldx, ldw, ldy, ldr; /* row pitches of x and dx; w and dw; y, dy and pre; res */
+} lms_linear_desc;
+typedef enum { LMS_LINEAR_FWD = 0, LMS_LINEAR_BWD = 1 } lms_linear_which;
+lms_status lms_linear_workspace_bytes(const lms_linear_desc* d, int32_t which, uint64_t* bytes);
+/* bias (n fp32 values), res (m x n, may be y itself if ldr = ldy) and pre may be NULL.  pre: x w + bias in the storage type, which
+ * lms_linear_bwd of a layer with an activation reads. */
+lms_status lms_linear_fwd(const lms_linear_desc* d, const void* x, const void* w, const float* bias, const void* res, void* y, void* pre,
+                          void* workspace, void* stream);
+/* dz = dy act'(pre), in the storage type where it enters the products; dx = dz w^T, dw = x^T dz, dbias = column sums of dz before it is rounded.
+ * The gradient of res is dy itself.  dx, dw and dbias may each be NULL and are then not computed (w is needed for dx only, x for dw only).
+ * pre may be NULL for LMS_ACT_NONE.  Deterministic. */
+lms_status lms_linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, const void* w, const void* pre, void* dx, void* dw, float* dbias,
+                          void* workspace, void* stream);
+
+/* Gated feed-forward projection of m rows, k inputs, f hidden units: h = act(x wg) * (x wu), one kernel. */
+typedef struct {
+  int64_t m;
+  int32_t f, k;
+  int32_t act, dtype, wgrad_dtype;   /* as in lms_linear_desc */
+  int64_t ldx, ldw, ldh;    /* row pitches of x and dx; wg, wu, dwg and dwu; h, g, u and dh.  wg and wu may be the halves of one (k, 2 f) matrix */
+} lms_gated_desc;
+typedef enum { LMS_GATED_FWD = 0, LMS_GATED_BWD = 1, LMS_GATED_BWD_RECOMPUTE = 2 } lms_gated_which;
+lms_status lms_gated_workspace_bytes(const lms_gated_desc* d, int32_t which, uint64_t* bytes);
+/* g = x wg and u = x wu (m x f each, storage type) are written where they are not NULL. */
+lms_status lms_gated_fwd(const lms_gated_desc* d, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, void* stream);
+/* dg = dh u act'(g) and du = dh act(g), in the storage type where they enter the products; dx = dg wg^T + du wu^T, dwg = x^T dg, dwu = x^T du.
+ * g and u: what the forward pass wrote, or both NULL: then they are computed again from x (a third more arithmetic, and 2 m f elements that need
+ * not be kept; workspace of LMS_GATED_BWD_RECOMPUTE).  dx may be NULL, and so may dwg and dwu together.  Deterministic. */
+lms_status lms_gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, const void* wg, const void* wu, const void* g, const void* u,
+                         void* dx, void* dwg, void* dwu, void* workspace, void* stream);
+
+/* Distillation from a teacher's top logits.  Row r: p = softmax(t[r] / T) over the entries of the row that are there, q = softmax(z[r] / T) over all
+ * classes, row loss T^2 sum_j p_j (log p_j - log q[ids[r][j]]), 0 for a row without entries.  loss = scale * sum_r weight[r] * (row loss),
+ * dz = scale * weight[r] * T * (q - p), 0 for rows without entries. */
+typedef struct {
+  int64_t rows;             /* >= 0 */
+  int32_t classes;          /* >= 1 */
+  int32_t k;                /* teacher entries of a row, 1 .. 1024 */
+  int32_t dtype;            /* of z and dz: LMS_BF16 or LMS_F32 */
+  int64_t ldz;              /* row pitch of z and dz, 0 = dense */
+  float temperature;        /* T > 0 */
+  float scale;              /* factor of the loss and its gradient, as 1 / (number of tokens) */
+} lms_distill_desc;
+typedef enum { LMS_DISTILL_FWD = 0, LMS_DISTILL_BWD = 1, LMS_DISTILL_LOSS_GRAD = 2 } lms_distill_which;
+lms_status lms_distill_workspace_bytes(const lms_distill_desc* d, int32_t which, uint64_t* bytes);
+/* z: rows x classes; t: rows x k fp32; ids: rows x k class numbers.  An entry is there if its id is in 0 .. classes-1 and its logit is above -inf; ids
+ * outside, as -1, mark the places that a row does not use, anywhere in it.  A class that comes more than once counts with the sum.  weight:
+ * rows fp32 values, or NULL for ones; a row of weight 0 gives neither loss nor gradient, whatever it holds.  Classes may be masked by -inf in z (q = 0;
+ * an entry with p > 0 on such a class makes the loss inf, and dz finite as elsewhere).
+ * loss: one fp32 value; row_loss (before scale and weight) and lse (logarithm of the sum over classes of exp(z / T), for lms_distill_bwd): rows fp32 values,
+ * each may be NULL.  Sums are fp32 within a row, fp64 over rows, in a fixed order. */
+lms_status lms_distill_fwd(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, float* loss,
+                           float* row_loss, float* lse, void* workspace, void* stream);
+/* dz may be z. */
+lms_status lms_distill_bwd(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, const float* lse,
+                           void* dz, void* workspace, void* stream);
+/* Loss and gradient in one launch over the rows. */
+lms_status lms_distill_loss_grad(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, float* loss,
+                                 void* dz, void* workspace, void* stream);
+
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,6 +17,10 @@ DEVICE, HOST = 0, 1
 F_RELU, F_AFFINE, F_BIAS, F_RES, F_ADDEND, F_MASK = 1, 2, 4, 8, 16, 32
 CHAIN_RULE, DIRECT_ORDER, OWN = 0, 1, 2
 X_POISON, X_NO_OVERLAP, X_KEEP_ALL, X_DMA_COPY, X_ENCODE_SWAPS, X_TIMING, X_STAGED_SWAPS = 1, 2, 4, 8, 16, 32, 64
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
+LINEAR_FWD, LINEAR_BWD = 0, 1
+GATED_FWD, GATED_BWD, GATED_BWD_RECOMPUTE = 0, 1, 2
+DISTILL_FWD, DISTILL_BWD, DISTILL_LOSS_GRAD = 0, 1, 2
 CONV_FWD, CONV_DGRAD, CONV_WGRAD, CONV_WGRAD_BIAS = 0, 1, 2, 3
 
 
@@ -62,6 +66,21 @@ class StepStats(C.Structure):
 class ConvDesc(C.Structure):
     _fields_ = [("ndim_sp", C.c_int32), ("n", C.c_int64), ("in_sp", C.c_int64 * 3), ("c", C.c_int32), ("k", C.c_int32),
                 ("filt", C.c_int32 * 3), ("stride", C.c_int32), ("pad", C.c_int32), ("flags", C.c_uint32)]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [("m", C.c_int64), ("n", C.c_int32), ("k", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32), ("wgrad_dtype", C.c_int32),
+                ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldy", C.c_int64), ("ldr", C.c_int64)]
+
+
+class GatedDesc(C.Structure):
+    _fields_ = [("m", C.c_int64), ("f", C.c_int32), ("k", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32), ("wgrad_dtype", C.c_int32),
+                ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldh", C.c_int64)]
+
+
+class DistillDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("classes", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32), ("ldz", C.c_int64),
+                ("temperature", C.c_float), ("scale", C.c_float)]
 
 
 P = C.POINTER
@@ -114,6 +133,16 @@ _SIGS = {
     "lms_swap_encode": (C.c_int, [VP, VP, C.c_uint64, VP]),
     "lms_swap_decode": (C.c_int, [VP, VP, C.c_uint64, VP]),
     "lms_swap_moved_bytes": (C.c_int, [VP, C.c_uint64, P(C.c_uint64)]),
+    "lms_linear_workspace_bytes": (C.c_int, [P(LinearDesc), C.c_int32, P(C.c_uint64)]),
+    "lms_linear_fwd": (C.c_int, [P(LinearDesc)] + [VP] * 8),
+    "lms_linear_bwd": (C.c_int, [P(LinearDesc)] + [VP] * 9),
+    "lms_gated_workspace_bytes": (C.c_int, [P(GatedDesc), C.c_int32, P(C.c_uint64)]),
+    "lms_gated_fwd": (C.c_int, [P(GatedDesc)] + [VP] * 8),
+    "lms_gated_bwd": (C.c_int, [P(GatedDesc)] + [VP] * 11),
+    "lms_distill_workspace_bytes": (C.c_int, [P(DistillDesc), C.c_int32, P(C.c_uint64)]),
+    "lms_distill_fwd": (C.c_int, [P(DistillDesc)] + [VP] * 9),
+    "lms_distill_bwd": (C.c_int, [P(DistillDesc)] + [VP] * 8),
+    "lms_distill_loss_grad": (C.c_int, [P(DistillDesc)] + [VP] * 8),
 }
 EXPORTS = sorted(_SIGS)
 

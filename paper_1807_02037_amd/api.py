@@ -284,3 +284,72 @@ def swap_moved_bytes(host, numel):
     b = C.c_uint64()
     _ck(A.lib().lms_swap_moved_bytes(host, numel, C.byref(b)))
     return b.value
+
+
+def linear_desc(m, n, k, act=A.ACT_NONE, dtype=A.BF16, wgrad_dtype=A.F32, ldx=0, ldw=0, ldy=0, ldr=0):
+    """m rows, n outputs, k inputs; ld*: row pitches in elements, 0 = dense."""
+    d = A.LinearDesc()
+    d.m, d.n, d.k, d.act, d.dtype, d.wgrad_dtype = m, n, k, act, dtype, wgrad_dtype
+    d.ldx, d.ldw, d.ldy, d.ldr = ldx, ldw, ldy, ldr
+    return d
+
+
+def linear_workspace_bytes(desc, which):
+    b = C.c_uint64()
+    _ck(A.lib().lms_linear_workspace_bytes(C.byref(desc), which, C.byref(b)))
+    return b.value
+
+
+def linear_fwd(desc, x, w, bias, res, y, pre, workspace, stream):
+    _ck(A.lib().lms_linear_fwd(C.byref(desc), x, w, bias, res, y, pre, workspace, stream))
+
+
+def linear_bwd(desc, dy, x, w, pre, dx, dw, dbias, workspace, stream):
+    _ck(A.lib().lms_linear_bwd(C.byref(desc), dy, x, w, pre, dx, dw, dbias, workspace, stream))
+
+
+def gated_desc(m, f, k, act=A.ACT_SILU, dtype=A.BF16, wgrad_dtype=A.F32, ldx=0, ldw=0, ldh=0):
+    """m rows, f hidden units, k inputs."""
+    d = A.GatedDesc()
+    d.m, d.f, d.k, d.act, d.dtype, d.wgrad_dtype = m, f, k, act, dtype, wgrad_dtype
+    d.ldx, d.ldw, d.ldh = ldx, ldw, ldh
+    return d
+
+
+def gated_workspace_bytes(desc, which):
+    b = C.c_uint64()
+    _ck(A.lib().lms_gated_workspace_bytes(C.byref(desc), which, C.byref(b)))
+    return b.value
+
+
+def gated_fwd(desc, x, wg, wu, h, g, u, workspace, stream):
+    _ck(A.lib().lms_gated_fwd(C.byref(desc), x, wg, wu, h, g, u, workspace, stream))
+
+
+def gated_bwd(desc, dh, x, wg, wu, g, u, dx, dwg, dwu, workspace, stream):
+    _ck(A.lib().lms_gated_bwd(C.byref(desc), dh, x, wg, wu, g, u, dx, dwg, dwu, workspace, stream))
+
+
+def distill_desc(rows, classes, k, temperature=1.0, scale=1.0, dtype=A.BF16, ldz=0):
+    """rows of logits over classes, k teacher entries a row."""
+    d = A.DistillDesc()
+    d.rows, d.classes, d.k, d.dtype, d.ldz, d.temperature, d.scale = rows, classes, k, dtype, ldz, temperature, scale
+    return d
+
+
+def distill_workspace_bytes(desc, which):
+    b = C.c_uint64()
+    _ck(A.lib().lms_distill_workspace_bytes(C.byref(desc), which, C.byref(b)))
+    return b.value
+
+
+def distill_fwd(desc, z, t, ids, weight, loss, row_loss, lse, workspace, stream):
+    _ck(A.lib().lms_distill_fwd(C.byref(desc), z, t, ids, weight, loss, row_loss, lse, workspace, stream))
+
+
+def distill_bwd(desc, z, t, ids, weight, lse, dz, workspace, stream):
+    _ck(A.lib().lms_distill_bwd(C.byref(desc), z, t, ids, weight, lse, dz, workspace, stream))
+
+
+def distill_loss_grad(desc, z, t, ids, weight, loss, dz, workspace, stream):
+    _ck(A.lib().lms_distill_loss_grad(C.byref(desc), z, t, ids, weight, loss, dz, workspace, stream))

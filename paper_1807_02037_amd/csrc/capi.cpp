@@ -29,6 +29,17 @@ lms_status swap_codec_staged(void* dst, const void* src, uint64_t numel, int64_t
                              void* stream);
 uint64_t swap_encoded_bytes(uint64_t numel);
 uint64_t swap_encoded_moved_bytes(const void* host, uint64_t numel);
+lms_status linear_workspace(const lms_linear_desc* d, int which, uint64_t* bytes);
+lms_status linear_fwd(const lms_linear_desc* d, const void* x, const void* w, const float* bias, const void* res, void* y, void* pre, void* ws, void* stream);
+lms_status linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, const void* w, const void* pre, void* dx, void* dw, float* db, void* ws,
+                      void* stream);
+lms_status gated_workspace(const lms_gated_desc* d, int which, uint64_t* bytes);
+lms_status gated_fwd(const lms_gated_desc* d, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* ws, void* stream);
+lms_status gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, const void* wg, const void* wu, const void* g, const void* u, void* dx, void* dwg,
+                     void* dwu, void* ws, void* stream);
+lms_status distill_workspace(const lms_distill_desc* d, int which, uint64_t* bytes);
+lms_status distill(const lms_distill_desc* d, int which, const void* z, const float* t, const int32_t* ids, const float* weight, const float* lse_in, float* loss,
+                   float* row_loss, float* lse, void* dz, void* ws, void* stream);
 }  // namespace lms
 
 using lms::set_error;
@@ -319,6 +330,53 @@ lms_status lms_swap_moved_bytes(const void* host, uint64_t numel, uint64_t* byte
   NEED(host && bytes, "lms_swap_moved_bytes: null pointer");
   *bytes = lms::swap_encoded_moved_bytes(host, numel);
   return LMS_OK;
+}
+
+lms_status lms_linear_workspace_bytes(const lms_linear_desc* d, int32_t which, uint64_t* bytes) {
+  NEED(d && bytes, "lms_linear_workspace_bytes: null argument");
+  return lms::linear_workspace(d, which, bytes);
+}
+lms_status lms_linear_fwd(const lms_linear_desc* d, const void* x, const void* w, const float* bias, const void* res, void* y, void* pre, void* workspace,
+                          void* stream) {
+  NEED(d && x && w && y, "lms_linear_fwd: null argument");
+  return lms::linear_fwd(d, x, w, bias, res, y, pre, workspace, stream);
+}
+lms_status lms_linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, const void* w, const void* pre, void* dx, void* dw, float* dbias,
+                          void* workspace, void* stream) {
+  NEED(d && dy, "lms_linear_bwd: null argument");
+  return lms::linear_bwd(d, dy, x, w, pre, dx, dw, dbias, workspace, stream);
+}
+lms_status lms_gated_workspace_bytes(const lms_gated_desc* d, int32_t which, uint64_t* bytes) {
+  NEED(d && bytes, "lms_gated_workspace_bytes: null argument");
+  return lms::gated_workspace(d, which, bytes);
+}
+lms_status lms_gated_fwd(const lms_gated_desc* d, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, void* stream) {
+  NEED(d && x && wg && wu && h, "lms_gated_fwd: null argument");
+  return lms::gated_fwd(d, x, wg, wu, h, g, u, workspace, stream);
+}
+lms_status lms_gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, const void* wg, const void* wu, const void* g, const void* u, void* dx,
+                         void* dwg, void* dwu, void* workspace, void* stream) {
+  NEED(d && dh, "lms_gated_bwd: null argument");
+  return lms::gated_bwd(d, dh, x, wg, wu, g, u, dx, dwg, dwu, workspace, stream);
+}
+lms_status lms_distill_workspace_bytes(const lms_distill_desc* d, int32_t which, uint64_t* bytes) {
+  NEED(d && bytes, "lms_distill_workspace_bytes: null argument");
+  return lms::distill_workspace(d, which, bytes);
+}
+lms_status lms_distill_fwd(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, float* loss, float* row_loss,
+                           float* lse, void* workspace, void* stream) {
+  NEED(d && z && t && ids, "lms_distill_fwd: null argument");
+  return lms::distill(d, LMS_DISTILL_FWD, z, t, ids, weight, nullptr, loss, row_loss, lse, nullptr, workspace, stream);
+}
+lms_status lms_distill_bwd(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, const float* lse, void* dz,
+                           void* workspace, void* stream) {
+  NEED(d && z && t && ids && lse && dz, "lms_distill_bwd: null argument");
+  return lms::distill(d, LMS_DISTILL_BWD, z, t, ids, weight, lse, nullptr, nullptr, nullptr, dz, workspace, stream);
+}
+lms_status lms_distill_loss_grad(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, float* loss, void* dz,
+                                 void* workspace, void* stream) {
+  NEED(d && z && t && ids && loss && dz, "lms_distill_loss_grad: null argument");
+  return lms::distill(d, LMS_DISTILL_LOSS_GRAD, z, t, ids, weight, nullptr, loss, nullptr, nullptr, dz, workspace, stream);
 }
 
 }  // extern "C"
