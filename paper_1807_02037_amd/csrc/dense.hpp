@@ -36,9 +36,16 @@ struct DenseP {
   float* part;                 // splits > 1: sums of a split, [split][source][M][N]
 };
 
-// p: everything up to out_f32, and part
+// The product by whichever kernel suits (dense_layers.hip): p holds everything up to out_f32, and part, of dense_ws bytes (a function of the sizes alone).
+hipError_t dense_product(int mode, bool f32, DenseP& p, hipStream_t s);
+uint64_t dense_ws(int mode, bool f32, long long M, int N, long long red, int segs, int srcs);
+
 hipError_t dense_bf16(int mode, DenseP& p, hipStream_t s);        // dense_gemm.hip
 hipError_t dense_f32(int mode, DenseP& p, hipStream_t s);         // dense_f32.hip
+hipError_t dense_join(int mode, bool f32, DenseP& p, hipStream_t s);        // dense_join.hip: p.part into the results
+bool dense_few_ok(int mode, long long M);                         // few rows (dense_few.hip)
+uint64_t dense_few_ws(int mode, bool f32, long long M, int N, long long red);
+hipError_t dense_few(int mode, bool f32, DenseP& p, hipStream_t s);
 
 namespace {
 

@@ -107,8 +107,6 @@ hipError_t fill_zero(void* out, long long rows, int N, long long ld, bool f32, h
   return hipGetLastError();
 }
 
-hipError_t product(int mode, bool f32, DenseP& p, hipStream_t s) { return f32 ? dense_f32(mode, p, s) : dense_bf16(mode, p, s); }
-
 // ---- what the two descriptors have in common ----
 struct Layer {
   long long m, ldx, ldw, ldy, ldr;
@@ -165,7 +163,7 @@ lms_status done(const char* what, hipError_t e) {
 }
 
 // dx = sum over sources of dz_s w_s^T; dw_s = x^T dz_s
-hipError_t layer_grads(const Layer& l, const void* const* dz, long long ldz, const void* x, const void* const* w, void* dx, void* const* dw, hipStream_t s) {
+hipError_t layer_grads(const Layer& l, const void* const* dz, long long ldz, const void* x, const void* const* w, void* dx, void* const* dw, float* part, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (dx) {
     DenseP p{};
@@ -174,7 +172,8 @@ hipError_t layer_grads(const Layer& l, const void* const* dz, long long ldz, con
     p.M = l.m; p.N = l.k; p.red = l.n;
     p.lda = ldz; p.ldb = l.ldw; p.ldo = l.ldx;
     p.segs = l.srcs; p.srcs = 1;
-    e = product(DENSE_DX, l.f32, p, s);
+    p.part = part;
+    e = dense_product(DENSE_DX, l.f32, p, s);
   }
   if (e == hipSuccess && dw[0]) {
     DenseP p{};
@@ -184,19 +183,34 @@ hipError_t layer_grads(const Layer& l, const void* const* dz, long long ldz, con
     p.lda = l.ldx; p.ldb = ldz; p.ldo = l.ldw;
     p.segs = 1; p.srcs = l.srcs;
     p.out_f32 = l.w32;
-    e = product(DENSE_DW, l.f32, p, s);
+    p.part = part;
+    e = dense_product(DENSE_DW, l.f32, p, s);
   }
   return e;
 }
 
+uint64_t grads_ws(const Layer& l, bool dx, bool dw) {
+  const uint64_t a = dx ? dense_ws(DENSE_DX, l.f32, l.m, l.k, l.n, l.srcs, 1) : 0, b = dw ? dense_ws(DENSE_DW, l.f32, l.k, l.n, l.m, 1, l.srcs) : 0;
+  return up(a > b ? a : b);
+}
+
 }  // namespace
+
+uint64_t dense_ws(int mode, bool f32, long long M, int N, long long red, int segs, int srcs) {
+  if (dense_few_ok(mode, M)) return dense_few_ws(mode, f32, M, N, red);
+  return 0;
+}
+hipError_t dense_product(int mode, bool f32, DenseP& p, hipStream_t s) {
+  if (dense_few_ok(mode, p.M)) return dense_few(mode, f32, p, s);
+  return f32 ? dense_f32(mode, p, s) : dense_bf16(mode, p, s);
+}
 
 lms_status linear_workspace(const lms_linear_desc* d, int which, uint64_t* bytes) {
   Layer l;
   if (const lms_status st = linear_layer(d, l)) return st;
   NEED(which == LMS_LINEAR_FWD || which == LMS_LINEAR_BWD, "lms_linear_workspace_bytes: unknown call %d", which);
-  *bytes = 0;
-  if (which == LMS_LINEAR_BWD) *bytes = (l.act != LMS_ACT_NONE ? grad_bytes(l) : 0) + chunk_bytes(l);
+  if (which == LMS_LINEAR_FWD) *bytes = up(dense_ws(DENSE_FWD, l.f32, l.m, l.n, l.k, 1, 1));
+  else *bytes = (l.act != LMS_ACT_NONE ? grad_bytes(l) : 0) + chunk_bytes(l) + grads_ws(l, true, true);
   return LMS_OK;
 }
 
@@ -218,7 +232,7 @@ lms_status linear_fwd(const lms_linear_desc* d, const void* x, const void* w, co
   p.lda = l.ldx; p.ldb = l.ldw; p.ldo = l.ldy; p.ldr = l.ldr;
   p.segs = 1; p.srcs = 1; p.act = l.act;
   p.part = (float*)ws;
-  return done("lms_linear_fwd", product(DENSE_FWD, l.f32, p, (hipStream_t)stream));
+  return done("lms_linear_fwd", dense_product(DENSE_FWD, l.f32, p, (hipStream_t)stream));
 }
 
 lms_status linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, const void* w, const void* pre, void* dx, void* dw, float* db, void* ws,
@@ -243,26 +257,26 @@ lms_status linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, c
   const bool with_act = l.act != LMS_ACT_NONE;
   const void* dz = dy;
   long long ldz = l.ldy;
+  char* at = (char*)ws;
   hipError_t e = hipSuccess;
   if (with_act || db) {
     GradP g{};
     g.d = dy; g.g = with_act ? pre : nullptr;
     g.M = l.m; g.N = l.n; g.act = l.act; g.ldd = l.ldy;
-    char* at = (char*)ws;
     if (with_act) {
       g.dz = at;
       g.ldo = ldz = grad_pitch(l.n);
       dz = at;
       at += grad_bytes(l);
     }
-    if (db) g.part = (float*)at;
+    if (db) { g.part = (float*)at; at += chunk_bytes(l); }
     e = act_grad(l.f32, g, db, s);
   }
   if (e == hipSuccess) {
     const void* const dzs[] = {dz};
     const void* const wsrc[] = {w};
     void* const dws[] = {dw};
-    e = layer_grads(l, dzs, ldz, x, wsrc, dx, dws, s);
+    e = layer_grads(l, dzs, ldz, x, wsrc, dx, dws, (float*)at, s);
   }
   return done("lms_linear_bwd", e);
 }
@@ -271,7 +285,9 @@ lms_status gated_workspace(const lms_gated_desc* d, int which, uint64_t* bytes) 
   Layer l;
   if (const lms_status st = gated_layer(d, l)) return st;
   NEED(which >= LMS_GATED_FWD && which <= LMS_GATED_BWD_RECOMPUTE, "lms_gated_workspace_bytes: unknown call %d", which);
-  *bytes = which == LMS_GATED_FWD ? 0 : 2 * grad_bytes(l);
+  const uint64_t fwd = up(dense_ws(DENSE_GATED, l.f32, l.m, l.n, l.k, 1, 2)), grads = grads_ws(l, true, true);
+  if (which == LMS_GATED_FWD) *bytes = fwd;
+  else *bytes = 2 * grad_bytes(l) + (which == LMS_GATED_BWD_RECOMPUTE && fwd > grads ? fwd : grads);
   return LMS_OK;
 }
 
@@ -281,6 +297,9 @@ lms_status gated_fwd(const lms_gated_desc* d, const void* x, const void* wg, con
   const void* all[] = {x, wg, wu, h, g, u};
   if (const lms_status st = aligned("lms_gated_fwd", l, all, 6)) return st;
   if (l.m == 0) return LMS_OK;
+  uint64_t need = 0;
+  gated_workspace(d, LMS_GATED_FWD, &need);
+  NEED(!need || ws, "lms_gated_fwd: workspace of %llu bytes required", (unsigned long long)need);
   DenseP p{};
   p.a[0] = x; p.b[0] = wg; p.b[1] = wu; p.out[0] = h;
   p.pre = g; p.pre1 = u;
@@ -288,7 +307,7 @@ lms_status gated_fwd(const lms_gated_desc* d, const void* x, const void* wg, con
   p.lda = l.ldx; p.ldb = l.ldw; p.ldo = l.ldy; p.ldr = l.ldy;
   p.segs = 1; p.srcs = 2; p.act = l.act;
   p.part = (float*)ws;
-  return done("lms_gated_fwd", product(DENSE_GATED, l.f32, p, (hipStream_t)stream));
+  return done("lms_gated_fwd", dense_product(DENSE_GATED, l.f32, p, (hipStream_t)stream));
 }
 
 lms_status gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, const void* wg, const void* wu, const void* g, const void* u, void* dx, void* dwg,
@@ -329,12 +348,13 @@ lms_status gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, con
     p.M = l.m; p.N = l.n; p.red = l.k;
     p.lda = l.ldx; p.ldb = l.ldw; p.ldo = ldz; p.ldr = l.ldy;
     p.segs = 1; p.srcs = 2; p.act = l.act;
-    e = product(DENSE_GATED, l.f32, p, s);
+    p.part = (float*)(at + 2 * grad_bytes(l));
+    e = dense_product(DENSE_GATED, l.f32, p, s);
   }
   if (e == hipSuccess) {
     const void* const w[] = {wg, wu};
     void* const dw[] = {dwg, dwu};
-    e = layer_grads(l, dz, ldz, x, w, dx, dw, s);
+    e = layer_grads(l, dz, ldz, x, w, dx, dw, (float*)(at + 2 * grad_bytes(l)), s);
   }
   return done("lms_gated_bwd", e);
 }
