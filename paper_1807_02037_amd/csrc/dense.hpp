@@ -41,6 +41,8 @@ hipError_t dense_product(int mode, bool f32, DenseP& p, hipStream_t s);
 uint64_t dense_ws(int mode, bool f32, long long M, int N, long long red, int segs, int srcs);
 
 hipError_t dense_bf16(int mode, DenseP& p, hipStream_t s);        // dense_gemm.hip
+uint64_t dense_bf16_ws(int mode, long long M, int N, long long red, int segs, int srcs);
+uint64_t dense_f32_ws(int mode, long long M, int N, long long red, int segs, int srcs);
 hipError_t dense_f32(int mode, DenseP& p, hipStream_t s);         // dense_f32.hip
 hipError_t dense_join(int mode, bool f32, DenseP& p, hipStream_t s);        // dense_join.hip: p.part into the results
 bool dense_few_ok(int mode, long long M);                         // few rows (dense_few.hip)
@@ -224,6 +226,7 @@ __device__ __forceinline__ void dense_epilogue(const DenseP& p, const f32x16 (&a
         if constexpr (MODE == DENSE_GATED) dense_part8(p, split, 1, row, n, cnt, u);
       } else dense_finish8<T, MODE>(p, src, row, n, cnt, v, u);
     }
+    __builtin_amdgcn_sched_barrier(0);                            // 32 rows after the other: together they are more than the registers hold
   }
 }
 

@@ -15,16 +15,17 @@ namespace lms {
 
 namespace {
 
-constexpr int FM = 128, FN = 128, FK = 32;
-constexpr int F_ROW = FK + 4, F_COL = FM + 8;                     // row pitches in LDS (floats): reads fall into different banks
-constexpr int F_TILE = FM * F_ROW > FK * F_COL ? FM * F_ROW : FK * F_COL;
-constexpr int F_LDS = 4 * F_TILE * 4;                             // two stages of two operands
-static_assert(F_LDS >= 4 * epi_wave_bytes(64) && 2 * F_LDS <= 163840, "epilogue, two work-groups a compute unit");
+constexpr int FK = 32, F_ROW = FK + 4;                            // reduction elements of a stage; row pitches in LDS (floats): reads fall into different banks
 
-template <int MODE>
-__global__ __launch_bounds__(256, 2) void dense_f32_kernel(DenseP p) {
+// A work-group computes FM x FM outputs, a wave FM / 2 x FM / 2.
+template <int MODE, int FM>
+__global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(DenseP p) {
   constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = MODE == DENSE_DX;
-  constexpr int OUT_N = MODE == DENSE_GATED ? FN / 2 : FN;
+  constexpr int FN = FM, OUT_N = MODE == DENSE_GATED ? FN / 2 : FN;
+  constexpr int W = FM / 2, TB = W / 32, EL = FM * FK / 256;      // extent of a wave, in blocks of 32; elements of a stage and operand per thread
+  constexpr int F_COL = FM + (FM == 128 ? 8 : 24);                // four rows apart: 32 banks further
+  constexpr int F_TILE = FM * F_ROW > FK * F_COL ? FM * F_ROW : FK * F_COL;
+  static_assert(16 * F_TILE >= 4 * epi_wave_bytes(W) && (FM == 128 ? 2 : 4) * 16 * F_TILE <= 163840, "two stages of two operands; epilogue; work-groups of a compute unit");
   __shared__ __attribute__((aligned(16))) float lds[4 * F_TILE];
 
   const int job = xcd_order(p.ntiles * p.splits);
@@ -44,10 +45,10 @@ __global__ __launch_bounds__(256, 2) void dense_f32_kernel(DenseP p) {
   const int half = lane >> 5, li = lane & 31;
 
   // Element j of this thread: along the extent, along the reduction.
-  auto e_of = [&](bool fast, int j) { return fast ? (tid >> 5) + 8 * j : tid & 127; };
-  auto r_of = [&](bool fast, int j) { return fast ? tid & 31 : (tid >> 7) + 2 * j; };
+  auto e_of = [&](bool fast, int j) { return fast ? (tid >> 5) + 8 * j : tid & (FM - 1); };
+  auto r_of = [&](bool fast, int j) { return fast ? tid & 31 : tid / FM + 256 / FM * j; };
   auto at = [](bool fast, int e, int r) { return fast ? e * F_ROW + r : r * F_COL + e; };
-  float ra[16], rb[16];
+  float ra[EL], rb[EL];
   auto pull = [&](int it) {
     int s = first + it;
     const bool second = MODE == DENSE_DX && p.segs == 2 && s >= seg_stages;
@@ -56,14 +57,14 @@ __global__ __launch_bounds__(256, 2) void dense_f32_kernel(DenseP p) {
     const float* a = (const float*)(second ? p.a[1] : p.a[0]);
     const float* b = (const float*)(second || (MODE == DENSE_DW && src) ? p.b[1] : p.b[0]);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
+    for (int j = 0; j < EL; ++j) {
       const long long e = m0 + e_of(A_FAST, j), r = r0 + r_of(A_FAST, j);
       const bool ok = e < p.M && r < p.red;
       const float v = a[ok ? (A_FAST ? e * p.lda + r : r * p.lda + e) : 0];
       ra[j] = ok ? v : 0.f;
     }
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
+    for (int j = 0; j < EL; ++j) {
       int c = e_of(B_FAST, j);
       const float* q = b;
       if (MODE == DENSE_GATED) {                                  // half of the tile's columns from each source
@@ -79,12 +80,12 @@ __global__ __launch_bounds__(256, 2) void dense_f32_kernel(DenseP p) {
   auto push = [&](int buf) {
     float* d = lds + buf * 2 * F_TILE;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) d[at(A_FAST, e_of(A_FAST, j), r_of(A_FAST, j))] = ra[j];
+    for (int j = 0; j < EL; ++j) d[at(A_FAST, e_of(A_FAST, j), r_of(A_FAST, j))] = ra[j];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) d[F_TILE + at(B_FAST, e_of(B_FAST, j), r_of(B_FAST, j))] = rb[j];
+    for (int j = 0; j < EL; ++j) d[F_TILE + at(B_FAST, e_of(B_FAST, j), r_of(B_FAST, j))] = rb[j];
   };
   // first column of the wave's block j within the tile
-  auto col = [&](int j) { return MODE == DENSE_GATED ? j * (FN / 2) + wn * 32 : wn * 64 + j * 32; };
+  auto col = [&](int j) { return MODE == DENSE_GATED ? j / (TB / 2 ? TB / 2 : 1) * (FN / 2) + wn * (W / 2) + j % (TB / 2 ? TB / 2 : 1) * 32 : wn * W + j * 32; };
   auto four = [&](bool fast, const float* t, int e, int s, float (&v)[4]) {
     if (fast) {
       const float4 q = *reinterpret_cast<const float4*>(t + e * F_ROW + 8 * s + 4 * half);
@@ -94,11 +95,11 @@ __global__ __launch_bounds__(256, 2) void dense_f32_kernel(DenseP p) {
       for (int u = 0; u < 4; ++u) v[u] = t[(8 * s + 4 * half + u) * F_COL + e];
   };
 
-  f32x16 acc[2][2];
+  f32x16 acc[TB][TB];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < TB; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < TB; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
@@ -110,49 +111,88 @@ __global__ __launch_bounds__(256, 2) void dense_f32_kernel(DenseP p) {
     const float* t = lds + (it & 1) * 2 * F_TILE;
 #pragma unroll
     for (int s = 0; s < FK / 8; ++s) {
-      float a[2][4], b[2][4];
+      float a[TB][4], b[TB][4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        four(A_FAST, t, wm * 64 + i * 32 + li, s, a[i]);
+      for (int i = 0; i < TB; ++i) {
+        four(A_FAST, t, wm * W + i * 32 + li, s, a[i]);
         four(B_FAST, t + F_TILE, col(i) + li, s, b[i]);
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < TB; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j][u], a[i][u], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j][u], a[i][u], acc[i][j], 0, 0, 0);
     }
     if (it + 1 < count) push((it + 1) & 1);
   }
   __syncthreads();
-  dense_epilogue<float, MODE, 64>(p, acc, reinterpret_cast<unsigned char*>(lds) + wave * epi_wave_bytes(64), m0 + wm * 64, n0 + wn * (MODE == DENSE_GATED ? 32 : 64), src, split);
+  dense_epilogue<float, MODE, W>(p, acc, reinterpret_cast<unsigned char*>(lds) + wave * epi_wave_bytes(W), m0 + wm * W, n0 + wn * (MODE == DENSE_GATED ? W / 2 : W), src, split);
 }
 
-template <int MODE>
+// Tile and splits, as in dense_gemm.hip; us of a stage of 32: one work-group on a compute unit, as many as it holds.
+struct F32Plan { int fm, splits; };
+struct F32Cost { int fm, per_cu; double alone, full; };
+constexpr F32Cost F32_COSTS[] = {{128, 2, 2.2, 3.6}, {64, 4, 0.8, 2.0}};
+
+F32Plan f32_plan(int mode, long long M, int N, long long red, int segs, int srcs) {
+  const long long stages = (red + FK - 1) / FK * segs;
+  F32Plan best = {128, 1};
+  double least = 1e300;
+  for (const F32Cost& t : F32_COSTS) {
+    if (mode == DENSE_GATED && t.fm == 64) continue;              // a wave needs columns of both sources
+    const int out_n = mode == DENSE_GATED ? t.fm / 2 : t.fm;
+    const long long tiles = (M + t.fm - 1) / t.fm * ((N + out_n - 1) / out_n) * (mode == DENSE_DW ? srcs : 1), slots = 256LL * t.per_cu;
+    for (int splits = 1; splits <= 16; ++splits) {
+      const long long per = (stages + splits - 1) / splits, jobs = tiles * splits, rounds = jobs / slots, rest = jobs - rounds * slots;
+      if (splits > 1 && per < 4) break;
+      double us = rounds * (per * t.full + 2.0) + (rest == 0 ? 0.0 : per * (t.alone + (t.full - t.alone) * ((double)(rest > 256 ? rest - 256 : 0) / slots)) + 2.0);
+      if (splits > 1) us += 3.0 + splits * (double)M * N * srcs * 2e-6;
+      if (us < least) { least = us; best = {t.fm, splits}; }
+    }
+  }
+  return best;
+}
+
+template <int MODE, int FM>
 hipError_t launch_f32(DenseP& p, hipStream_t s) {
-  const int out_n = MODE == DENSE_GATED ? FN / 2 : FN;
+  p.stages = (int)((p.red + FK - 1) / FK) * p.segs;
+  p.stages_per_split = (p.stages + p.splits - 1) / p.splits;
+  p.splits = (p.stages + p.stages_per_split - 1) / p.stages_per_split;
+  const int out_n = MODE == DENSE_GATED ? FM / 2 : FM;
   const long long tm = (p.M + FM - 1) / FM, tn = (long long)((p.N + out_n - 1) / out_n) * (MODE == DENSE_DW ? p.srcs : 1);
   if (tm * tn * p.splits > 0x7fffff00LL) return hipErrorInvalidValue;
   p.ntm = (int)tm;
   p.ntn = (int)tn;
   p.ntiles = (int)(tm * tn);
-  hipLaunchKernelGGL((dense_f32_kernel<MODE>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(256), 0, s, p);
-  return hipGetLastError();
+  hipLaunchKernelGGL((dense_f32_kernel<MODE, FM>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(256), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess && p.splits > 1 ? dense_join(MODE, true, p, s) : e;
+}
+
+template <int MODE>
+hipError_t f32_mode(DenseP& p, hipStream_t s) {
+  const F32Plan plan = f32_plan(MODE, p.M, p.N, p.red, p.segs, p.srcs);
+  p.splits = plan.splits;
+  if constexpr (MODE != DENSE_GATED)
+    if (plan.fm == 64) return launch_f32<MODE, 64>(p, s);
+  return launch_f32<MODE, 128>(p, s);
 }
 
 }  // namespace
 
 hipError_t dense_f32(int mode, DenseP& p, hipStream_t s) {
-  p.stages = (int)((p.red + FK - 1) / FK) * p.segs;
-  p.splits = 1;
-  p.stages_per_split = p.stages;
   switch (mode) {
-    case DENSE_FWD: return launch_f32<DENSE_FWD>(p, s);
-    case DENSE_GATED: return launch_f32<DENSE_GATED>(p, s);
-    case DENSE_DX: return launch_f32<DENSE_DX>(p, s);
-    default: return launch_f32<DENSE_DW>(p, s);
+    case DENSE_FWD: return f32_mode<DENSE_FWD>(p, s);
+    case DENSE_GATED: return f32_mode<DENSE_GATED>(p, s);
+    case DENSE_DX: return f32_mode<DENSE_DX>(p, s);
+    default: return f32_mode<DENSE_DW>(p, s);
   }
+}
+
+uint64_t dense_f32_ws(int mode, long long M, int N, long long red, int segs, int srcs) {
+  const int splits = f32_plan(mode, M, N, red, segs, srcs).splits;
+  return splits > 1 ? (uint64_t)splits * srcs * M * N * 4 : 0;
 }
 
 }  // namespace lms

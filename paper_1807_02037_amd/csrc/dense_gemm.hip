@@ -20,38 +20,38 @@ namespace lms {
 
 namespace {
 
-constexpr int DK = 64;               // reduction elements of a stage
-constexpr int NKS = DK / 16;         // steps of a stage: one 32x32x16 product per pair of operand fragments
-constexpr int DSL = DK / 8;          // 16-byte slots of a row of DK
-
-// 16-byte slots within a row of DK are permuted by this, and 64-byte blocks within a row of W columns by that, so that the rows a read touches at a
+// 16-byte slots within a row of DK reduction elements are permuted by this, and 64-byte blocks within a row of W columns by that, so that the rows a read touches at a
 // time fall into different banks.
-__device__ __forceinline__ int row_swz(int row) { return (row >> 1) & 7; }
+template <int DK>
+__device__ __forceinline__ int row_swz(int row) { return DK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 template <int W>
-__device__ __forceinline__ int col_swz(int r) { return W == 128 ? r & 3 : (r >> 1) & 1; }
+__device__ __forceinline__ int col_swz(int r) { return W == 128 ? r & 3 : W == 64 ? (r >> 1) & 1 : 0; }
 
-template <int BM_, int BN_>
+template <int BM_, int BN_, int DK_, int RING_, int WM_ = 2, int WN_ = 2>
 struct DenseTile {
-  static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2, NT = 256;
+  static constexpr int DK = DK_;                                  // reduction elements of a stage
+  static constexpr int RING = RING_;                              // stages in LDS
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NT = 256;
   static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
   static constexpr int A_BYTES = BM * DK * 2, B_BYTES = BN * DK * 2, STAGE = A_BYTES + B_BYTES;
   static constexpr int AV = A_BYTES / (16 * NT), BV = B_BYTES / (16 * NT);      // vectors of a stage per thread
   static constexpr int EPI_WAVE = epi_wave_bytes(WTN);
-  static constexpr int LDS_BYTES = 2 * STAGE > 4 * EPI_WAVE ? 2 * STAGE : 4 * EPI_WAVE;
+  static constexpr int LDS_BYTES = RING * STAGE > 4 * EPI_WAVE ? RING * STAGE : 4 * EPI_WAVE;
   static constexpr int OCC = 163840 / LDS_BYTES < 4 ? 163840 / LDS_BYTES : 4;   // work-groups of a compute unit, waves of a SIMD
 };
 
 // One operand's tile in LDS: EXT rows or columns of the result by DK of the reduction.
 //   RED_FAST: element (e, r) at base[e * ld + r]; in LDS rows e of DK.
 //   else:     element (e, r) at base[r * ld + e]; in LDS SUB columns wide pieces of rows r, one after the other.
-template <int EXT, bool RED_FAST, int SUB>
+template <int EXT, bool RED_FAST, int SUB, int DK>
 struct Operand {
+  static constexpr int NKS = DK / 16, DSL = DK / 8;     // steps of a stage: one 32x32x16 product per pair of operand fragments; 16-byte slots of a row of DK
   static constexpr int V = EXT * DK / (8 * 256);        // vectors per thread
   // Vector v: its element along the extent, and along the reduction.
   __device__ static __forceinline__ void where(int v, int& e, int& r) {
     if constexpr (RED_FAST) {
       e = v / DSL;
-      r = ((v % DSL) ^ row_swz(e)) * 8;
+      r = ((v % DSL) ^ row_swz<DK>(e)) * 8;
     } else {
       constexpr int VPR = SUB / 8;
       const int piece = v / (DK * VPR), w = v % (DK * VPR);
@@ -59,16 +59,30 @@ struct Operand {
       e = piece * SUB + (((w % VPR) >> 2) ^ col_swz<SUB>(r)) * 32 + (w & 3) * 8;
     }
   }
-  // LDS address of this lane's piece of the fragment of elements e0 .. e0+31 (e0: a multiple of 32) at step ks.
-  __device__ static __forceinline__ int address(int e0, int ks, int lane) {
+  // LDS address of this lane's piece of the fragment of elements e0 .. e0+31 (e0: a multiple of 32) at step ks: rd[] of N registers from prepare(), plus a constant.
+  static constexpr int N = RED_FAST ? NKS : EXT / 32;             // registers: of the steps, or of the fragments (at most)
+  __device__ static __forceinline__ int base(int e0, int ks, int lane) {
     if constexpr (RED_FAST) {
       const int row = e0 + (lane & 31);
-      return row * (DK * 2) + (((ks * 2 + (lane >> 5)) ^ row_swz(row)) << 4);
+      return row * (DK * 2) + (((ks * 2 + (lane >> 5)) ^ row_swz<DK>(row)) << 4);
     } else {
       const int li = lane & 15, lg = lane >> 4;
-      const int r = ks * 16 + 8 * (lg >> 1) + (li >> 2);
+      const int r = 8 * (lg >> 1) + (li >> 2);                    // + 16 ks, which the permutation does not see
       return (e0 / SUB) * (DK * SUB * 2) + r * (SUB * 2) + ((((e0 % SUB) >> 5) ^ col_swz<SUB>(r)) << 6) + 32 * (lg & 1) + 8 * (li & 3);
     }
+  }
+  template <int TILES, typename F>
+  __device__ static __forceinline__ void prepare(int (&rd)[N], int lane, F&& first) {
+    if constexpr (RED_FAST)
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) rd[ks] = base(first(0), ks, lane);
+    else
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) rd[i] = base(first(i), 0, lane);
+  }
+  __device__ static __forceinline__ int address(const int (&rd)[N], int i, int ks) {
+    if constexpr (RED_FAST) return rd[ks] + i * (32 * DK * 2);    // fragments of a wave follow one another: 32 rows further the permutation is the same
+    else return rd[i] + ks * (16 * SUB * 2);
   }
   __device__ static __forceinline__ bf16x8 fragment(const unsigned char* at) {
     if constexpr (RED_FAST) return *reinterpret_cast<const bf16x8*>(at);
@@ -92,8 +106,9 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
   constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = MODE == DENSE_DX;
   constexpr int BM = T::BM, BN = T::BN, TM = T::TM, TN = T::TN, AV = T::AV, BV = T::BV, SUB = dense_sub<MODE, BN>();
   constexpr int OUT_N = MODE == DENSE_GATED ? BN / 2 : BN;       // output columns of a tile
-  typedef Operand<BM, A_FAST, BM < 128 ? BM : 128> OpA;
-  typedef Operand<BN, B_FAST, SUB> OpB;
+  constexpr int DK = T::DK, NKS = DK / 16;
+  typedef Operand<BM, A_FAST, BM < 128 ? BM : 128, DK> OpA;
+  typedef Operand<BN, B_FAST, SUB, DK> OpB;
   extern __shared__ __attribute__((aligned(256))) unsigned char dense_smem[];
 
   const int job = xcd_order(p.ntiles * p.splits);
@@ -116,62 +131,71 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
   const int wm = wave / T::WN, wn = wave % T::WN;
 
   // ---- loads ----
-  const uint16_t* const a0 = (const uint16_t*)p.a[0];
-  const uint16_t* const b0 = (const uint16_t*)(MODE == DENSE_DW && src ? p.b[1] : p.b[0]);
-  const uint16_t* const a1 = (const uint16_t*)p.a[1];
-  const uint16_t* const b1 = (const uint16_t*)p.b[1];
+  const long long m_left = p.M - m0, n_left = (long long)p.N - n0;
   int a_e[AV], a_r[AV], b_e[BV], b_r[BV];                         // place of a vector in the tile; b_e of DENSE_GATED counts within a source
-  unsigned a_off[AV], b_off[BV];
 #pragma unroll
-  for (int j = 0; j < AV; ++j) {
-    OpA::where(tid + j * 256, a_e[j], a_r[j]);
-    a_off[j] = m0 + a_e[j] < p.M ? (unsigned)((A_FAST ? a_e[j] * p.lda + a_r[j] : a_r[j] * p.lda + a_e[j]) * 2) : DMA_OOB;
-  }
+  for (int j = 0; j < AV; ++j) OpA::where(tid + j * 256, a_e[j], a_r[j]);
 #pragma unroll
   for (int j = 0; j < BV; ++j) {
     OpB::where(tid + j * 256, b_e[j], b_r[j]);
     if (MODE == DENSE_GATED) b_e[j] %= SUB;
-    b_off[j] = n0 + b_e[j] < p.N ? (unsigned)((B_FAST ? b_e[j] * p.ldb + b_r[j] : b_r[j] * p.ldb + b_e[j]) * 2) : DMA_OOB;
   }
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)dense_smem + wave * 1024);
-  const long long a_end = A_FAST ? (p.M - 1) * p.lda + p.red : (p.red - 1) * p.lda + p.M;     // elements of a segment
-  const long long b_end = B_FAST ? (long long)(p.N - 1) * p.ldb + p.red : (p.red - 1) * p.ldb + p.N;
+  struct Source { const uint16_t *a, *b, *bu; };
+  // the operands at reduction element r of a segment
+  auto source = [&](int seg, long long r) {
+    const long long ao = A_FAST ? m0 * p.lda + r : r * p.lda + m0, bo = B_FAST ? n0 * p.ldb + r : r * p.ldb + n0;
+    const int bs = MODE == DENSE_DX ? seg : MODE == DENSE_DW ? src : 0;
+    return Source{(const uint16_t*)p.a[MODE == DENSE_DX ? seg : 0] + ao, (const uint16_t*)p.b[bs] + bo, MODE == DENSE_GATED ? (const uint16_t*)p.b[1] + bo : nullptr};
+  };
 
-  // stage `it` of this work-group: reduction elements r0 .. r0+63 of a segment
-  struct At { const uint16_t *a, *b, *bu; long long a_left, b_left; long long r0; bool whole; };
-  auto stage_at = [&](int it) {
-    int s = first + it;
-    bool second = false;
-    if (MODE == DENSE_DX && s >= seg_stages && p.segs == 2) { s -= seg_stages; second = true; }
-    At t;
-    t.r0 = (long long)s * DK;
-    const long long ao = A_FAST ? m0 * p.lda + t.r0 : t.r0 * p.lda + m0, bo = B_FAST ? n0 * p.ldb + t.r0 : t.r0 * p.ldb + n0;
-    t.a = (second ? a1 : a0) + ao;
-    t.b = (second ? b1 : b0) + bo;
-    t.bu = MODE == DENSE_GATED ? b1 + bo : nullptr;
-    t.whole = t.r0 + DK <= p.red;
-    t.a_left = it < count ? (a_end - ao) * 2 : 0;                 // beyond the last stage: nothing but zeros
-    t.b_left = it < count ? (b_end - bo) * 2 : 0;
-    return t;
-  };
-  auto clip = [](long long bytes) { return bytes < 0 ? 0 : bytes; };
-  // buffer loads that write LDS
-  auto dma_a = [&](const At& t, const v4u& rs, int buf, int j) {
-    const bool in = !A_FAST || t.whole || t.r0 + a_r[j] < p.red;  // otherwise the rows beyond the last lie beyond the buffer
-    load_lds16(rs, lds0 + buf * T::STAGE + j * 4096, in ? a_off[j] : DMA_OOB, 0);
-  };
-  auto dma_b = [&](const At& t, const v4u& rs, int buf, int j) {
-    const bool in = !B_FAST || t.whole || t.r0 + b_r[j] < p.red;
-    load_lds16(rs, lds0 + buf * T::STAGE + T::A_BYTES + j * 4096, in ? b_off[j] : DMA_OOB, 0);
-  };
-  auto fetch = [&](int it, int buf) {
-    const At t = stage_at(it);
-    const v4u rs_a = buffer_rsrc(t.a, clip(t.a_left)), rs_b = buffer_rsrc(t.b, clip(t.b_left));
-    const v4u rs_u = MODE == DENSE_GATED ? buffer_rsrc(t.bu, clip(t.b_left)) : rs_b;
+  // Buffer loads that write LDS.  The descriptors move along the reduction with the stages; the vectors' offsets from them stay, those of rows or columns that do not
+  // exist beyond every buffer.  The last stage of a segment may be partial: there the vectors beyond the end are moved out as well, or lie beyond the buffer.
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)dense_smem + wave * 1024);
+  unsigned a_off[DMA ? AV : 1], b_off[DMA ? BV : 1];
+  v4u rs_a = {}, rs_b = {}, rs_u = {};
+  int to_load = count, load_seg = 0;                              // stages not asked for yet
+  long long load_r = 0;
+  auto enter = [&](int seg, long long r) {                        // the next stage is of segment seg, element r
+    load_seg = seg;
+    load_r = r;
+    const Source t = source(seg, r);
+    rs_a = buffer_rsrc(t.a, 0x7fffffff);
+    rs_b = buffer_rsrc(t.b, 0x7fffffff);
+    if (MODE == DENSE_GATED) rs_u = buffer_rsrc(t.bu, 0x7fffffff);
 #pragma unroll
-    for (int j = 0; j < AV; ++j) dma_a(t, rs_a, buf, j);
+    for (int j = 0; j < AV; ++j) a_off[j] = a_e[j] < m_left ? (unsigned)((A_FAST ? a_e[j] * p.lda + a_r[j] : a_r[j] * p.lda + a_e[j]) * 2) : DMA_OOB;
 #pragma unroll
-    for (int j = 0; j < BV; ++j) dma_b(t, MODE == DENSE_GATED && j >= BV / 2 ? rs_u : rs_b, buf, j);
+    for (int j = 0; j < BV; ++j) b_off[j] = b_e[j] < n_left ? (unsigned)((B_FAST ? b_e[j] * p.ldb + b_r[j] : b_r[j] * p.ldb + b_e[j]) * 2) : DMA_OOB;
+  };
+  auto last = [&]() {                                             // the next stage is partial
+#pragma unroll
+    for (int j = 0; j < AV; ++j) a_off[j] = load_r + a_r[j] < p.red ? a_off[j] : DMA_OOB;
+#pragma unroll
+    for (int j = 0; j < BV; ++j) b_off[j] = load_r + b_r[j] < p.red ? b_off[j] : DMA_OOB;
+  };
+  auto advance = [&]() {
+    if (--to_load <= 0) {                                         // beyond the last: nothing but zeros
+      rs_a[2] = rs_b[2] = rs_u[2] = 0;
+      return;
+    }
+    load_r += DK;
+    if (MODE == DENSE_DX && load_r >= p.red) enter(1, 0);
+    else {
+      auto move = [](v4u& rs, long long bytes) {
+        const unsigned long long base = ((unsigned long long)rs[1] << 32 | rs[0]) + bytes;
+        rs[0] = (unsigned)base;
+        rs[1] = (unsigned)(base >> 32);
+      };
+      move(rs_a, (A_FAST ? DK : DK * p.lda) * 2);
+      move(rs_b, (B_FAST ? DK : DK * p.ldb) * 2);
+      if (MODE == DENSE_GATED) move(rs_u, DK * p.ldb * 2);
+    }
+    if (load_r + DK > p.red) last();
+  };
+  constexpr int LOADS = AV + BV;
+  auto load = [&](unsigned at, int v) {                           // load v of a stage into the buffer at `at`
+    if (v < AV) load_lds16(rs_a, lds0 + at + v * 4096, a_off[v < AV ? v : 0], 0);
+    else load_lds16(MODE == DENSE_GATED && v - AV >= BV / 2 ? rs_u : rs_b, lds0 + at + T::A_BYTES + (v - AV) * 4096, b_off[v < AV ? 0 : v - AV], 0);
   };
   // through registers, at any address
   v4u ra[DMA ? 1 : AV], rb[DMA ? 1 : BV];
@@ -185,15 +209,17 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
     return v;
   };
   auto pull = [&](int it) {
-    const At t = stage_at(it);
+    const int st = first + it, seg = MODE == DENSE_DX && st >= seg_stages ? 1 : 0;
+    const long long r0 = (long long)(st - seg * seg_stages) * DK;
+    const Source t = source(seg, r0);
 #pragma unroll
     for (int j = 0; j < AV; ++j) {
-      const long long red = p.red - t.r0 - a_r[j], ext = p.M - m0 - a_e[j];
+      const long long red = p.red - r0 - a_r[j], ext = m_left - a_e[j];
       ra[j] = vector(t.a + (A_FAST ? a_e[j] * p.lda + a_r[j] : a_r[j] * p.lda + a_e[j]), red > 0 && ext > 0 ? (A_FAST ? red : ext) : 0);
     }
 #pragma unroll
     for (int j = 0; j < BV; ++j) {
-      const long long red = p.red - t.r0 - b_r[j], ext = (long long)p.N - n0 - b_e[j];
+      const long long red = p.red - r0 - b_r[j], ext = n_left - b_e[j];
       rb[j] = vector((MODE == DENSE_GATED && j >= BV / 2 ? t.bu : t.b) + (B_FAST ? b_e[j] * p.ldb + b_r[j] : b_r[j] * p.ldb + b_e[j]),
                      red > 0 && ext > 0 ? (B_FAST ? red : ext) : 0);
     }
@@ -206,16 +232,11 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
     for (int j = 0; j < BV; ++j) *reinterpret_cast<v4u*>(d + T::A_BYTES + j * 4096) = rb[j];
   };
 
-  // ---- LDS read addresses ----
-  int a_rd[TM][NKS], b_rd[TN][NKS];
-#pragma unroll
-  for (int ks = 0; ks < NKS; ++ks) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) a_rd[i][ks] = OpA::address(wm * T::WTM + i * 32, ks, lane);
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-      b_rd[j][ks] = T::A_BYTES + OpB::address(MODE == DENSE_GATED ? (j / (TN / 2)) * SUB + (wn * (TN / 2) + j % (TN / 2)) * 32 : wn * T::WTN + j * 32, ks, lane);
-  }
+  int a_rd[OpA::N], b_rd[OpB::N];
+  OpA::template prepare<TM>(a_rd, lane, [&](int i) { return wm * T::WTM + i * 32; });
+  OpB::template prepare<TN>(b_rd, lane, [&](int j) {
+    return MODE == DENSE_GATED ? (j / (TN / 2)) * SUB + (wn * (TN / 2) + j % (TN / 2)) * 32 : wn * T::WTN + j * 32;
+  });
 
   f32x16 acc[TM][TN];
 #pragma unroll
@@ -224,37 +245,78 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  bf16x8 af[2][TM], bf[2][TN];                                    // operands are read one step ahead of their products
+  auto read = [&](const unsigned char* t, int ks, int f) {        // fragment f of step ks
+    if (f < TN) bf[ks & 1][f] = OpB::fragment(t + T::A_BYTES + OpB::address(b_rd, f, ks));
+    else af[ks & 1][f - TN] = OpA::fragment(t + OpA::address(a_rd, f - TN, ks));
+  };
+  auto product = [&](int ks, int q) {
+    const int i = q / TN, j = q % TN;
+    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][j], af[ks & 1][i], acc[i][j], 0, 0, 0);
+  };
   auto multiply = [&](int buf) {
     const unsigned char* t = dense_smem + buf * T::STAGE;
-    bf16x8 af[2][TM], bf[2][TN];
-    auto load = [&](int ks) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) bf[ks & 1][j] = OpB::fragment(t + b_rd[j][ks]);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) af[ks & 1][i] = OpA::fragment(t + a_rd[i][ks]);
-    };
-    load(0);
+    for (int f = 0; f < TM + TN; ++f) read(t, 0, f);
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) {
-      if (ks + 1 < NKS) load(ks + 1);
+      if (ks + 1 < NKS)
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int f = 0; f < TM + TN; ++f) read(t, ks + 1, f);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][j], af[ks & 1][i], acc[i][j], 0, 0, 0);
+      for (int q = 0; q < TM * TN; ++q) product(ks, q);
     }
   };
 
   if constexpr (DMA) {
-    fetch(0, 0);
-    for (int it = 0; it < count; it += 2) {
-      unrolled<2>([&](auto k) {
-        constexpr int buf = decltype(k)::value;
-        if (it + buf >= count) return;
-        wait_barrier<0>();                                        // this stage has landed, and every wave is done with the other buffer
-        fetch(it + buf + 1, buf ^ 1);
-        multiply(buf);
-      });
+    // The last step of a stage has its operands in registers before it begins, so the barrier stands in front of it: there every wave is done with this buffer, and
+    // the next stage has landed.  From there to the next barrier the loads of the stage RING further go out into this buffer, spread between the
+    // products (in a row they fill the queue of the address unit and the products behind them wait), and the next stage's first operands are
+    // read: the matrix cores wait for nothing but the waves' skew at the barrier.
+    constexpr int SLOTS = NKS * TM * TN;                          // products of a stage, counted from the barrier
+    constexpr int EARLY = (TM * TN * LOADS + SLOTS - 1) / SLOTS;  // loads of the step behind the barrier
+    {
+      const int seg = MODE == DENSE_DX && first >= seg_stages ? 1 : 0;
+      enter(seg, (long long)(first - seg * seg_stages) * DK);
+      if (load_r + DK > p.red) last();
     }
+#pragma unroll
+    for (int it = 0; it < T::RING; ++it) {
+      if (it) advance();
+#pragma unroll
+      for (int v = 0; v < (it == T::RING - 1 ? EARLY : LOADS); ++v) load(it * T::STAGE, v);
+    }
+    wait_barrier<(T::RING - 2) * LOADS + EARLY>();
+#pragma unroll
+    for (int f = 0; f < TM + TN; ++f) read(dense_smem, 0, f);
+    int it = 0;
+    unsigned at = 0, pat = (T::RING - 1) * T::STAGE;              // this stage's buffer, and the last one's
+    do {                                                          // at least one stage
+      const unsigned nat = at + T::STAGE < T::RING * T::STAGE ? at + T::STAGE : 0;
+      const unsigned char *t = dense_smem + at, *next = dense_smem + nat;
+      unrolled<NKS>([&](auto s) {
+        constexpr int ks = decltype(s)::value;
+        if constexpr (ks == NKS - 1) {
+          advance();
+          wait_barrier<(T::RING - 2) * LOADS>();
+        }
+#pragma unroll
+        for (int q = 0; q < TM * TN; ++q) {
+          constexpr int from = (ks + 1) % NKS * TM * TN;          // slot of q = 0
+          product(ks, q);
+          if (q < TM + TN) read(ks == NKS - 1 ? next : t, (ks + 1) % NKS, q);
+#pragma unroll
+          for (int v = 0; v < LOADS; ++v)
+            if (v * SLOTS / LOADS == from + q) load(ks == NKS - 1 ? at : pat, v);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (TM + TN > TM * TN)
+#pragma unroll
+          for (int f = TM * TN; f < TM + TN; ++f) read(ks == NKS - 1 ? next : t, (ks + 1) % NKS, f);
+      });
+      pat = at;
+      at = nat;
+    } while (++it < count);
     wait_loads();
   } else {
     pull(0);
@@ -274,6 +336,9 @@ template <typename T, int MODE, bool DMA>
 hipError_t launch_dense(DenseP& p, hipStream_t s) {
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(dense_kernel<T, MODE, DMA>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
   if (attr != hipSuccess) return attr;
+  p.stages = (int)((p.red + T::DK - 1) / T::DK) * p.segs;
+  p.stages_per_split = (p.stages + p.splits - 1) / p.splits;
+  p.splits = (p.stages + p.stages_per_split - 1) / p.stages_per_split;      // none without a stage
   const int out_n = MODE == DENSE_GATED ? T::BN / 2 : T::BN;
   const long long tm = (p.M + T::BM - 1) / T::BM, tn = (long long)((p.N + out_n - 1) / out_n) * (MODE == DENSE_DW ? p.srcs : 1);
   if (tm * tn * p.splits > 0x7fffff00LL) return hipErrorInvalidValue;
@@ -284,7 +349,55 @@ hipError_t launch_dense(DenseP& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-typedef DenseTile<128, 128> Tile128;
+// Deep rings hide what a stage takes to arrive where there is one work-group on a compute unit; two work-groups hide each other's.
+typedef DenseTile<256, 256, 32, 4> Tile256;
+typedef DenseTile<128, 128, 64, 2> Tile128;
+typedef DenseTile<128, 128, 64, 5> Tile128D;
+typedef DenseTile<64, 128, 64, 3> Tile64x128;
+typedef DenseTile<64, 64, 64, 5> Tile64;
+typedef DenseTile<32, 128, 64, 4, 1, 4> Tile32;
+enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
+
+// Tile and splits of a reduction, from the sizes alone (workspaces are planned before there are addresses), by an estimate of the time: rounds of work-groups
+// through the compute units, stages of 64 of the reduction each, and for splits the join's launch (3 us) and its passes over the sums (4 TB/s).  us of a stage, measured
+// where a work-group is alone on its compute unit and where all units hold as many as they can (forward, bf16, rows x inputs x outputs):
+//                  alone            full
+//   256 x 256      1.7              1.8      8192 x 65536 x 4096
+//   128 x 128      0.86 (two stages ahead at most)   1.16     64 x 4096 x 4096, 2048 x 4096 x 4096
+//   the same, deep 0.50             0.65     1024 x 2048 x 4096
+//   64 x 128       0.48             0.80     512 x 4096 x 4096, 1024 x 2048 x 4096
+//   64 x 64        0.33             0.52     64 x 4096 x 4096, 512 x 4096 x 4096
+//   32 x 128       0.38             0.62
+// us by tile and splits, of which it takes the starred:
+//                         128 x 128: 1    2      4      8     deep: 1  2      4     64 x 128: 1  2     4      64 x 64: 1  2      4
+//   24 x 2048 x 8192             30.9   21.3   15.7   16.7    18.9   16.1   14.9       18.8   15.8   13.9*      14.3   14.6   15.5
+//   256 x 2048 x 2048            26.0   17.8   14.9   16.9    19.9   15.6   14.1       16.3   13.9   13.4       12.8*  12.7   13.6
+//   512 x 4096 x 4096            61.8   42.2   39.2   51.2    42.9   34.2   43.9       36.0*  39.1   47.1       40.6   47.9   56.1
+//   1024 x 2048 x 4096           36.2   38.4   52.7   83.4    27.5*  44.3   62.7       31.2   45.9   61.8       40.0   54.1   70.5
+//   2048 x 4096 x 4096           79.5*  107    137    192     85.8   118    164        102    129    148        129    153    173
+struct DensePlan { int tile, splits; };
+struct TileCost { int tile, bm, bn, per_cu; float alone, full; };
+constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.7f, 1.8f}, {TILE_128, 128, 128, 2, 0.86f, 1.16f}, {TILE_128D, 128, 128, 1, 0.50f, 0.65f},
+                              {TILE_64X128, 64, 128, 2, 0.48f, 0.80f}, {TILE_64, 64, 64, 2, 0.33f, 0.52f}, {TILE_32, 32, 128, 2, 0.38f, 0.62f}};
+
+DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int srcs) {
+  const long long stages = (red + 63) / 64 * segs;
+  DensePlan best = {TILE_128, 1};
+  double least = 1e300;
+  for (const TileCost& t : COSTS) {
+    if (mode == DENSE_GATED && (t.tile == TILE_64 || t.tile == TILE_32)) continue;     // a wave needs columns of both sources
+    const int out_n = mode == DENSE_GATED ? t.bn / 2 : t.bn;
+    const long long tiles = (M + t.bm - 1) / t.bm * ((N + out_n - 1) / out_n) * (mode == DENSE_DW ? srcs : 1), slots = 256LL * t.per_cu;
+    for (int splits = 1; splits <= 16; ++splits) {
+      const long long per = (stages + splits - 1) / splits, jobs = tiles * splits, rounds = jobs / slots, rest = jobs - rounds * slots;
+      if (splits > 1 && per < 2) break;
+      double us = rounds * (per * (double)t.full + 2.0) + (rest == 0 ? 0.0 : per * (double)(rest > 256 ? t.full : t.alone) + 2.0);
+      if (splits > 1) us += 3.0 + splits * (double)M * N * srcs * 2e-6;
+      if (us < least) { least = us; best = {t.tile, splits}; }
+    }
+  }
+  return best;
+}
 
 // Loads that write LDS need whole 16-byte vectors: addresses and pitches in multiples of 8 elements, and lengths too, since a vector across the end of a row
 // would bring in what lies behind it.  32-bit offsets within a tile bound the pitch.
@@ -298,21 +411,34 @@ bool dma_ok(int mode, const DenseP& p) {
 
 template <int MODE>
 hipError_t dense_mode(DenseP& p, hipStream_t s) {
-  return dma_ok(MODE, p) ? launch_dense<Tile128, MODE, true>(p, s) : launch_dense<Tile128, MODE, false>(p, s);
+  const DensePlan plan = dense_plan(MODE, p.M, p.N, p.red, p.segs, p.srcs);
+  p.splits = plan.splits;
+  hipError_t e;
+  if (!dma_ok(MODE, p)) e = plan.tile <= TILE_128D ? launch_dense<Tile128, MODE, false>(p, s) : launch_dense<Tile64x128, MODE, false>(p, s);
+  else if (plan.tile == TILE_256) e = launch_dense<Tile256, MODE, true>(p, s);
+  else if (plan.tile == TILE_128) e = launch_dense<Tile128, MODE, true>(p, s);
+  else if (plan.tile == TILE_128D) e = launch_dense<Tile128D, MODE, true>(p, s);
+  else if constexpr (MODE == DENSE_GATED) e = launch_dense<Tile64x128, MODE, true>(p, s);
+  else if (plan.tile == TILE_64X128) e = launch_dense<Tile64x128, MODE, true>(p, s);
+  else if (plan.tile == TILE_64) e = launch_dense<Tile64, MODE, true>(p, s);
+  else e = launch_dense<Tile32, MODE, true>(p, s);
+  return e == hipSuccess && p.splits > 1 ? dense_join(MODE, false, p, s) : e;
 }
 
 }  // namespace
 
 hipError_t dense_bf16(int mode, DenseP& p, hipStream_t s) {
-  p.stages = (int)((p.red + DK - 1) / DK) * p.segs;
-  p.splits = 1;
-  p.stages_per_split = p.stages;
   switch (mode) {
     case DENSE_FWD: return dense_mode<DENSE_FWD>(p, s);
     case DENSE_GATED: return dense_mode<DENSE_GATED>(p, s);
     case DENSE_DX: return dense_mode<DENSE_DX>(p, s);
     default: return dense_mode<DENSE_DW>(p, s);
   }
+}
+
+uint64_t dense_bf16_ws(int mode, long long M, int N, long long red, int segs, int srcs) {
+  const int splits = dense_plan(mode, M, N, red, segs, srcs).splits;
+  return splits > 1 ? (uint64_t)splits * srcs * M * N * 4 : 0;
 }
 
 }  // namespace lms
