@@ -8,6 +8,7 @@
 // The matrix cores bound it; see dense_f32.
 #include <hip/hip_runtime.h>
 
+#include "conv_tile.hpp"
 #include "dense.hpp"
 #include "kernels.hpp"
 
@@ -18,12 +19,13 @@ namespace {
 constexpr int FK = 32, F_ROW = FK + 4;                            // reduction elements of a stage; row pitches in LDS (floats): reads fall into different banks
 
 // A work-group computes FM x FM outputs, a wave FM / 2 x FM / 2.
-template <int MODE, int FM>
+// WIDE: pitches beyond 32-bit offsets within a tile; else loads by buffers, beyond whose end they give zeros.
+template <int MODE, int FM, bool WIDE>
 __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(DenseP p) {
   constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = MODE == DENSE_DX;
   constexpr int FN = FM, OUT_N = MODE == DENSE_GATED ? FN / 2 : FN;
   constexpr int W = FM / 2, TB = W / 32, EL = FM * FK / 256;      // extent of a wave, in blocks of 32; elements of a stage and operand per thread
-  constexpr int F_COL = FM + (FM == 128 ? 8 : 24);                // four rows apart: 32 banks further
+  constexpr int F_COL = FM + 8;                                    // four rows apart: 32 banks further
   constexpr int F_TILE = FM * F_ROW > FK * F_COL ? FM * F_ROW : FK * F_COL;
   static_assert(16 * F_TILE >= 4 * epi_wave_bytes(W) && (FM == 128 ? 2 : 4) * 16 * F_TILE <= 163840, "two stages of two operands; epilogue; work-groups of a compute unit");
   __shared__ __attribute__((aligned(16))) float lds[4 * F_TILE];
@@ -49,6 +51,14 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
   auto r_of = [&](bool fast, int j) { return fast ? tid & 31 : tid / FM + 256 / FM * j; };
   auto at = [](bool fast, int e, int r) { return fast ? e * F_ROW + r : r * F_COL + e; };
   float ra[EL], rb[EL];
+  const unsigned none = DMA_OOB;
+  // bytes of an element's row step, and of this thread's first element of a tile
+  const long long a_step = (A_FAST ? 8 : 256 / FM) * p.lda * 4, b_step = (B_FAST ? 8 : 256 / FM) * p.ldb * 4;
+  const int be = MODE == DENSE_GATED ? e_of(B_FAST, 0) & (FN / 2 - 1) : e_of(B_FAST, 0);
+  const unsigned a_at = (unsigned)((A_FAST ? e_of(true, 0) * p.lda + r_of(true, 0) : r_of(false, 0) * p.lda + e_of(false, 0)) * 4);
+  const unsigned b_at = (unsigned)((B_FAST ? e_of(true, 0) * p.ldb + r_of(true, 0) : r_of(false, 0) * p.ldb + be) * 4);
+  const long long a_end = A_FAST ? (p.M - 1) * p.lda + p.red : (p.red - 1) * p.lda + p.M;     // elements of a segment
+  const long long b_end = B_FAST ? (long long)(p.N - 1) * p.ldb + p.red : (p.red - 1) * p.ldb + p.N;
   auto pull = [&](int it) {
     int s = first + it;
     const bool second = MODE == DENSE_DX && p.segs == 2 && s >= seg_stages;
@@ -56,6 +66,31 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
     const long long r0 = (long long)s * FK;
     const float* a = (const float*)(second ? p.a[1] : p.a[0]);
     const float* b = (const float*)(second || (MODE == DENSE_DW && src) ? p.b[1] : p.b[0]);
+    if constexpr (!WIDE) {
+      const long long ao = A_FAST ? m0 * p.lda + r0 : r0 * p.lda + m0, bo = B_FAST ? n0 * p.ldb + r0 : r0 * p.ldb + n0;
+      auto rsrc = [](const float* q, long long left) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(q), 0, (int)(left < 0x1fffffff ? left * 4 : 0x7ffffffc), 0x00020000);
+      };
+      const auto rs_a = rsrc(a + ao, a_end - ao), rs_b = rsrc(b + bo, b_end - bo), rs_u = rsrc(MODE == DENSE_GATED ? (const float*)p.b[1] + bo : b, b_end - bo);
+      // what lies behind the end of a row is not beyond the buffer: along the reduction, or along the extent
+      const unsigned av = (A_FAST ? r0 + r_of(true, 0) < p.red : m0 + e_of(false, 0) < p.M) ? a_at : none;
+      const unsigned bv = (B_FAST ? r0 + r_of(true, 0) < p.red : n0 + be < p.N) ? b_at : none;
+#pragma unroll
+      for (int j = 0; j < EL; ++j) ra[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_a, (int)(av + j * (unsigned)a_step), 0, 0));
+      if constexpr (MODE == DENSE_GATED) {                        // half of the tile's columns, whole waves, from each source
+        static_assert(FN / 2 >= 64 || MODE != DENSE_GATED, "a wave's columns are of one source");
+        const bool up = __builtin_amdgcn_readfirstlane(e_of(false, 0)) >= FN / 2;
+        if (up)
+#pragma unroll
+          for (int j = 0; j < EL; ++j) rb[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_u, (int)(bv + j * (unsigned)b_step), 0, 0));
+        else
+#pragma unroll
+          for (int j = 0; j < EL; ++j) rb[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_b, (int)(bv + j * (unsigned)b_step), 0, 0));
+      } else
+#pragma unroll
+        for (int j = 0; j < EL; ++j) rb[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_b, (int)(bv + j * (unsigned)b_step), 0, 0));
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < EL; ++j) {
       const long long e = m0 + e_of(A_FAST, j), r = r0 + r_of(A_FAST, j);
@@ -67,7 +102,7 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
     for (int j = 0; j < EL; ++j) {
       int c = e_of(B_FAST, j);
       const float* q = b;
-      if (MODE == DENSE_GATED) {                                  // half of the tile's columns from each source
+      if (MODE == DENSE_GATED) {
         if (c >= FN / 2) q = (const float*)p.b[1];
         c &= FN / 2 - 1;
       }
@@ -154,7 +189,7 @@ F32Plan f32_plan(int mode, long long M, int N, long long red, int segs, int srcs
   return best;
 }
 
-template <int MODE, int FM>
+template <int MODE, int FM, bool WIDE>
 hipError_t launch_f32(DenseP& p, hipStream_t s) {
   p.stages = (int)((p.red + FK - 1) / FK) * p.segs;
   p.stages_per_split = (p.stages + p.splits - 1) / p.splits;
@@ -165,7 +200,7 @@ hipError_t launch_f32(DenseP& p, hipStream_t s) {
   p.ntm = (int)tm;
   p.ntn = (int)tn;
   p.ntiles = (int)(tm * tn);
-  hipLaunchKernelGGL((dense_f32_kernel<MODE, FM>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((dense_f32_kernel<MODE, FM, WIDE>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(256), 0, s, p);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess && p.splits > 1 ? dense_join(MODE, true, p, s) : e;
 }
@@ -174,9 +209,10 @@ template <int MODE>
 hipError_t f32_mode(DenseP& p, hipStream_t s) {
   const F32Plan plan = f32_plan(MODE, p.M, p.N, p.red, p.segs, p.srcs);
   p.splits = plan.splits;
+  if (p.lda >= 1 << 21 || p.ldb >= 1 << 21) return launch_f32<MODE, 128, true>(p, s);
   if constexpr (MODE != DENSE_GATED)
-    if (plan.fm == 64) return launch_f32<MODE, 64>(p, s);
-  return launch_f32<MODE, 128>(p, s);
+    if (plan.fm == 64) return launch_f32<MODE, 64, false>(p, s);
+  return launch_f32<MODE, 128, false>(p, s);
 }
 
 }  // namespace

@@ -267,6 +267,26 @@ def test_rows_beyond_32_bit_offsets():
     near(dw, wdw, e_dw, "dw")
 
 
+def test_wide_pitches_in_fp32():
+    """Rows of 2^21 elements and more, whose tiles have no 32-bit offsets."""
+    torch, L, A = setup()
+    m, k, n, pitch = 150, 40, 72, (1 << 21) + 3
+    big = torch.empty(m * pitch, device="cuda")
+    x, y, dx = (big.as_strided((m, c), (pitch, 1), at) for c, at in ((k, 0), (n, 1000), (k, 5000)))
+    x.copy_(matrix(torch, 1, m, k, torch.float32))
+    w = matrix(torch, 2, k, n, torch.float32)
+    d = L.linear_desc(m, n, k, dtype=A.F32, ldx=pitch, ldy=pitch)
+    ws = space(torch, max(L.linear_workspace_bytes(d, A.LINEAR_FWD), L.linear_workspace_bytes(d, A.LINEAR_BWD)))
+    L.linear_fwd(d, ptr(x), ptr(w), None, None, ptr(y), None, ptr(ws), stream(torch))
+    want, _, e, _ = O.linear_fwd("none", O.f64(x), O.f64(w), None, None, torch.float32)
+    near(y, want, e, "y")
+    dw = out(torch, k, n, torch.float32)
+    L.linear_bwd(d, ptr(y), ptr(x), ptr(w), None, ptr(dx), ptr(dw), None, ptr(ws), stream(torch))
+    wdx, e_dx, wdw, e_dw, _, _ = O.linear_bwd("none", O.f64(y), O.f64(x), O.f64(w), None, torch.float32, torch.float32)
+    near(dx, wdx, e_dx, "dx")
+    near(dw, wdw, e_dw, "dw")
+
+
 def test_replays_of_a_captured_step():
     """Forward and backward captured into a graph, replayed between eager work: each replay has the eager bits for its inputs."""
     torch, L, A = setup()
