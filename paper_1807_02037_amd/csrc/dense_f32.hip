@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
   auto e_of = [&](bool fast, int j) { return fast ? (tid >> 5) + 8 * j : tid & (FM - 1); };
   auto r_of = [&](bool fast, int j) { return fast ? tid & 31 : tid / FM + 256 / FM * j; };
   auto at = [](bool fast, int e, int r) { return fast ? e * F_ROW + r : r * F_COL + e; };
-  float ra[EL], rb[EL];
+  float ra[2][EL], rb[2][EL];                                     // stages are asked for two ahead
   const unsigned none = DMA_OOB;
   // bytes of an element's row step, and of this thread's first element of a tile
   const long long a_step = (A_FAST ? 8 : 256 / FM) * p.lda * 4, b_step = (B_FAST ? 8 : 256 / FM) * p.ldb * 4;
@@ -59,7 +59,8 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
   const unsigned b_at = (unsigned)((B_FAST ? e_of(true, 0) * p.ldb + r_of(true, 0) : r_of(false, 0) * p.ldb + be) * 4);
   const long long a_end = A_FAST ? (p.M - 1) * p.lda + p.red : (p.red - 1) * p.lda + p.M;     // elements of a segment
   const long long b_end = B_FAST ? (long long)(p.N - 1) * p.ldb + p.red : (p.red - 1) * p.ldb + p.N;
-  auto pull = [&](int it) {
+  auto pull = [&](int it, auto set) {
+    constexpr int S = decltype(set)::value;
     int s = first + it;
     const bool second = MODE == DENSE_DX && p.segs == 2 && s >= seg_stages;
     if (second) s -= seg_stages;
@@ -76,19 +77,19 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
       const unsigned av = (A_FAST ? r0 + r_of(true, 0) < p.red : m0 + e_of(false, 0) < p.M) ? a_at : none;
       const unsigned bv = (B_FAST ? r0 + r_of(true, 0) < p.red : n0 + be < p.N) ? b_at : none;
 #pragma unroll
-      for (int j = 0; j < EL; ++j) ra[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_a, (int)(av + j * (unsigned)a_step), 0, 0));
+      for (int j = 0; j < EL; ++j) ra[S][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_a, (int)(av + j * (unsigned)a_step), 0, 0));
       if constexpr (MODE == DENSE_GATED) {                        // half of the tile's columns, whole waves, from each source
         static_assert(FN / 2 >= 64 || MODE != DENSE_GATED, "a wave's columns are of one source");
         const bool up = __builtin_amdgcn_readfirstlane(e_of(false, 0)) >= FN / 2;
         if (up)
 #pragma unroll
-          for (int j = 0; j < EL; ++j) rb[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_u, (int)(bv + j * (unsigned)b_step), 0, 0));
+          for (int j = 0; j < EL; ++j) rb[S][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_u, (int)(bv + j * (unsigned)b_step), 0, 0));
         else
 #pragma unroll
-          for (int j = 0; j < EL; ++j) rb[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_b, (int)(bv + j * (unsigned)b_step), 0, 0));
+          for (int j = 0; j < EL; ++j) rb[S][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_b, (int)(bv + j * (unsigned)b_step), 0, 0));
       } else
 #pragma unroll
-        for (int j = 0; j < EL; ++j) rb[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_b, (int)(bv + j * (unsigned)b_step), 0, 0));
+        for (int j = 0; j < EL; ++j) rb[S][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs_b, (int)(bv + j * (unsigned)b_step), 0, 0));
       return;
     }
 #pragma unroll
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
       const long long e = m0 + e_of(A_FAST, j), r = r0 + r_of(A_FAST, j);
       const bool ok = e < p.M && r < p.red;
       const float v = a[ok ? (A_FAST ? e * p.lda + r : r * p.lda + e) : 0];
-      ra[j] = ok ? v : 0.f;
+      ra[S][j] = ok ? v : 0.f;
     }
 #pragma unroll
     for (int j = 0; j < EL; ++j) {
@@ -109,15 +110,16 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
       const long long e = n0 + c, r = r0 + r_of(B_FAST, j);
       const bool ok = e < p.N && r < p.red;
       const float v = q[ok ? (B_FAST ? e * p.ldb + r : r * p.ldb + e) : 0];
-      rb[j] = ok ? v : 0.f;
+      rb[S][j] = ok ? v : 0.f;
     }
   };
-  auto push = [&](int buf) {
+  auto push = [&](auto set) {                                     // into the buffer of the same number
+    constexpr int buf = decltype(set)::value;
     float* d = lds + buf * 2 * F_TILE;
 #pragma unroll
-    for (int j = 0; j < EL; ++j) d[at(A_FAST, e_of(A_FAST, j), r_of(A_FAST, j))] = ra[j];
+    for (int j = 0; j < EL; ++j) d[at(A_FAST, e_of(A_FAST, j), r_of(A_FAST, j))] = ra[buf][j];
 #pragma unroll
-    for (int j = 0; j < EL; ++j) d[F_TILE + at(B_FAST, e_of(B_FAST, j), r_of(B_FAST, j))] = rb[j];
+    for (int j = 0; j < EL; ++j) d[F_TILE + at(B_FAST, e_of(B_FAST, j), r_of(B_FAST, j))] = rb[buf][j];
   };
   // first column of the wave's block j within the tile
   auto col = [&](int j) { return MODE == DENSE_GATED ? j / (TB / 2 ? TB / 2 : 1) * (FN / 2) + wn * (W / 2) + j % (TB / 2 ? TB / 2 : 1) * 32 : wn * W + j * 32; };
@@ -138,12 +140,15 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
-  pull(0);
-  push(0);
-  for (int it = 0; it < count; ++it) {
+  const std::integral_constant<int, 0> even{};
+  const std::integral_constant<int, 1> odd{};
+  pull(0, even);
+  if (count > 1) pull(1, odd);
+  push(even);
+  auto stage = [&](int it, auto set, auto other) {
     __syncthreads();                                              // this stage is in LDS, and every wave is done with the other buffer
-    if (it + 1 < count) pull(it + 1);
-    const float* t = lds + (it & 1) * 2 * F_TILE;
+    if (it + 2 < count) pull(it + 2, set);
+    const float* t = lds + decltype(set)::value * 2 * F_TILE;
 #pragma unroll
     for (int s = 0; s < FK / 8; ++s) {
       float a[TB][4], b[TB][4];
@@ -159,16 +164,25 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
 #pragma unroll
           for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(b[j][u], a[i][u], acc[i][j], 0, 0, 0);
     }
-    if (it + 1 < count) push((it + 1) & 1);
+    if (it + 1 < count) push(other);
+  };
+  for (int it = 0; it < count; it += 2) {
+    stage(it, even, odd);
+    if (it + 1 < count) stage(it + 1, odd, even);
   }
   __syncthreads();
-  dense_epilogue<float, MODE, W>(p, acc, reinterpret_cast<unsigned char*>(lds) + wave * epi_wave_bytes(W), m0 + wm * W, n0 + wn * (MODE == DENSE_GATED ? W / 2 : W), src, split);
+  dense_epilogue<float, MODE, W, 0>(p, acc, reinterpret_cast<unsigned char*>(lds) + wave * epi_wave_bytes(W), m0 + wm * W, n0 + wn * (MODE == DENSE_GATED ? W / 2 : W), src, split,
+                                 Beside<MODE, W, 0>{});
 }
 
-// Tile and splits, as in dense_gemm.hip; us of a stage of 32: one work-group on a compute unit, as many as it holds.
+// Tile and splits by an estimate as in dense_gemm.hip.  us of a stage of 32: of a work-group alone on its compute unit, and what each adds where there are more.
+// us by tile and splits (the starred are taken):   128: 1    2    4    8      64: 1    2    4    8
+//   64 x 4096 x 4096                                   308  160   86   52     111   62   37   33*
+//   1000 x 1024 x 1000                                  82   50   37   42      33*  33   34   40
+//   2048 x 2048 x 2048                                 162  157  165  199     158* 160  167  186
 struct F32Plan { int fm, splits; };
-struct F32Cost { int fm, per_cu; double alone, full; };
-constexpr F32Cost F32_COSTS[] = {{128, 2, 2.2, 3.6}, {64, 4, 0.8, 2.0}};
+struct F32Cost { int fm, per_cu; double alone, each; };
+constexpr F32Cost F32_COSTS[] = {{128, 2, 2.4, 2.2}, {64, 4, 0.86, 0.6}};
 
 F32Plan f32_plan(int mode, long long M, int N, long long red, int segs, int srcs) {
   const long long stages = (red + FK - 1) / FK * segs;
@@ -181,7 +195,8 @@ F32Plan f32_plan(int mode, long long M, int N, long long red, int segs, int srcs
     for (int splits = 1; splits <= 16; ++splits) {
       const long long per = (stages + splits - 1) / splits, jobs = tiles * splits, rounds = jobs / slots, rest = jobs - rounds * slots;
       if (splits > 1 && per < 4) break;
-      double us = rounds * (per * t.full + 2.0) + (rest == 0 ? 0.0 : per * (t.alone + (t.full - t.alone) * ((double)(rest > 256 ? rest - 256 : 0) / slots)) + 2.0);
+      const double held = (double)((rest + 255) / 256) * t.each;
+      double us = rounds * (per * t.per_cu * t.each + 2.0) + (rest == 0 ? 0.0 : per * (held > t.alone ? held : t.alone) + 2.0);
       if (splits > 1) us += 3.0 + splits * (double)M * N * srcs * 2e-6;
       if (us < least) { least = us; best = {t.fm, splits}; }
     }

@@ -26,30 +26,6 @@ namespace {
 
 constexpr int FT = 512;              // threads
 
-// N elements as they lie in memory (as words: in an array of halves the compiler takes the loads apart).
-template <typename T, int N>
-struct Raw {
-  unsigned q[N * sizeof(T) / 4];
-  __device__ __forceinline__ float get(int e) const {
-    if constexpr (sizeof(T) == 2) return __uint_as_float((e & 1) ? (q[e >> 1] & 0xffff0000u) : (q[e >> 1] << 16));
-    else return __uint_as_float(q[e]);
-  }
-};
-template <int N, typename T>
-__device__ __forceinline__ Raw<T, N> raw(const T* p, int cnt) {
-  Raw<T, N> r;
-  if (cnt >= N) { __builtin_memcpy(&r, p, sizeof(r)); return r; }
-#pragma unroll
-  for (unsigned& w : r.q) w = 0;
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (e < cnt) {
-      if constexpr (sizeof(T) == 2) r.q[e >> 1] |= (unsigned)p[e] << ((e & 1) * 16);
-      else r.q[e] = __float_as_uint(p[e]);
-    }
-  return r;
-}
-
 template <typename T, int MODE, int R, int CB>
 __global__ __launch_bounds__(FT) void dense_few_kernel(DenseP p) {
   constexpr int S = MODE == DENSE_GATED ? 2 : 1, LC = CB / 8, KG = FT / LC;
@@ -61,6 +37,12 @@ __global__ __launch_bounds__(FT) void dense_few_kernel(DenseP p) {
   const int tid = threadIdx.x, c = (tid % LC) * 8, n = (job - split * p.ntiles) * CB + c, cnt = p.N - n < 8 ? p.N - n : 8;
   const int rows = (int)p.M;
   const T* x = (const T*)p.a[0];
+  float fb[8], fr[8];                                             // of the thread that finishes a row's eight columns
+  const bool finisher = tid < R * LC && tid / LC < rows && cnt > 0;
+  if (finisher && p.splits == 1) {
+    dense_bias8<MODE>(p, n, cnt, fb);
+    dense_beside8<T, MODE>(p, tid / LC, n, cnt, fr);
+  }
   const T* w[2] = {(const T*)p.b[0] + n, (const T*)p.b[1] + n};
 
   const long long per = (p.red / p.splits + 7) / 8 * 8, k_begin = split * per, k_end = split + 1 < p.splits && k_begin + per < p.red ? k_begin + per : p.red;
@@ -130,11 +112,11 @@ __global__ __launch_bounds__(FT) void dense_few_kernel(DenseP p) {
         if constexpr (S == 2) u[e] += sums[i][1][r][c + e];
       }
     }
-    if (r >= rows || cnt <= 0) return;
+    if (!finisher) return;
     if (p.splits > 1) {
       dense_part8(p, split, 0, r, n, cnt, v);
       if constexpr (S == 2) dense_part8(p, split, 1, r, n, cnt, u);
-    } else dense_finish8<T, MODE>(p, 0, r, n, cnt, v, u);
+    } else dense_finish8<T, MODE>(p, 0, r, n, cnt, v, u, fb, fr);
   }
 }
 
@@ -167,12 +149,14 @@ template <typename T, int MODE>
 hipError_t few_mode(DenseP& p, hipStream_t s) {
   if (p.M == 1) return few_rows<T, MODE, 1>(p, s);
   if (p.M == 2) return few_rows<T, MODE, 2>(p, s);
-  return p.M <= 4 ? few_rows<T, MODE, 4>(p, s) : few_rows<T, MODE, 8>(p, s);
+  if constexpr (MODE == DENSE_FWD)
+    if (p.M > 4) return few_rows<T, MODE, 8>(p, s);
+  return few_rows<T, MODE, 4>(p, s);
 }
 
 }  // namespace
 
-bool dense_few_ok(int mode, long long M) { return (mode == DENSE_FWD || mode == DENSE_GATED) && M <= 8; }
+bool dense_few_ok(int mode, long long M) { return (mode == DENSE_FWD && M <= 8) || (mode == DENSE_GATED && M <= 4); }       // registers
 
 uint64_t dense_few_ws(int mode, bool f32, long long M, int N, long long red) {
   const int splits = few_splits(mode, f32, N, red);

@@ -238,6 +238,10 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
     return MODE == DENSE_GATED ? (j / (TN / 2)) * SUB + (wn * (TN / 2) + j % (TN / 2)) * 32 : wn * T::WTN + j * 32;
   });
 
+  const long long wm0 = m0 + wm * T::WTM;                         // the wave's first row and column
+  const int wn0 = n0 + wn * (MODE == DENSE_GATED ? T::WTN / 2 : T::WTN);
+  constexpr int PRE = !DMA ? 0 : TM < 2 ? TM : 2;
+  Beside<MODE, T::WTN, PRE> beside;
   f32x16 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -286,7 +290,8 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
 #pragma unroll
       for (int v = 0; v < (it == T::RING - 1 ? EARLY : LOADS); ++v) load(it * T::STAGE, v);
     }
-    wait_barrier<(T::RING - 2) * LOADS + EARLY>();
+    beside.ask(p, wm0, wn0, epilogue_whole<MODE, T::WTN, TM>(p, wm0, wn0));
+    wait_barrier<(T::RING - 2) * LOADS + EARLY>();                // more loads behind those it counts only make it wait longer
 #pragma unroll
     for (int f = 0; f < TM + TN; ++f) read(dense_smem, 0, f);
     int it = 0;
@@ -329,7 +334,7 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
     }
   }
   __syncthreads();                                                // the buffers are free for the epilogue
-  dense_epilogue<uint16_t, MODE, T::WTN>(p, acc, dense_smem + wave * T::EPI_WAVE, m0 + wm * T::WTM, n0 + wn * (MODE == DENSE_GATED ? T::WTN / 2 : T::WTN), src, split);
+  dense_epilogue<uint16_t, MODE, T::WTN, PRE>(p, acc, dense_smem + wave * T::EPI_WAVE, wm0, wn0, src, split, beside);
 }
 
 template <typename T, int MODE, bool DMA>
@@ -362,7 +367,7 @@ enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 // through the compute units, stages of 64 of the reduction each, and for splits the join's launch (3 us) and its passes over the sums (4 TB/s).  us of a stage, measured
 // where a work-group is alone on its compute unit and where all units hold as many as they can (forward, bf16, rows x inputs x outputs):
 //                  alone            full
-//   256 x 256      1.7              1.8      8192 x 65536 x 4096
+//   256 x 256      1.7              1.7      8192 x 65536 x 4096
 //   128 x 128      0.86 (two stages ahead at most)   1.16     64 x 4096 x 4096, 2048 x 4096 x 4096
 //   the same, deep 0.50             0.65     1024 x 2048 x 4096
 //   64 x 128       0.48             0.80     512 x 4096 x 4096, 1024 x 2048 x 4096
@@ -377,7 +382,7 @@ enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 //   2048 x 4096 x 4096           79.5*  107    137    192     85.8   118    164        102    129    148        129    153    173
 struct DensePlan { int tile, splits; };
 struct TileCost { int tile, bm, bn, per_cu; float alone, full; };
-constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.7f, 1.8f}, {TILE_128, 128, 128, 2, 0.86f, 1.16f}, {TILE_128D, 128, 128, 1, 0.50f, 0.65f},
+constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.7f, 1.7f}, {TILE_128, 128, 128, 2, 0.86f, 1.16f}, {TILE_128D, 128, 128, 1, 0.50f, 0.65f},
                               {TILE_64X128, 64, 128, 2, 0.48f, 0.80f}, {TILE_64, 64, 64, 2, 0.33f, 0.52f}, {TILE_32, 32, 128, 2, 0.38f, 0.62f}};
 
 DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int srcs) {

@@ -39,10 +39,12 @@ __global__ __launch_bounds__(64) void dense_join_kernel(DenseP p) {
       for (int e = 0; e < 8; ++e) v[e] += t[e];
     }
   };
-  float v[8], u[8];
+  float v[8], u[8], b[8], r[8];
+  dense_bias8<MODE>(p, n, cnt, b);
+  dense_beside8<T, MODE>(p, row, n, cnt, r);
   add(at, v);
   if constexpr (MODE == DENSE_GATED) add(at + plane, u);
-  dense_finish8<T, MODE>(p, src, row, n, cnt, v, u);
+  dense_finish8<T, MODE>(p, src, row, n, cnt, v, u, b, r);
 }
 
 template <typename T, int MODE>

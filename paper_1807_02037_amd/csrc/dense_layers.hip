@@ -13,7 +13,7 @@ namespace {
 //
 // A work-group takes ROWS_PER rows of 512 columns, eight columns a thread: each input is read once, the gradient is written once in the storage type, and
 // the columns' sums over the work-group's rows, of the values before rounding, go to part[chunk of rows][n].  sum_rows adds the chunks in order.
-constexpr int PT = 256, PC = 512, ROWS_PER = 64, LANES = PC / 8, WAYS = PT / LANES;
+constexpr int PT = 256, PC = 512, ROWS_PER = 32, LANES = PC / 8, WAYS = PT / LANES;
 
 struct GradP {
   const void *d, *g, *u;       // gradient that comes in; linear: g = pre; gated: g and u
@@ -30,32 +30,47 @@ __global__ __launch_bounds__(PT) void act_grad_kernel(GradP p) {
   const int c = (threadIdx.x % LANES) * 8, way = threadIdx.x / LANES, n = c0 + c, cnt = p.N - n < 8 ? p.N - n : 8;
   const long long r0 = (long long)chunk * ROWS_PER;
   float total[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (cnt > 0)
-    for (int r = way; r < ROWS_PER; r += WAYS) {
-      const long long row = r0 + r;
-      if (row >= p.M) break;
-      float d[8], v[8], u[8];
-      load8((const T*)p.d + row * p.ldd + n, cnt, d);
-      if (p.gated) {
-        load8((const T*)p.g + row * p.ldd + n, cnt, v);
-        load8((const T*)p.u + row * p.ldd + n, cnt, u);
-        gated_grad8(p.act, d, v, u);
-        store8((T*)p.dz + row * p.ldo + n, cnt, v);
-        store8((T*)p.du + row * p.ldo + n, cnt, u);
-        continue;
-      }
-      if (p.g) {
-        load8((const T*)p.g + row * p.ldd + n, cnt, v);
+  constexpr int U = 4;                                            // rows in flight
+  auto rows = [&](auto gated_c, auto slope_c) {                   // what is read: d; g; g and u
+    constexpr bool GATED = decltype(gated_c)::value, SLOPE = decltype(slope_c)::value;
+    for (int r = way; r < ROWS_PER && r0 + r < p.M; r += WAYS * U) {
+      Raw<T, 8> d[U], g[SLOPE ? U : 1], u[GATED ? U : 1];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = 1.f;
-        gated_grad8(p.act, d, v, u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = v[e];
-        if (p.dz) store8((T*)p.dz + row * p.ldo + n, cnt, d);
+      for (int k = 0; k < U; ++k) {
+        const long long row = r0 + r + k * WAYS, at = (row < p.M ? row : r0 + r) * p.ldd + n;       // rows beyond the last: one that is there, for nothing
+        d[k] = raw<8>((const T*)p.d + at, cnt);
+        if constexpr (SLOPE) g[k] = raw<8>((const T*)p.g + at, cnt);
+        if constexpr (GATED) u[k] = raw<8>((const T*)p.u + at, cnt);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) total[e] += d[e];
+      for (int k = 0; k < U; ++k) {
+        const long long row = r0 + r + k * WAYS;
+        if (row >= p.M) break;
+        float dv[8], gv[8], uv[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          dv[e] = d[k].get(e);
+          if constexpr (SLOPE) gv[e] = g[k].get(e);
+          if constexpr (GATED) uv[e] = u[k].get(e);
+          else uv[e] = 1.f;
+        }
+        if constexpr (SLOPE) {
+          gated_grad8(p.act, dv, gv, uv);
+          store8((T*)p.dz + row * p.ldo + n, cnt, gv);
+          if constexpr (GATED) store8((T*)p.du + row * p.ldo + n, cnt, uv);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) total[e] += SLOPE ? gv[e] : dv[e];
+      }
     }
+  };
+  const std::true_type yes{};
+  const std::false_type no{};
+  if (cnt > 0) {
+    if (p.gated) rows(yes, yes);
+    else if (p.g) rows(no, yes);
+    else rows(no, no);
+  }
   if (!p.part) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) sums[way][c + e] = total[e];
@@ -74,8 +89,16 @@ __global__ __launch_bounds__(PT) void sum_rows_kernel(const float* part, long lo
   __shared__ float sums[8][32];
   const int c = threadIdx.x & 31, way = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
   float t = 0.f;
-  if (n < N)
-    for (long long i = way; i < chunks; i += 8) t += part[i * N + n];
+  if (n < N) {
+    long long i = way;
+    for (; i + 24 < chunks; i += 32) {
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = part[(i + 8 * u) * N + n];
+      t += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    for (; i < chunks; i += 8) t += part[i * N + n];
+  }
   sums[way][c] = t;
   __syncthreads();
   if (way == 0 && n < N) {
