@@ -197,8 +197,35 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
     if (v < AV) load_lds16(rs_a, lds0 + at + v * 4096, a_off[v < AV ? v : 0], 0);
     else load_lds16(MODE == DENSE_GATED && v - AV >= BV / 2 ? rs_u : rs_b, lds0 + at + T::A_BYTES + (v - AV) * 4096, b_off[v < AV ? 0 : v - AV], 0);
   };
-  // through registers, at any address
+  // Through registers, at any address.  Vectors move along the reduction by pointers.  Rows and columns beyond the last: any that is there, their results are not
+  // stored.  A vector of columns across the end of a row is the row's last eight elements, shifted.  The last stage of a segment, if it is partial, and
+  // rows of fewer than eight columns go element by element.
   v4u ra[DMA ? 1 : AV], rb[DMA ? 1 : BV];
+  const uint16_t *pa[DMA ? 1 : AV], *pb[DMA ? 1 : BV];
+  int a_shift = 0, b_shift = 0;                                   // elements; the same for all of a thread's vectors
+  const bool tiny = (!A_FAST && p.M < 8) || (!B_FAST && p.N < 8);
+  const bool a_cut = !A_FAST && m_left < BM, b_cut = !B_FAST && n_left < OUT_N;
+  auto at_start = [&](int seg, long long r0) {
+    const Source t = source(seg, r0);
+#pragma unroll
+    for (int j = 0; j < AV; ++j) {
+      const long long most = A_FAST ? m_left - 1 : m_left - 8;
+      const long long e = a_e[j] <= most ? a_e[j] : most;         // may lie before the tile
+      if (!A_FAST) a_shift = a_e[j] < m_left ? (int)(a_e[j] - e) : 0;
+      pa[j] = t.a + (A_FAST ? e * p.lda + a_r[j] : a_r[j] * p.lda + e);
+    }
+#pragma unroll
+    for (int j = 0; j < BV; ++j) {
+      const long long most = B_FAST ? n_left - 1 : n_left - 8;
+      const long long e = b_e[j] <= most ? b_e[j] : most;
+      if (!B_FAST) b_shift = b_e[j] < n_left ? (int)(b_e[j] - e) : 0;
+      pb[j] = (MODE == DENSE_GATED && j >= BV / 2 ? t.bu : t.b) + (B_FAST ? e * p.ldb + b_r[j] : b_r[j] * p.ldb + e);
+    }
+  };
+  auto shifted = [](v4u v, int by) {                              // elements by .. 7 to the front
+    const unsigned __int128 w = __builtin_bit_cast(unsigned __int128, v) >> (16 * by);
+    return __builtin_bit_cast(v4u, w);
+  };
   auto vector = [&](const uint16_t* q, long long have) {
     v4u v = {0u, 0u, 0u, 0u};
     if (have >= 8) __builtin_memcpy(&v, q, 16);
@@ -211,6 +238,20 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
   auto pull = [&](int it) {
     const int st = first + it, seg = MODE == DENSE_DX && st >= seg_stages ? 1 : 0;
     const long long r0 = (long long)(st - seg * seg_stages) * DK;
+    if (it == 0 || (MODE == DENSE_DX && r0 == 0)) at_start(seg, r0);
+    if (r0 + DK <= p.red && !tiny) {
+#pragma unroll
+      for (int j = 0; j < AV; ++j) {
+        __builtin_memcpy(&ra[j], pa[j], 16);
+        pa[j] += A_FAST ? DK : DK * p.lda;
+      }
+#pragma unroll
+      for (int j = 0; j < BV; ++j) {
+        __builtin_memcpy(&rb[j], pb[j], 16);
+        pb[j] += B_FAST ? DK : DK * p.ldb;
+      }
+      return;
+    }
     const Source t = source(seg, r0);
 #pragma unroll
     for (int j = 0; j < AV; ++j) {
@@ -224,8 +265,16 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
                      red > 0 && ext > 0 ? (B_FAST ? red : ext) : 0);
     }
   };
-  auto push = [&](int buf) {
-    unsigned char* d = dense_smem + buf * T::STAGE + tid * 16;
+  auto push = [&](int it) {
+    unsigned char* d = dense_smem + (it & 1) * T::STAGE + tid * 16;
+    const int st = first + it, seg = MODE == DENSE_DX && st >= seg_stages ? 1 : 0;
+    const bool whole = (long long)(st - seg * seg_stages + 1) * DK <= p.red && !tiny;     // else its vectors are in place
+    if (a_cut && whole)
+#pragma unroll
+      for (int j = 0; j < AV; ++j) ra[j] = shifted(ra[j], a_shift);
+    if (b_cut && whole)
+#pragma unroll
+      for (int j = 0; j < BV; ++j) rb[j] = shifted(rb[j], b_shift);
 #pragma unroll
     for (int j = 0; j < AV; ++j) *reinterpret_cast<v4u*>(d + j * 4096) = ra[j];
 #pragma unroll
@@ -330,7 +379,7 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
       __syncthreads();                                            // this stage is in LDS, and every wave is done with the other buffer
       if (it + 1 < count) pull(it + 1);
       multiply(it & 1);
-      if (it + 1 < count) push((it + 1) & 1);
+      if (it + 1 < count) push(it + 1);
     }
   }
   __syncthreads();                                                // the buffers are free for the epilogue

@@ -9,7 +9,8 @@ pytestmark = pytest.mark.gpu
 
 # m, k, n: single elements, tokens one by one, tiles not filled, filled and passed by one, lengths that no vector divides
 SIZES = [(1, 1, 1), (1, 64, 64), (2, 7, 9), (1, 520, 136), (3, 8, 8), (8, 264, 1032), (17, 96, 260), (33, 65, 129), (64, 1000, 77), (127, 64, 128),
-         (129, 200, 136), (256, 136, 264), (300, 264, 328), (515, 72, 520)]
+         (129, 200, 136), (256, 136, 264), (300, 264, 328), (515, 72, 520),
+         (260, 393, 94), (9, 131, 135), (140, 7, 300), (7, 200, 5), (131, 193, 193)]
 DTYPES = ["bf16", "fp32"]
 
 
