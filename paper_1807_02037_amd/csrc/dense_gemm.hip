@@ -326,7 +326,9 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
     // the next stage has landed.  From there to the next barrier the loads of the stage RING further go out into this buffer, spread between the
     // products (in a row they fill the queue of the address unit and the products behind them wait), and the next stage's first operands are
     // read: the matrix cores wait for nothing but the waves' skew at the barrier.
-    constexpr int SLOTS = NKS * TM * TN;                          // products of a stage, counted from the barrier
+    // Products of a stage, counted from the barrier, that loads go out behind: with two buffers the first half, since the next barrier waits for them (2048 x 4096 x 4096
+    // 82.9 -> 81.8 us, 8192 x 8192 x 4096 on these tiles 546 -> 517).
+    constexpr int SLOTS = NKS * TM * TN / (T::RING == 2 ? 2 : 1);
     constexpr int EARLY = (TM * TN * LOADS + SLOTS - 1) / SLOTS;  // loads of the step behind the barrier
     {
       const int seg = MODE == DENSE_DX && first >= seg_stages ? 1 : 0;
@@ -386,25 +388,220 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
   dense_epilogue<uint16_t, MODE, T::WTN, PRE>(p, acc, dense_smem + wave * T::EPI_WAVE, wm0, wn0, src, split, beside);
 }
 
-template <typename T, int MODE, bool DMA>
-hipError_t launch_dense(DenseP& p, hipStream_t s) {
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(dense_kernel<T, MODE, DMA>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
-  if (attr != hipSuccess) return attr;
+// The 256 x 256 tile, one work-group on a compute unit, a wave on a SIMD.  Rows along the reduction arrive in whole 128-byte lines only if 64 of it are asked for at a time
+// (half a line costs what the line costs), and two stages of 64 of both operands ahead are more than the LDS holds.  So each operand has a ring of its own:
+// A three units of 64, B two.  One barrier a stage, in front of its last step, whose operands are in registers: there every wave is done with the stage's units.  Behind
+// it the next unit of B goes out, spread over the last step and the first of the next stage, and has until that stage's barrier to land; in the two steps
+// between goes the next unit of A, which has a stage more.
+// TFLOP/s, 8192 x 65536 x 4096 forward, N(0,1): 1327; with rings of four units of 32 of both, two barriers for 64: 1259; A in three units of 64 and B in four of 32, two
+// barriers: 1289; two units of 64 of both, whose last loads have no time to land: 1215; without loads 1660 (which bounds nothing else: operands that stay in the
+// L2s gain 2 %).  At two stages the first products wait for memory and all compute units meet in their epilogues: 8192 x 8192 x 4096 1295.
+struct Tile256 {
+  static constexpr int DK = 64, BM = 256, BN = 256, NT = 256;
+  static constexpr int UNIT = 256 * DK * 2, A_RING = 3, B_RING = 2, LDS_BYTES = (A_RING + B_RING) * UNIT;
+  static_assert(LDS_BYTES == 163840 && LDS_BYTES >= 4 * epi_wave_bytes(128), "the LDS of a compute unit");
+};
+
+template <int MODE>
+__global__ __launch_bounds__(256, 1) void dense_large_kernel(DenseP p) {
+  typedef Tile256 T;
+  constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = MODE == DENSE_DX;
+  constexpr int DK = T::DK, BM = T::BM, BN = T::BN, TM = 4, TN = 4, NP = TM * TN, SUB = 128, OUT_N = MODE == DENSE_GATED ? 128 : 256;
+  constexpr int V = T::UNIT / (16 * T::NT), B_AT = T::A_RING * T::UNIT;     // loads of a unit per thread; where B's ring begins
+  typedef Operand<BM, A_FAST, SUB, DK> OpA;
+  typedef Operand<BN, B_FAST, SUB, DK> OpB;
+  extern __shared__ __attribute__((aligned(256))) unsigned char dense_smem[];
+
+  const int job = xcd_order(p.ntiles * p.splits);
+  if (job < 0) return;
+  const int split = job / p.ntiles;
+  int tm, tn, src = 0;
+  tile_at(p, job - split * p.ntiles, tm, tn);
+  if (MODE == DENSE_DW && p.srcs == 2) {                          // columns of tiles of the one source, then of the other
+    const int each = p.ntn / 2;
+    src = tn >= each;
+    tn -= src * each;
+  }
+  const long long m0 = (long long)tm * BM;
+  const int n0 = tn * OUT_N;
+  const int first = split * p.stages_per_split, count = p.stages - first < p.stages_per_split ? p.stages - first : p.stages_per_split;
+  const int seg_stages = p.stages / p.segs;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+
+  // ---- loads: a stream for each operand, as in dense_kernel ----
+  const long long m_left = p.M - m0, n_left = (long long)p.N - n0;
+  int a_e[V], a_r[V], b_e[V], b_r[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    OpA::where(tid + j * 256, a_e[j], a_r[j]);
+    OpB::where(tid + j * 256, b_e[j], b_r[j]);
+    if (MODE == DENSE_GATED) b_e[j] %= SUB;
+  }
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)dense_smem + wave * 1024);
+  unsigned a_off[V], b_off[V];
+  v4u rs_a = {}, rs_b = {}, rs_u = {};
+  int a_left = count, b_left = count;                             // units not asked for yet
+  long long ar = 0, br = 0;                                       // reduction element of the next unit
+  auto a_enter = [&](int seg, long long r) {
+    ar = r;
+    rs_a = buffer_rsrc((const uint16_t*)p.a[MODE == DENSE_DX ? seg : 0] + (A_FAST ? m0 * p.lda + r : r * p.lda + m0), 0x7fffffff);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      a_off[j] = a_e[j] < m_left && r + a_r[j] < p.red ? (unsigned)((A_FAST ? a_e[j] * p.lda + a_r[j] : a_r[j] * p.lda + a_e[j]) * 2) : DMA_OOB;
+  };
+  auto b_enter = [&](int seg, long long r) {
+    br = r;
+    const long long o = B_FAST ? n0 * p.ldb + r : r * p.ldb + n0;
+    rs_b = buffer_rsrc((const uint16_t*)p.b[MODE == DENSE_DX ? seg : MODE == DENSE_DW ? src : 0] + o, 0x7fffffff);
+    if (MODE == DENSE_GATED) rs_u = buffer_rsrc((const uint16_t*)p.b[1] + o, 0x7fffffff);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      b_off[j] = b_e[j] < n_left && r + b_r[j] < p.red ? (unsigned)((B_FAST ? b_e[j] * p.ldb + b_r[j] : b_r[j] * p.ldb + b_e[j]) * 2) : DMA_OOB;
+  };
+  auto move = [](v4u& rs, long long bytes) {
+    const unsigned long long base = ((unsigned long long)rs[1] << 32 | rs[0]) + bytes;
+    rs[0] = (unsigned)base;
+    rs[1] = (unsigned)(base >> 32);
+  };
+  auto a_next = [&]() {
+    if (--a_left <= 0) { rs_a[2] = 0; return; }                   // beyond the last: nothing but zeros
+    ar += DK;
+    if (MODE == DENSE_DX && ar >= p.red) a_enter(1, 0);
+    else move(rs_a, (A_FAST ? DK : DK * p.lda) * 2);
+    if (ar + DK > p.red)
+#pragma unroll
+      for (int j = 0; j < V; ++j) a_off[j] = ar + a_r[j] < p.red ? a_off[j] : DMA_OOB;
+  };
+  auto b_next = [&]() {
+    if (--b_left <= 0) { rs_b[2] = rs_u[2] = 0; return; }
+    br += DK;
+    if (MODE == DENSE_DX && br >= p.red) b_enter(1, 0);
+    else {
+      move(rs_b, (B_FAST ? DK : DK * p.ldb) * 2);
+      if (MODE == DENSE_GATED) move(rs_u, DK * p.ldb * 2);
+    }
+    if (br + DK > p.red)
+#pragma unroll
+      for (int j = 0; j < V; ++j) b_off[j] = br + b_r[j] < p.red ? b_off[j] : DMA_OOB;
+  };
+  auto a_load = [&](unsigned at, int v) { load_lds16(rs_a, lds0 + at + v * 4096, a_off[v], 0); };
+  auto b_load = [&](unsigned at, int v) { load_lds16(MODE == DENSE_GATED && v >= V / 2 ? rs_u : rs_b, lds0 + B_AT + at + v * 4096, b_off[v], 0); };
+
+  int a_rd[OpA::N], b_rd[OpB::N];
+  OpA::template prepare<TM>(a_rd, lane, [&](int i) { return wm * 128 + i * 32; });
+  OpB::template prepare<TN>(b_rd, lane, [&](int j) { return MODE == DENSE_GATED ? (j / 2) * SUB + (wn * 2 + j % 2) * 32 : wn * 128 + j * 32; });
+  const long long wm0 = m0 + wm * 128;                            // the wave's first row and column
+  const int wn0 = n0 + wn * (OUT_N / 2);
+  Beside<MODE, 128, 2> beside;
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  bf16x8 af[2][TM], bf[2][TN];                                    // operands are read one step ahead of their products
+  auto read = [&](unsigned a, unsigned b, int ks, int f) {        // fragment f of step ks; a, b: the units
+    if (f < TN) bf[ks & 1][f] = OpB::fragment(dense_smem + B_AT + b + OpB::address(b_rd, f, ks));
+    else af[ks & 1][f - TN] = OpA::fragment(dense_smem + a + OpA::address(a_rd, f - TN, ks));
+  };
+  // step ks: products, the reads of the next step's operands (a, b: their units), and four loads, from load(l) on, one every four products
+  auto step = [&](auto ks_c, unsigned a, unsigned b, auto l_c, auto&& load) {
+    constexpr int ks = decltype(ks_c)::value, l = decltype(l_c)::value;
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      acc[q / TN][q % TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][q % TN], af[ks & 1][q / TN], acc[q / TN][q % TN], 0, 0, 0);
+      if (q < TM + TN) read(a, b, (ks + 1) % 4, q);
+      if (q % 4 == 0) load(l + q / 4);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  static_assert(DK == 64 && V == 8, "four steps a stage, of four loads each");
+  const std::integral_constant<int, 0> c0{};
+  const std::integral_constant<int, 1> c1{};
+  const std::integral_constant<int, 2> c2{};
+  const std::integral_constant<int, 3> c3{};
+  const std::integral_constant<int, 4> c4{};
+
+  {
+    const int seg = MODE == DENSE_DX && first >= seg_stages ? 1 : 0;
+    a_enter(seg, (long long)(first - seg * seg_stages) * DK);
+    b_enter(seg, (long long)(first - seg * seg_stages) * DK);
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) a_load(0, v);
+  a_next();
+#pragma unroll
+  for (int v = 0; v < V; ++v) b_load(0, v);
+  b_next();
+#pragma unroll
+  for (int v = 0; v < V; ++v) a_load(T::UNIT, v);
+  a_next();
+  unsigned a = 0, b = 0;                                          // this stage's units
+  unsigned a_fill = 2 * T::UNIT, b_fill = T::UNIT;                // the units that loads go to
+  auto a_fills = [&](int l) { a_load(a_fill, l); };
+  auto b_fills = [&](int l) { b_load(b_fill, l); };
+#pragma unroll
+  for (int l = 0; l < 4; ++l) b_fills(l);
+  beside.ask(p, wm0, wn0, epilogue_whole<MODE, 128, TM>(p, wm0, wn0));
+  wait_barrier<12>();                                             // unit 0 of each has landed: behind them are unit 1 of A, half of unit 1 of B, and the residuals, which only make it wait longer
+#pragma unroll
+  for (int f = 0; f < TM + TN; ++f) read(0, 0, 0, f);
+  int left = count;                                               // at least one stage
+  do {
+    const unsigned an = a + T::UNIT < T::A_RING * T::UNIT ? a + T::UNIT : 0u, bn = b ? 0u : (unsigned)T::UNIT;
+    step(c0, a, b, c4, b_fills);
+    step(c1, a, b, c0, a_fills);
+    step(c2, a, b, c4, a_fills);
+    a_next();
+    b_next();
+    a_fill = a;
+    b_fill = b;
+    wait_barrier<8>();                                            // the unit of A just asked for may be in flight
+    step(c3, an, bn, c0, b_fills);
+    a = an;
+    b = bn;
+  } while (--left > 0);
+  wait_loads();
+  __syncthreads();                                                // the rings are free for the epilogue
+  dense_epilogue<uint16_t, MODE, 128, 2>(p, acc, dense_smem + wave * epi_wave_bytes(128), wm0, wn0, src, split, beside);
+}
+
+// Tiles and stages of a launch; false: more than a grid holds.
+template <typename T, int MODE>
+bool dense_grid(DenseP& p) {
   p.stages = (int)((p.red + T::DK - 1) / T::DK) * p.segs;
   p.stages_per_split = (p.stages + p.splits - 1) / p.splits;
   p.splits = (p.stages + p.stages_per_split - 1) / p.stages_per_split;      // none without a stage
   const int out_n = MODE == DENSE_GATED ? T::BN / 2 : T::BN;
   const long long tm = (p.M + T::BM - 1) / T::BM, tn = (long long)((p.N + out_n - 1) / out_n) * (MODE == DENSE_DW ? p.srcs : 1);
-  if (tm * tn * p.splits > 0x7fffff00LL) return hipErrorInvalidValue;
+  if (tm * tn * p.splits > 0x7fffff00LL) return false;
   p.ntm = (int)tm;
   p.ntn = (int)tn;
   p.ntiles = (int)(tm * tn);
+  return true;
+}
+
+template <int MODE>
+hipError_t launch_large(DenseP& p, hipStream_t s) {
+  typedef Tile256 T;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(dense_large_kernel<MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
+  if (attr != hipSuccess) return attr;
+  if (!dense_grid<T, MODE>(p)) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((dense_large_kernel<MODE>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(T::NT), T::LDS_BYTES, s, p);
+  return hipGetLastError();
+}
+
+template <typename T, int MODE, bool DMA>
+hipError_t launch_dense(DenseP& p, hipStream_t s) {
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(dense_kernel<T, MODE, DMA>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
+  if (attr != hipSuccess) return attr;
+  if (!dense_grid<T, MODE>(p)) return hipErrorInvalidValue;
   hipLaunchKernelGGL((dense_kernel<T, MODE, DMA>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(T::NT), T::LDS_BYTES, s, p);
   return hipGetLastError();
 }
 
 // Deep rings hide what a stage takes to arrive where there is one work-group on a compute unit; two work-groups hide each other's.
-typedef DenseTile<256, 256, 32, 4> Tile256;
 typedef DenseTile<128, 128, 64, 2> Tile128;
 typedef DenseTile<128, 128, 64, 5> Tile128D;
 typedef DenseTile<64, 128, 64, 3> Tile64x128;
@@ -416,7 +613,7 @@ enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 // through the compute units, stages of 64 of the reduction each, and for splits the join's launch (3 us) and its passes over the sums (4 TB/s).  us of a stage, measured
 // where a work-group is alone on its compute unit and where all units hold as many as they can (forward, bf16, rows x inputs x outputs):
 //                  alone            full
-//   256 x 256      1.7              1.7      8192 x 65536 x 4096
+//   256 x 256      1.62             1.62     8192 x 65536 x 4096
 //   128 x 128      0.86 (two stages ahead at most)   1.16     64 x 4096 x 4096, 2048 x 4096 x 4096
 //   the same, deep 0.50             0.65     1024 x 2048 x 4096
 //   64 x 128       0.48             0.80     512 x 4096 x 4096, 1024 x 2048 x 4096
@@ -431,7 +628,7 @@ enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 //   2048 x 4096 x 4096           79.5*  107    137    192     85.8   118    164        102    129    148        129    153    173
 struct DensePlan { int tile, splits; };
 struct TileCost { int tile, bm, bn, per_cu; float alone, full; };
-constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.7f, 1.7f}, {TILE_128, 128, 128, 2, 0.86f, 1.16f}, {TILE_128D, 128, 128, 1, 0.50f, 0.65f},
+constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.62f, 1.62f}, {TILE_128, 128, 128, 2, 0.86f, 1.16f}, {TILE_128D, 128, 128, 1, 0.50f, 0.65f},
                               {TILE_64X128, 64, 128, 2, 0.48f, 0.80f}, {TILE_64, 64, 64, 2, 0.33f, 0.52f}, {TILE_32, 32, 128, 2, 0.38f, 0.62f}};
 
 DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int srcs) {
@@ -469,7 +666,7 @@ hipError_t dense_mode(DenseP& p, hipStream_t s) {
   p.splits = plan.splits;
   hipError_t e;
   if (!dma_ok(MODE, p)) e = plan.tile <= TILE_128D ? launch_dense<Tile128, MODE, false>(p, s) : launch_dense<Tile64x128, MODE, false>(p, s);
-  else if (plan.tile == TILE_256) e = launch_dense<Tile256, MODE, true>(p, s);
+  else if (plan.tile == TILE_256) e = launch_large<MODE>(p, s);
   else if (plan.tile == TILE_128) e = launch_dense<Tile128, MODE, true>(p, s);
   else if (plan.tile == TILE_128D) e = launch_dense<Tile128D, MODE, true>(p, s);
   else if constexpr (MODE == DENSE_GATED) e = launch_dense<Tile64x128, MODE, true>(p, s);
