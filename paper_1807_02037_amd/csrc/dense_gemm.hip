@@ -614,11 +614,14 @@ enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 // where a work-group is alone on its compute unit and where all units hold as many as they can (forward, bf16, rows x inputs x outputs):
 //                  alone            full
 //   256 x 256      1.62             1.62     8192 x 65536 x 4096
-//   128 x 128      0.86 (two stages ahead at most)   1.16     64 x 4096 x 4096, 2048 x 4096 x 4096
+//   128 x 128      0.86 (one stage ahead)   1.10     64 x 4096 x 4096, 2048 x 4096 x 4096
 //   the same, deep 0.50             0.65     1024 x 2048 x 4096
 //   64 x 128       0.48             0.80     512 x 4096 x 4096, 1024 x 2048 x 4096
 //   64 x 64        0.33             0.52     64 x 4096 x 4096, 512 x 4096 x 4096
 //   32 x 128       0.38             0.62
+// Beside its stages a tile costs its first loads and its epilogue: 1 or 2 us where another work-group on the unit covers the rest, but with 256 x 256, where all units
+// write 128 KB each at a time, more: LARGE_FIXED, with a residual for the forward product (us, 256 x 256 / 128 x 128: 4096 x 512 x 4096 29 / 25, 4096 x 1024 x 4096 44 / 39, 4096 x 2048 x 4096 69 / 81; 7493 x 960 x 13760, SiLU,
+// residual 326 / 244).
 // us by tile and splits, of which it takes the starred:
 //                         128 x 128: 1    2      4      8     deep: 1  2      4     64 x 128: 1  2     4      64 x 64: 1  2      4
 //   24 x 2048 x 8192             30.9   21.3   15.7   16.7    18.9   16.1   14.9       18.8   15.8   13.9*      14.3   14.6   15.5
@@ -627,9 +630,11 @@ enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 //   1024 x 2048 x 4096           36.2   38.4   52.7   83.4    27.5*  44.3   62.7       31.2   45.9   61.8       40.0   54.1   70.5
 //   2048 x 4096 x 4096           79.5*  107    137    192     85.8   118    164        102    129    148        129    153    173
 struct DensePlan { int tile, splits; };
-struct TileCost { int tile, bm, bn, per_cu; float alone, full; };
-constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.62f, 1.62f}, {TILE_128, 128, 128, 2, 0.86f, 1.16f}, {TILE_128D, 128, 128, 1, 0.50f, 0.65f},
-                              {TILE_64X128, 64, 128, 2, 0.48f, 0.80f}, {TILE_64, 64, 64, 2, 0.33f, 0.52f}, {TILE_32, 32, 128, 2, 0.38f, 0.62f}};
+struct TileCost { int tile, bm, bn, per_cu; double alone, full, fixed; };
+constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.62, 1.62, 0.0}, {TILE_128, 128, 128, 2, 0.86, 1.10, 2.0}, {TILE_128D, 128, 128, 1, 0.50, 0.65, 2.0},
+                              {TILE_64X128, 64, 128, 2, 0.48, 0.80, 1.0}, {TILE_64, 64, 64, 2, 0.33, 0.52, 1.0}, {TILE_32, 32, 128, 2, 0.38, 0.62, 1.0}};
+
+constexpr double LARGE_FIXED[] = {20.0, 15.0, 8.0, 5.0};           // DENSE_FWD, GATED, DX, DW
 
 DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int srcs) {
   const long long stages = (red + 63) / 64 * segs;
@@ -639,10 +644,11 @@ DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int 
     if (mode == DENSE_GATED && (t.tile == TILE_64 || t.tile == TILE_32)) continue;     // a wave needs columns of both sources
     const int out_n = mode == DENSE_GATED ? t.bn / 2 : t.bn;
     const long long tiles = (M + t.bm - 1) / t.bm * ((N + out_n - 1) / out_n) * (mode == DENSE_DW ? srcs : 1), slots = 256LL * t.per_cu;
+    const double fixed = t.tile == TILE_256 ? LARGE_FIXED[mode] : t.fixed;
     for (int splits = 1; splits <= 16; ++splits) {
       const long long per = (stages + splits - 1) / splits, jobs = tiles * splits, rounds = jobs / slots, rest = jobs - rounds * slots;
       if (splits > 1 && per < 2) break;
-      double us = rounds * (per * (double)t.full + 2.0) + (rest == 0 ? 0.0 : per * (double)(rest > 256 ? t.full : t.alone) + 2.0);
+      double us = rounds * (per * t.full + fixed) + (rest == 0 ? 0.0 : per * (rest > 256 ? t.full : t.alone) + fixed);
       if (splits > 1) us += 3.0 + splits * (double)M * N * srcs * 2e-6;
       if (us < least) { least = us; best = {t.tile, splits}; }
     }
