@@ -11,16 +11,21 @@ namespace {
 
 // ---- gradients that enter the products, and column sums ----
 //
-// A work-group takes ROWS_PER rows of 512 columns, eight columns a thread: each input is read once, the gradient is written once in the storage type, and
+// A work-group takes a chunk of 32 rows (more where there are many, so that the chunks' sums stay small) of 512 columns, eight columns a thread: each input is read once, the gradient is written once in the storage type, and
 // the columns' sums over the work-group's rows, of the values before rounding, go to part[chunk of rows][n].  sum_rows adds the chunks in order.
-constexpr int PT = 256, PC = 512, ROWS_PER = 32, LANES = PC / 8, WAYS = PT / LANES;
+constexpr int PT = 256, PC = 512, LANES = PC / 8, WAYS = PT / LANES;
+int chunk_rows(long long m) {
+  int rows = 32;
+  while (rows < 1024 && m > 2048LL * rows) rows *= 2;
+  return rows;
+}
 
 struct GradP {
   const void *d, *g, *u;       // gradient that comes in; linear: g = pre; gated: g and u
   void *dz, *du;
   float* part;                 // or null
   long long M, ldd, ldo;       // ldd: d, g, u; ldo: dz, du
-  int N, act, gated;
+  int N, act, gated, rows;     // rows: of a chunk
 };
 
 template <typename T>
@@ -28,12 +33,12 @@ __global__ __launch_bounds__(PT) void act_grad_kernel(GradP p) {
   __shared__ float sums[WAYS][PC];
   const int across = (p.N + PC - 1) / PC, chunk = blockIdx.x / across, c0 = (int)(blockIdx.x % across) * PC;
   const int c = (threadIdx.x % LANES) * 8, way = threadIdx.x / LANES, n = c0 + c, cnt = p.N - n < 8 ? p.N - n : 8;
-  const long long r0 = (long long)chunk * ROWS_PER;
+  const long long r0 = (long long)chunk * p.rows;
   float total[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   constexpr int U = 4;                                            // rows in flight
   auto rows = [&](auto gated_c, auto slope_c) {                   // what is read: d; g; g and u
     constexpr bool GATED = decltype(gated_c)::value, SLOPE = decltype(slope_c)::value;
-    for (int r = way; r < ROWS_PER && r0 + r < p.M; r += WAYS * U) {
+    for (int r = way; r < p.rows && r0 + r < p.M; r += WAYS * U) {
       Raw<T, 8> d[U], g[SLOPE ? U : 1], u[GATED ? U : 1];
 #pragma unroll
       for (int k = 0; k < U; ++k) {
@@ -114,8 +119,9 @@ __global__ __launch_bounds__(PT) void zero_kernel(uint16_t* p, long long ld, int
     for (int h = 0; h < halves; ++h) p[(row * ld + i % N) * halves + h] = 0;
 }
 
-hipError_t act_grad(bool f32, const GradP& p, float* sums, hipStream_t s) {
-  const long long chunks = (p.M + ROWS_PER - 1) / ROWS_PER;
+hipError_t act_grad(bool f32, GradP& p, float* sums, hipStream_t s) {
+  p.rows = chunk_rows(p.M);
+  const long long chunks = (p.M + p.rows - 1) / p.rows;
   const long long groups = chunks * ((p.N + PC - 1) / PC);
   if (groups > 0x7fffffffLL) return hipErrorInvalidValue;
   const dim3 grid((unsigned)groups);
@@ -141,7 +147,7 @@ constexpr uint64_t WS_ALIGN = 256;
 uint64_t up(uint64_t b) { return (b + WS_ALIGN - 1) / WS_ALIGN * WS_ALIGN; }
 long long grad_pitch(int n) { return (n + 7) / 8 * 8; }
 uint64_t grad_bytes(const Layer& l) { return up((uint64_t)l.m * grad_pitch(l.n) * (l.f32 ? 4 : 2)); }
-uint64_t chunk_bytes(const Layer& l) { return up((uint64_t)((l.m + ROWS_PER - 1) / ROWS_PER) * l.n * 4); }
+uint64_t chunk_bytes(const Layer& l) { return up((uint64_t)((l.m + chunk_rows(l.m) - 1) / chunk_rows(l.m)) * l.n * 4); }
 
 #define NEED(cond, ...)        \
   do {                         \
@@ -154,6 +160,7 @@ uint64_t chunk_bytes(const Layer& l) { return up((uint64_t)((l.m + ROWS_PER - 1)
 lms_status check(const char* what, const Layer& l, int dtype, int wgrad_dtype) {
   NEED(l.m >= 0 && l.n >= 1 && l.k >= 1, "%s: rows must be >= 0, widths >= 1", what);
   NEED(l.m <= 0x7fffffffLL, "%s: more than 2^31 - 1 rows", what);
+  NEED(l.n <= 1 << 30 && l.k <= 1 << 30, "%s: widths above 2^30", what);
   NEED(l.act >= LMS_ACT_NONE && l.act <= LMS_ACT_GELU_TANH, "%s: unknown activation %d", what, l.act);
   NEED(dtype == LMS_BF16 || dtype == LMS_F32, "%s: dtype must be LMS_BF16 or LMS_F32", what);
   NEED(wgrad_dtype == LMS_F32 || wgrad_dtype == dtype, "%s: wgrad_dtype must be LMS_F32 or the dtype", what);
@@ -177,6 +184,12 @@ lms_status gated_layer(const lms_gated_desc* d, Layer& l) {
 lms_status aligned(const char* what, const Layer& l, const void* const* p, int count) {
   const uintptr_t low = l.f32 ? 3 : 1;
   for (int i = 0; i < count; ++i) NEED(((uintptr_t)p[i] & low) == 0, "%s: a pointer is not aligned to its elements", what);
+  return LMS_OK;
+}
+// what a call's workspace holds besides nothing
+lms_status space(const char* what, uint64_t need, const void* ws) {
+  NEED(!need || ws, "%s: workspace of %llu bytes required", what, (unsigned long long)need);
+  NEED(((uintptr_t)ws & 15) == 0, "%s: the workspace is not aligned", what);
   return LMS_OK;
 }
 lms_status done(const char* what, hipError_t e) {
@@ -247,7 +260,7 @@ lms_status linear_fwd(const lms_linear_desc* d, const void* x, const void* w, co
   if (l.m == 0) return LMS_OK;
   uint64_t need = 0;
   linear_workspace(d, LMS_LINEAR_FWD, &need);
-  NEED(!need || ws, "lms_linear_fwd: workspace of %llu bytes required", (unsigned long long)need);
+  if (const lms_status st = space("lms_linear_fwd", need, ws)) return st;
   DenseP p{};
   p.a[0] = x; p.b[0] = w; p.out[0] = y;
   p.bias = bias; p.res = res; p.pre = pre;
@@ -276,7 +289,7 @@ lms_status linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, c
   }
   uint64_t need = 0;
   linear_workspace(d, LMS_LINEAR_BWD, &need);
-  NEED(!need || ws, "lms_linear_bwd: workspace of %llu bytes required", (unsigned long long)need);
+  if (const lms_status st = space("lms_linear_bwd", need, ws)) return st;
   const bool with_act = l.act != LMS_ACT_NONE;
   const void* dz = dy;
   long long ldz = l.ldy;
@@ -322,7 +335,7 @@ lms_status gated_fwd(const lms_gated_desc* d, const void* x, const void* wg, con
   if (l.m == 0) return LMS_OK;
   uint64_t need = 0;
   gated_workspace(d, LMS_GATED_FWD, &need);
-  NEED(!need || ws, "lms_gated_fwd: workspace of %llu bytes required", (unsigned long long)need);
+  if (const lms_status st = space("lms_gated_fwd", need, ws)) return st;
   DenseP p{};
   p.a[0] = x; p.b[0] = wg; p.b[1] = wu; p.out[0] = h;
   p.pre = g; p.pre1 = u;
@@ -353,7 +366,7 @@ lms_status gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, con
   }
   uint64_t need = 0;
   gated_workspace(d, g ? LMS_GATED_BWD : LMS_GATED_BWD_RECOMPUTE, &need);
-  NEED(!need || ws, "lms_gated_bwd: workspace of %llu bytes required", (unsigned long long)need);
+  if (const lms_status st = space("lms_gated_bwd", need, ws)) return st;
   char* at = (char*)ws;
   const long long ldz = grad_pitch(l.n);
   const void* const dz[] = {at, at + grad_bytes(l)};

@@ -299,6 +299,7 @@ hipError_t launch_distill(bool f32, const DistillP& p, float* loss, hipStream_t 
 lms_status check(const char* what, const lms_distill_desc* d) {
   NEED(d->rows >= 0 && d->classes >= 1, "%s: rows must be >= 0, classes >= 1", what);
   NEED(d->rows <= 0x7fffffffLL, "%s: more than 2^31 - 1 rows", what);
+  NEED(d->classes <= 1 << 30, "%s: more than 2^30 classes", what);
   NEED(d->k >= 1 && d->k <= MAX_K, "%s: k must be in 1 .. %d", what, MAX_K);
   NEED(d->dtype == LMS_BF16 || d->dtype == LMS_F32, "%s: dtype must be LMS_BF16 or LMS_F32", what);
   NEED(d->ldz == 0 || (d->ldz >= d->classes && d->ldz <= (1LL << 40)), "%s: row pitch shorter than the row, or above 2^40", what);
@@ -325,6 +326,7 @@ lms_status distill(const lms_distill_desc* d, int which, const void* z, const fl
   NEED((((uintptr_t)t | (uintptr_t)ids | (uintptr_t)weight | (uintptr_t)lse_in | (uintptr_t)loss | (uintptr_t)row_loss | (uintptr_t)lse) & 3) == 0,
        "%s: a pointer is not aligned to its elements", what);
   NEED(!loss || ws || d->rows == 0, "%s: workspace of %llu bytes required", what, (unsigned long long)d->rows * 4);
+  NEED(((uintptr_t)ws & 15) == 0, "%s: the workspace is not aligned", what);
   DistillP p{};
   p.z = z; p.t = t; p.ids = ids; p.weight = weight; p.lse_in = lse_in;
   p.row_loss = row_loss; p.lse = lse; p.dz = dz;

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 
 import layer_oracle as O
+from helpers import kernel_names
 
 pytestmark = pytest.mark.gpu
 
@@ -286,6 +287,86 @@ def test_wide_pitches_in_fp32():
     wdx, e_dx, wdw, e_dw, _, _ = O.linear_bwd("none", O.f64(y), O.f64(x), O.f64(w), None, torch.float32, torch.float32)
     near(dx, wdx, e_dx, "dx")
     near(dw, wdw, e_dw, "dw")
+
+
+def test_wide_pitches_in_bf16():
+    """The same in bf16, through registers: pitches of 2^21 elements and more."""
+    torch, L, A = setup()
+    m, k, n, pitch = 300, 72, 136, (1 << 21) + 8
+    big = torch.empty(m * pitch, dtype=torch.bfloat16, device="cuda")
+    x, y, dx = (big.as_strided((m, c), (pitch, 1), at) for c, at in ((k, 0), (n, 1024), (k, 4096)))
+    x.copy_(matrix(torch, 1, m, k, torch.bfloat16))
+    w = matrix(torch, 2, k, n, torch.bfloat16, 0, 0.125)
+    d = L.linear_desc(m, n, k, ldx=pitch, ldy=pitch)
+    ws = space(torch, max(L.linear_workspace_bytes(d, A.LINEAR_FWD), L.linear_workspace_bytes(d, A.LINEAR_BWD)))
+    L.linear_fwd(d, ptr(x), ptr(w), None, None, ptr(y), None, ptr(ws), stream(torch))
+    want, _, e, _ = O.linear_fwd("none", O.f64(x), O.f64(w), None, None, torch.bfloat16)
+    near(y, want, e, "y")
+    dw, db = out(torch, k, n, torch.float32), out(torch, 1, n, torch.float32)
+    L.linear_bwd(d, ptr(y), ptr(x), ptr(w), None, ptr(dx), ptr(dw), ptr(db), ptr(ws), stream(torch))
+    wdx, e_dx, wdw, e_dw, wdb, e_db = O.linear_bwd("none", O.f64(y), O.f64(x), O.f64(w), None, torch.bfloat16, torch.float32)
+    near(dx, wdx, e_dx, "dx")
+    near(dw, wdw, e_dw, "dw")
+    near(db[0], wdb, e_db, "db")
+
+
+def test_bias_gradient_of_many_rows():
+    """More rows than chunks of the smallest size; the sums of a column of ones are exact."""
+    torch, L, A = setup()
+    m, k, n = 70001, 8, 24
+    dy = torch.ones(m, n, dtype=torch.bfloat16, device="cuda")
+    dy[:, 3] = -2.0
+    x, db = torch.ones(m, k, dtype=torch.bfloat16, device="cuda"), out(torch, 1, n, torch.float32)
+    dw = out(torch, k, n, torch.float32)
+    d = L.linear_desc(m, n, k)
+    ws = space(torch, L.linear_workspace_bytes(d, A.LINEAR_BWD))
+    L.linear_bwd(d, ptr(dy), ptr(x), None, None, None, ptr(dw), ptr(db), ptr(ws), stream(torch))
+    want = torch.full((n,), float(m), device="cuda")
+    want[3] = -2.0 * m
+    assert torch.equal(db[0], want) and torch.equal(dw, want.expand(k, n))
+
+
+@pytest.mark.parametrize("act", range(5))
+def test_whole_large_tiles(act):
+    """Several 256 x 256 tiles, whole and cut, of every product, against fp64 in norm: each element is rounded once, and what enters the backward products once more."""
+    torch, L, A = setup()
+    m, k, n = 4091, 4096, 4096
+    x, w, res = matrix(torch, 1, m, k, torch.bfloat16), matrix(torch, 2, k, n, torch.bfloat16, 0, k ** -0.5), matrix(torch, 3, m, n, torch.bfloat16)
+    bias = torch.randn(n, generator=torch.Generator().manual_seed(4)).cuda()
+    d = L.linear_desc(m, n, k, act=act)
+    ws = space(torch, max(L.linear_workspace_bytes(d, A.LINEAR_FWD), L.linear_workspace_bytes(d, A.LINEAR_BWD)))
+    y, pre, dx, dw, db = (out(torch, *s, t) for s, t in (((m, n), torch.bfloat16), ((m, n), torch.bfloat16), ((m, k), torch.bfloat16), ((k, n), torch.float32),
+                                                         ((1, n), torch.float32)))
+    L.linear_fwd(d, ptr(x), ptr(w), ptr(bias), ptr(res), ptr(y), ptr(pre), ptr(ws), stream(torch))
+    names = kernel_names(lambda: L.linear_bwd(d, ptr(res), ptr(x), ptr(w), ptr(pre), ptr(dx), ptr(dw), ptr(db), ptr(ws), stream(torch)))
+    assert sum("dense_large_kernel" in v for v in names) == 2, names
+    X, W, R, B = x.double(), w.double(), res.double(), bias.double()
+    P = X @ W + B
+    name = O.ACTS[act]
+
+    def same(got, want, u, what):
+        assert ((got.double() - want).norm() / want.norm()).item() <= u, what
+    Y, _ = O.act(name, P.cpu().numpy())
+    same(pre, P, 2.0 ** -8, "pre")
+    same(y, torch.from_numpy(Y).cuda() + R, 2.0 ** -8, "y")
+    D = R * torch.from_numpy(O.act(name, O.f64(pre))[1]).cuda()
+    same(dx, D @ W.T, 2.0 ** -7, "dx")
+    same(dw, X.T @ D, 2.0 ** -8 if act else 1e-5, "dw")
+    same(db[0], D.sum(0), 1e-5, "db")
+    g = L.gated_desc(m, n, k, act=act)
+    gws = space(torch, max(L.gated_workspace_bytes(g, c) for c in range(3)))
+    w2 = matrix(torch, 5, k, n, torch.bfloat16, 0, k ** -0.5)
+    h, dwg, dwu = out(torch, m, n, torch.bfloat16), out(torch, k, n, torch.float32), out(torch, k, n, torch.float32)
+    L.gated_fwd(g, ptr(x), ptr(w), ptr(w2), ptr(h), None, None, ptr(gws), stream(torch))
+    L.gated_bwd(g, ptr(res), ptr(x), ptr(w), ptr(w2), None, None, ptr(dx), ptr(dwg), ptr(dwu), ptr(gws), stream(torch))
+    W2 = w2.double()
+    G, U = X @ W, X @ W2
+    a, s = (torch.from_numpy(v).cuda() for v in O.act(name, G.cpu().numpy()))
+    DG, DU = R * U * s, R * a
+    same(h, a * U, 2.0 ** -8, "h")
+    same(dx, DG @ W.T + DU @ W2.T, 2.0 ** -7, "gated dx")
+    same(dwg, X.T @ DG, 2.0 ** -8, "dwg")
+    same(dwu, X.T @ DU, 2.0 ** -8, "dwu")
 
 
 def test_replays_of_a_captured_step():

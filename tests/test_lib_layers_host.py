@@ -27,7 +27,7 @@ def distill(**kw):
 
 BAD_SHAPES = [(dict(m=-1), "rows must be"), (dict(k=0), "widths"), (dict(m=1 << 31), "rows"), (dict(act=5), "activation"), (dict(act=-1), "activation"),
               (dict(dtype=A.I32), "dtype"), (dict(wgrad_dtype=A.I32), "wgrad_dtype"), (dict(dtype=A.F32, wgrad_dtype=A.BF16), "wgrad_dtype"),
-              (dict(ldx=15), "pitch"), (dict(ldw=7), "pitch"), (dict(ldx=-16), "pitch"), (dict(ldx=1 << 41), "pitch")]
+              (dict(k=(1 << 30) + 1, ldx=0), "widths above"), (dict(ldx=15), "pitch"), (dict(ldw=7), "pitch"), (dict(ldx=-16), "pitch"), (dict(ldx=1 << 41), "pitch")]
 
 
 @pytest.mark.parametrize("kw,match", BAD_SHAPES + [(dict(n=0), "widths"), (dict(ldy=7), "pitch"), (dict(ldr=1), "pitch")])
@@ -46,7 +46,7 @@ def test_gated_descriptors(kw, match):
     refused(L.gated_bwd, d, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, match=match)
 
 
-@pytest.mark.parametrize("kw,match", [(dict(rows=-1), "rows"), (dict(rows=1 << 31), "rows"), (dict(classes=0), "classes"), (dict(k=0), "k must be"), (dict(k=1025), "k must be"),
+@pytest.mark.parametrize("kw,match", [(dict(rows=-1), "rows"), (dict(rows=1 << 31), "rows"), (dict(classes=(1 << 30) + 1), "classes"), (dict(classes=0), "classes"), (dict(k=0), "k must be"), (dict(k=1025), "k must be"),
                                       (dict(dtype=A.I32), "dtype"), (dict(ldz=99), "pitch"), (dict(ldz=-1), "pitch"), (dict(temperature=0.0), "temperature"),
                                       (dict(temperature=-1.0), "temperature"), (dict(temperature=float("nan")), "temperature"),
                                       (dict(temperature=float("inf")), "temperature"), (dict(scale=float("inf")), "scale"), (dict(scale=float("nan")), "scale")])
@@ -114,6 +114,9 @@ def test_missing_workspaces():
     d = gated(m=100)
     assert L.gated_workspace_bytes(d, A.GATED_BWD) >= 2 * 100 * 8 * 2
     refused(L.gated_bwd, d, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, None, match="workspace of")
+    refused(L.linear_bwd, linear(m=100), PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR + 8, None, match="workspace is not aligned")
+    refused(L.gated_bwd, gated(), PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR + 4, None, match="workspace is not aligned")
+    refused(L.distill_loss_grad, distill(), PTR, PTR, PTR, None, PTR, PTR, PTR + 4, None, match="workspace is not aligned")
     refused(L.linear_workspace_bytes, linear(), 2, match="unknown call")
     refused(L.gated_workspace_bytes, gated(), 3, match="unknown call")
     refused(L.distill_workspace_bytes, distill(), -1, match="unknown call")
