@@ -41,6 +41,7 @@ hipError_t dense_product(int mode, bool f32, DenseP& p, hipStream_t s);
 uint64_t dense_ws(int mode, bool f32, long long M, int N, long long red, int segs, int srcs);
 
 hipError_t dense_bf16(int mode, DenseP& p, hipStream_t s);        // dense_gemm.hip
+hipError_t dense_bf16_pair(DenseP& dx, DenseP& dw, bool& taken, hipStream_t s);
 uint64_t dense_bf16_ws(int mode, long long M, int N, long long red, int segs, int srcs);
 uint64_t dense_f32_ws(int mode, long long M, int N, long long red, int segs, int srcs);
 hipError_t dense_f32(int mode, DenseP& p, hipStream_t s);         // dense_f32.hip

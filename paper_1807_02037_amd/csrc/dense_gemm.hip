@@ -102,7 +102,7 @@ __device__ __forceinline__ void tile_at(const DenseP& p, int tile, int& tm, int&
 }
 
 template <typename T, int MODE, bool DMA>
-__global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
+__device__ __forceinline__ void dense_tile(const DenseP& p, int job) {
   constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = MODE == DENSE_DX;
   constexpr int BM = T::BM, BN = T::BN, TM = T::TM, TN = T::TN, AV = T::AV, BV = T::BV, SUB = dense_sub<MODE, BN>();
   constexpr int OUT_N = MODE == DENSE_GATED ? BN / 2 : BN;       // output columns of a tile
@@ -111,8 +111,6 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
   typedef Operand<BN, B_FAST, SUB, DK> OpB;
   extern __shared__ __attribute__((aligned(256))) unsigned char dense_smem[];
 
-  const int job = xcd_order(p.ntiles * p.splits);
-  if (job < 0) return;
   const int split = job / p.ntiles;
   int tm, tn;
   tile_at(p, job - split * p.ntiles, tm, tn);
@@ -386,6 +384,20 @@ __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
   }
   __syncthreads();                                                // the buffers are free for the epilogue
   dense_epilogue<uint16_t, MODE, T::WTN, PRE>(p, acc, dense_smem + wave * T::EPI_WAVE, wm0, wn0, src, split, beside);
+}
+
+template <typename T, int MODE, bool DMA>
+__global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
+  const int job = xcd_order(p.ntiles * p.splits);
+  if (job >= 0) dense_tile<T, MODE, DMA>(p, job);
+}
+// Both products of a backward pass in one launch: of few tiles each, one after the other they leave most compute units idle twice.
+template <typename T>
+__global__ __launch_bounds__(T::NT, T::OCC) void dense_pair_kernel(DenseP dx, DenseP dw) {
+  const int job = xcd_order(dx.ntiles + dw.ntiles);
+  if (job < 0) return;
+  if (job < dx.ntiles) dense_tile<T, DENSE_DX, true>(dx, job);
+  else dense_tile<T, DENSE_DW, true>(dw, job - dx.ntiles);
 }
 
 // The 256 x 256 tile, one work-group on a compute unit, a wave on a SIMD.  Rows along the reduction arrive in whole 128-byte lines only if 64 of it are asked for at a time
@@ -683,6 +695,21 @@ hipError_t dense_mode(DenseP& p, hipStream_t s) {
 }
 
 }  // namespace
+
+// dx and dw together where both take 64 x 64 tiles and do not split; taken: whether they were.
+hipError_t dense_bf16_pair(DenseP& dx, DenseP& dw, bool& taken, hipStream_t s) {
+  typedef Tile64 T;
+  const DensePlan a = dense_plan(DENSE_DX, dx.M, dx.N, dx.red, dx.segs, dx.srcs), b = dense_plan(DENSE_DW, dw.M, dw.N, dw.red, dw.segs, dw.srcs);
+  taken = false;
+  if (a.tile != TILE_64 || b.tile != TILE_64 || a.splits != 1 || b.splits != 1 || !dma_ok(DENSE_DX, dx) || !dma_ok(DENSE_DW, dw)) return hipSuccess;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(dense_pair_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
+  if (attr != hipSuccess) return attr;
+  dx.splits = dw.splits = 1;
+  if (!dense_grid<T, DENSE_DX>(dx) || !dense_grid<T, DENSE_DW>(dw)) return hipErrorInvalidValue;
+  taken = true;
+  hipLaunchKernelGGL((dense_pair_kernel<T>), dim3((unsigned)xcd_grid((long long)dx.ntiles + dw.ntiles)), dim3(T::NT), T::LDS_BYTES, s, dx, dw);
+  return hipGetLastError();
+}
 
 hipError_t dense_bf16(int mode, DenseP& p, hipStream_t s) {
   switch (mode) {

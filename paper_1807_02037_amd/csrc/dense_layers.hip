@@ -200,28 +200,32 @@ lms_status done(const char* what, hipError_t e) {
 
 // dx = sum over sources of dz_s w_s^T; dw_s = x^T dz_s
 hipError_t layer_grads(const Layer& l, const void* const* dz, long long ldz, const void* x, const void* const* w, void* dx, void* const* dw, float* part, hipStream_t s) {
-  hipError_t e = hipSuccess;
+  DenseP px{}, pw{};
   if (dx) {
-    DenseP p{};
-    for (int i = 0; i < l.srcs; ++i) { p.a[i] = dz[i]; p.b[i] = w[i]; }
-    p.out[0] = dx;
-    p.M = l.m; p.N = l.k; p.red = l.n;
-    p.lda = ldz; p.ldb = l.ldw; p.ldo = l.ldx;
-    p.segs = l.srcs; p.srcs = 1;
-    p.part = part;
-    e = dense_product(DENSE_DX, l.f32, p, s);
+    for (int i = 0; i < l.srcs; ++i) { px.a[i] = dz[i]; px.b[i] = w[i]; }
+    px.out[0] = dx;
+    px.M = l.m; px.N = l.k; px.red = l.n;
+    px.lda = ldz; px.ldb = l.ldw; px.ldo = l.ldx;
+    px.segs = l.srcs; px.srcs = 1;
+    px.part = part;
   }
-  if (e == hipSuccess && dw[0]) {
-    DenseP p{};
-    p.a[0] = x;
-    for (int i = 0; i < l.srcs; ++i) { p.b[i] = dz[i]; p.out[i] = dw[i]; }
-    p.M = l.k; p.N = l.n; p.red = l.m;
-    p.lda = l.ldx; p.ldb = ldz; p.ldo = l.ldw;
-    p.segs = 1; p.srcs = l.srcs;
-    p.out_f32 = l.w32;
-    p.part = part;
-    e = dense_product(DENSE_DW, l.f32, p, s);
+  if (dw[0]) {
+    pw.a[0] = x;
+    for (int i = 0; i < l.srcs; ++i) { pw.b[i] = dz[i]; pw.out[i] = dw[i]; }
+    pw.M = l.k; pw.N = l.n; pw.red = l.m;
+    pw.lda = l.ldx; pw.ldb = ldz; pw.ldo = l.ldw;
+    pw.segs = 1; pw.srcs = l.srcs;
+    pw.out_f32 = l.w32;
+    pw.part = part;
   }
+  hipError_t e = hipSuccess;
+  if (dx && dw[0] && !l.f32) {
+    bool taken;
+    e = dense_bf16_pair(px, pw, taken, s);
+    if (taken || e != hipSuccess) return e;
+  }
+  if (dx) e = dense_product(DENSE_DX, l.f32, px, s);
+  if (e == hipSuccess && dw[0]) e = dense_product(DENSE_DW, l.f32, pw, s);
   return e;
 }
 
