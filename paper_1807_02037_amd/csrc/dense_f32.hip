@@ -356,6 +356,8 @@ struct F32Plan { int fm, splits; };
 struct F32Cost { int fm, per_cu; double alone, each; };
 constexpr F32Cost F32_COSTS[] = {{128, 2, 2.1, 1.95}, {64, 2, 0.66, 0.6}};
 
+constexpr int MAX_SPLITS = 48;
+
 F32Plan f32_plan(int mode, long long M, int N, long long red, int segs, int srcs) {
   const long long stages = (red + FK - 1) / FK * segs;
   F32Plan best = {128, 1};
@@ -364,12 +366,12 @@ F32Plan f32_plan(int mode, long long M, int N, long long red, int segs, int srcs
     if (mode == DENSE_GATED && t.fm == 64) continue;              // a wave needs columns of both sources
     const int out_n = mode == DENSE_GATED ? t.fm / 2 : t.fm;
     const long long tiles = (M + t.fm - 1) / t.fm * ((N + out_n - 1) / out_n) * (mode == DENSE_DW ? srcs : 1), slots = 256LL * t.per_cu;
-    for (int splits = 1; splits <= 16; ++splits) {
+    for (int splits = 1; splits <= MAX_SPLITS; ++splits) {
       const long long per = (stages + splits - 1) / splits, jobs = tiles * splits, rounds = jobs / slots, rest = jobs - rounds * slots;
       if (splits > 1 && per < 4) break;
       const double held = (double)((rest + 255) / 256) * t.each;
       double us = rounds * (per * t.per_cu * t.each + 2.0) + (rest == 0 ? 0.0 : per * (held > t.alone ? held : t.alone) + 2.0);
-      if (splits > 1) us += 3.0 + splits * (double)M * N * srcs * 2e-6;
+      if (splits > 1) us += 3.0 + splits * (0.15 + (double)M * N * srcs * 2e-6);
       if (us < least) { least = us; best = {t.fm, splits}; }
     }
   }

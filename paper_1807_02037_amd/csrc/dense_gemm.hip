@@ -622,7 +622,7 @@ typedef DenseTile<32, 128, 64, 4, 1, 4> Tile32;
 enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 
 // Tile and splits of a reduction, from the sizes alone (workspaces are planned before there are addresses), by an estimate of the time: rounds of work-groups
-// through the compute units, stages of 64 of the reduction each, and for splits the join's launch (3 us) and its passes over the sums (4 TB/s).  us of a stage, measured
+// through the compute units, stages of 64 of the reduction each, and for splits the join's launch (3 us, 0.15 a split) and its passes over the sums (4 TB/s).  us of a stage, measured
 // where a work-group is alone on its compute unit and where all units hold as many as they can (forward, bf16, rows x inputs x outputs):
 //                  alone            full
 //   256 x 256      1.62             1.62     8192 x 65536 x 4096
@@ -648,6 +648,8 @@ constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.62, 1.62, 0.0}, {TILE_12
 
 constexpr double LARGE_FIXED[] = {20.0, 15.0, 8.0, 5.0};           // DENSE_FWD, GATED, DX, DW
 
+constexpr int MAX_SPLITS = 48;
+
 DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int srcs) {
   const long long stages = (red + 63) / 64 * segs;
   DensePlan best = {TILE_128, 1};
@@ -657,11 +659,11 @@ DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int 
     const int out_n = mode == DENSE_GATED ? t.bn / 2 : t.bn;
     const long long tiles = (M + t.bm - 1) / t.bm * ((N + out_n - 1) / out_n) * (mode == DENSE_DW ? srcs : 1), slots = 256LL * t.per_cu;
     const double fixed = t.tile == TILE_256 ? LARGE_FIXED[mode] : t.fixed;
-    for (int splits = 1; splits <= 16; ++splits) {
+    for (int splits = 1; splits <= MAX_SPLITS; ++splits) {
       const long long per = (stages + splits - 1) / splits, jobs = tiles * splits, rounds = jobs / slots, rest = jobs - rounds * slots;
       if (splits > 1 && per < 2) break;
       double us = rounds * (per * t.full + fixed) + (rest == 0 ? 0.0 : per * (rest > 256 ? t.full : t.alone) + fixed);
-      if (splits > 1) us += 3.0 + splits * (double)M * N * srcs * 2e-6;
+      if (splits > 1) us += 3.0 + splits * (0.15 + (double)M * N * srcs * 2e-6);
       if (us < least) { least = us; best = {t.tile, splits}; }
     }
   }
