@@ -46,7 +46,7 @@ uint64_t dense_bf16_ws(int mode, long long M, int N, long long red, int segs, in
 uint64_t dense_f32_ws(int mode, long long M, int N, long long red, int segs, int srcs);
 hipError_t dense_f32(int mode, DenseP& p, hipStream_t s);         // dense_f32.hip
 hipError_t dense_join(int mode, bool f32, DenseP& p, hipStream_t s);        // dense_join.hip: p.part into the results
-bool dense_few_ok(int mode, long long M);                         // few rows (dense_few.hip)
+bool dense_few_ok(int mode, bool f32, long long M);               // few rows (dense_few.hip)
 uint64_t dense_few_ws(int mode, bool f32, long long M, int N, long long red);
 hipError_t dense_few(int mode, bool f32, DenseP& p, hipStream_t s);
 

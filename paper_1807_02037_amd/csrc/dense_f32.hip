@@ -371,7 +371,7 @@ F32Plan f32_plan(int mode, long long M, int N, long long red, int segs, int srcs
       if (splits > 1 && per < 4) break;
       const double held = (double)((rest + 255) / 256) * t.each;
       double us = rounds * (per * t.per_cu * t.each + 2.0) + (rest == 0 ? 0.0 : per * (held > t.alone ? held : t.alone) + 2.0);
-      if (splits > 1) us += 3.0 + splits * (0.15 + (double)M * N * srcs * 2e-6);
+      if (splits > 1) us += 5.0 + splits * (0.15 + (double)M * N * srcs * 2e-6);
       if (us < least) { least = us; best = {t.fm, splits}; }
     }
   }

@@ -1,8 +1,8 @@
 // Linear layers and gated projections of few rows (tokens answered one by one): bound by reading the weights once.
 //
 // A work-group takes CB columns, CB / 8 lanes for eight columns each of one reduction index; the other lanes and waves take others, KU consecutive ones at a
-// time: that many 16-byte loads of weights in flight a lane, and one load of each row of x.  Products are ordinary fp32 instructions; up to eight
-// rows they stay behind the loads.  The partial sums meet by shuffles and in LDS, in a fixed order.
+// time: that many 16-byte loads of weights in flight a lane, and one load of each row of x.  Products are ordinary fp32 instructions, which for
+// so few rows stay behind the loads.  The partial sums meet by shuffles and in LDS, in a fixed order.
 //
 // Memory gives its rate only to whole 128-byte lines of a row of weights, and only if all 256 compute units ask.  So layers of at least 16384 columns take CB = 64
 // and the whole reduction; narrower ones take 128 columns and split the reduction until there are 256 work-groups, and a second launch joins the
@@ -148,15 +148,19 @@ hipError_t few_rows(DenseP& p, hipStream_t s) {
 template <typename T, int MODE>
 hipError_t few_mode(DenseP& p, hipStream_t s) {
   if (p.M == 1) return few_rows<T, MODE, 1>(p, s);
-  if (p.M == 2) return few_rows<T, MODE, 2>(p, s);
-  if constexpr (MODE == DENSE_FWD)
-    if (p.M > 4) return few_rows<T, MODE, 8>(p, s);
-  return few_rows<T, MODE, 4>(p, s);
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (MODE == DENSE_FWD)
+      if (p.M > 4) return few_rows<T, MODE, 8>(p, s);
+    if (p.M > 2) return few_rows<T, MODE, 4>(p, s);
+  }
+  return few_rows<T, MODE, 2>(p, s);
 }
 
 }  // namespace
 
-bool dense_few_ok(int mode, long long M) { return (mode == DENSE_FWD && M <= 8) || (mode == DENSE_GATED && M <= 4); }       // registers
+// In bf16 from three rows on the matrix cores' tiles are as fast or faster (us, rows here / there: 4096 -> 4096 4 rows 15.3, 8 rows 17.8 / 13.4; 4096 -> 16384 8 rows 37.6 / 30.7; gated
+// 4096 -> 8192 4 rows 35.7 / 34.9); in fp32 they are slower up to eight (24.0 / 29.6), of which a gated projection's do not fit the registers.
+bool dense_few_ok(int mode, bool f32, long long M) { return (mode == DENSE_FWD || mode == DENSE_GATED) && M <= (!f32 ? 2 : mode == DENSE_FWD ? 8 : 4); }
 
 uint64_t dense_few_ws(int mode, bool f32, long long M, int N, long long red) {
   const int splits = few_splits(mode, f32, N, red);

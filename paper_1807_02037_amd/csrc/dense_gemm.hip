@@ -622,7 +622,7 @@ typedef DenseTile<32, 128, 64, 4, 1, 4> Tile32;
 enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 
 // Tile and splits of a reduction, from the sizes alone (workspaces are planned before there are addresses), by an estimate of the time: rounds of work-groups
-// through the compute units, stages of 64 of the reduction each, and for splits the join's launch (3 us, 0.15 a split) and its passes over the sums (4 TB/s).  us of a stage, measured
+// through the compute units, stages of 64 of the reduction each, and for splits the join's launch (5 us: 3 on the device, and the host's; 0.15 a split) and its passes over the sums (4 TB/s).  us of a stage, measured
 // where a work-group is alone on its compute unit and where all units hold as many as they can (forward, bf16, rows x inputs x outputs):
 //                  alone            full
 //   256 x 256      1.62             1.62     8192 x 65536 x 4096
@@ -637,7 +637,7 @@ enum { TILE_256, TILE_128, TILE_128D, TILE_64X128, TILE_64, TILE_32 };
 // us by tile and splits, of which it takes the starred:
 //                         128 x 128: 1    2      4      8     deep: 1  2      4     64 x 128: 1  2     4      64 x 64: 1  2      4
 //   24 x 2048 x 8192             30.9   21.3   15.7   16.7    18.9   16.1   14.9       18.8   15.8   13.9       14.3   14.6   15.5   (32 x 128, 4: 13.9*)
-//   256 x 2048 x 2048            26.0   17.8   14.9   16.9    19.9   15.6   14.1       16.3   13.9   13.4       12.8   12.7*  13.6
+//   256 x 2048 x 2048            26.0   17.8   14.9   16.9    19.9   15.6   14.1       16.3   13.9   13.4       12.8*  12.7   13.6
 //   512 x 4096 x 4096            61.8   42.2   39.2   51.2    42.9   34.2   43.9       36.0*  39.1   47.1       40.6   47.9   56.1
 //   1024 x 2048 x 4096           36.2   38.4   52.7   83.4    27.5*  44.3   62.7       31.2   45.9   61.8       40.0   54.1   70.5
 //   2048 x 4096 x 4096           79.5*  107    137    192     85.8   118    164        102    129    148        129    153    173
@@ -663,7 +663,7 @@ DensePlan dense_plan(int mode, long long M, int N, long long red, int segs, int 
       const long long per = (stages + splits - 1) / splits, jobs = tiles * splits, rounds = jobs / slots, rest = jobs - rounds * slots;
       if (splits > 1 && per < 2) break;
       double us = rounds * (per * t.full + fixed) + (rest == 0 ? 0.0 : per * (rest > 256 ? t.full : t.alone) + fixed);
-      if (splits > 1) us += 3.0 + splits * (0.15 + (double)M * N * srcs * 2e-6);
+      if (splits > 1) us += 5.0 + splits * (0.15 + (double)M * N * srcs * 2e-6);
       if (us < least) { least = us; best = {t.tile, splits}; }
     }
   }

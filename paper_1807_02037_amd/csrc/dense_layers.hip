@@ -237,11 +237,11 @@ uint64_t grads_ws(const Layer& l, bool dx, bool dw) {
 }  // namespace
 
 uint64_t dense_ws(int mode, bool f32, long long M, int N, long long red, int segs, int srcs) {
-  if (dense_few_ok(mode, M)) return dense_few_ws(mode, f32, M, N, red);
+  if (dense_few_ok(mode, f32, M)) return dense_few_ws(mode, f32, M, N, red);
   return f32 ? dense_f32_ws(mode, M, N, red, segs, srcs) : dense_bf16_ws(mode, M, N, red, segs, srcs);
 }
 hipError_t dense_product(int mode, bool f32, DenseP& p, hipStream_t s) {
-  if (dense_few_ok(mode, p.M)) return dense_few(mode, f32, p, s);
+  if (dense_few_ok(mode, f32, p.M)) return dense_few(mode, f32, p, s);
   return f32 ? dense_f32(mode, p, s) : dense_bf16(mode, p, s);
 }
 
