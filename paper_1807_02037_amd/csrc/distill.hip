@@ -183,16 +183,17 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillP p) {
   if (!p.lse_in) l = __builtin_amdgcn_logf(s);                    // -inf where all classes are masked
   if (p.lse && tid == 0) p.lse[row] = m / p.temp + l * LN2;
 
+  // T^2 sum p (log p - log q) as T sum p (T log p + T log sum - (z - m)): neither the type's lowest value in z nor T^2 overflows on the way to a loss that does not
   if (p.part || p.row_loss) {
     const float log_total = __builtin_amdgcn_logf(total);
     float loss = 0.f, unused = 0.f;
     for (int j = tid; j < p.k; j += NT)
       if (s_id[j] >= 0) {
         const float log_p = (s_p[j] - top) * c2 - log_total, prob = __builtin_amdgcn_exp2f(log_p);
-        if (prob != 0.f) loss += s_q[j] == -inf ? inf : prob * (log_p - ((s_q[j] - m) * c2 - l));     // on a masked class: inf
+        if (prob != 0.f) loss += s_q[j] == -inf ? inf : prob * (p.temp * LN2 * (log_p + l) - (s_q[j] - m));     // on a masked class: inf
       }
     group_reduce<NT>(loss, unused, s_red, add, add);
-    loss *= LN2 * p.temp * p.temp;
+    loss *= p.temp;
     if (tid == 0) {
       if (p.row_loss) p.row_loss[row] = loss;
       if (p.part) p.part[row] = weight == 0.f ? 0.f : weight * loss;

@@ -1,0 +1,48 @@
+"""The distillation loss where numbers are as large as the types hold: student logits of the type's lowest value, temperatures whose square overflows."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_teacher_on_classes_of_the_lowest_value(dtype):
+    """A student's logit of the type's lowest value is an ordinary number: the loss of a teacher's entry there is large and finite, T p (max z - z) and what is beside it nothing."""
+    import torch
+    import paper_1807_02037_amd as L
+    A = L.abi
+    kind, code = (torch.bfloat16, A.BF16) if dtype == "bf16" else (torch.float32, A.F32)
+    low = torch.finfo(kind).min
+    z = torch.zeros(3, 70, device="cuda").to(kind)
+    z[:, 5] = low
+    z[2, 6] = low
+    ids = torch.tensor([[5, -1], [5, 9], [5, 6]], dtype=torch.int32, device="cuda")
+    t = torch.zeros(3, 2, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    for temp in (1.0, 0.5, 0.25):
+        d = L.distill_desc(3, 70, 2, temperature=temp, scale=0.125, dtype=code)
+        ws, row, loss = torch.empty(256, dtype=torch.uint8, device="cuda"), torch.empty(3, device="cuda"), torch.empty(1, device="cuda")
+        dz = torch.empty_like(z)
+        L.distill_fwd(d, z.data_ptr(), t.data_ptr(), ids.data_ptr(), None, loss.data_ptr(), row.data_ptr(), None, ws.data_ptr(), s)
+        L.distill_loss_grad(d, z.data_ptr(), t.data_ptr(), ids.data_ptr(), None, loss.data_ptr(), dz.data_ptr(), ws.data_ptr(), s)
+        torch.cuda.synchronize()
+        want = [-low * temp, -low * temp / 2, -low * temp]
+        # a handful of roundings of 32 bits
+        for r in range(3):
+            assert abs(row[r].item() - want[r]) <= 8 * 2.0 ** -24 * want[r], (temp, row.tolist())
+        assert abs(loss.item() - 0.125 * sum(want)) <= 16 * 2.0 ** -24 * 0.125 * sum(want)
+        assert torch.isfinite(dz.float()).all() and abs(dz[0, 5].float().item() + 0.125 * temp) < 1e-6
+
+
+def test_very_large_temperatures():
+    """T^2 beyond the largest number: rows on which teacher and student agree have no loss, and not NaN."""
+    import torch
+    import paper_1807_02037_amd as L
+    A = L.abi
+    z, t = torch.zeros(2, 1, device="cuda"), torch.zeros(2, 1, device="cuda")
+    ids = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    d = L.distill_desc(2, 1, 1, temperature=1e20, dtype=A.F32)
+    ws, loss, dz = torch.empty(256, dtype=torch.uint8, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(z)
+    L.distill_loss_grad(d, z.data_ptr(), t.data_ptr(), ids.data_ptr(), None, loss.data_ptr(), dz.data_ptr(), ws.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert loss.item() == 0.0 and not dz.any() and not math.isnan(loss.item())
