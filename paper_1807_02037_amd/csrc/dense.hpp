@@ -79,7 +79,7 @@ __device__ __forceinline__ void act_one(float v, float& value, float& slope) {
   if constexpr (ACT == LMS_ACT_GELU_TANH) {                       // (1 + tanh t) / 2 = sigmoid(2 t)
     const float s = sigmoid(2.f * GELU_A * (v + GELU_B * v * v * v));
     value = v * s;
-    slope = s + value * (1.f - s) * 2.f * GELU_A * (1.f + 3.f * GELU_B * v * v);
+    slope = s + value * (1.f - s) * 2.f * GELU_A * (1.f + 3.f * GELU_B * __builtin_fminf(v * v, 1e30f));     // finite where value (1 - s) is 0
   }
 }
 // f(integral_constant<int, act>): one uniform branch around the arithmetic of a vector
