@@ -33,6 +33,7 @@ struct DenseP {
   int out_f32;                 // DW: out is fp32 (else the storage type)
   int splits, stages_per_split, stages;   // the reduction's stages, segments one after the other
   int ntm, ntn, ntiles;
+  int job0, jobs;              // of ntiles * splits work-groups, those of this launch (launch_jobs)
   float* part;                 // splits > 1: sums of a split, [split][source][M][N]
 };
 
@@ -51,6 +52,26 @@ uint64_t dense_few_ws(int mode, bool f32, long long M, int N, long long red);
 hipError_t dense_few(int mode, bool f32, DenseP& p, hipStream_t s);
 
 namespace {
+
+// A grid holds less than 2^32 threads: the work-groups of a product, NT threads each, go in as many launches as that takes.
+template <int NT, typename F>
+hipError_t launch_jobs(DenseP& p, F&& launch) {
+  constexpr long long most = (1LL << 31) / NT;
+  const long long total = (long long)p.ntiles * p.splits;
+  for (long long at = 0; at < total; at += most) {
+    p.job0 = (int)at;
+    p.jobs = (int)(total - at < most ? total - at : most);
+    launch(dim3((unsigned)xcd_grid(p.jobs)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+// A work-group's number among ntiles * splits, or -1.
+__device__ __forceinline__ int dense_job(const DenseP& p) {
+  const int job = xcd_order(p.jobs);
+  return job < 0 ? -1 : p.job0 + job;
+}
 
 // act(v) and act'(v) by the definitions.  exp(x) as 2^(x log2 e) in one instruction and the reciprocal's instruction are each within an ulp, far below
 // the rounding of a 16-bit result; for 32 bits the product of x and log2 e adds |x| 2^-24, which counts only where the sigmoid vanishes.

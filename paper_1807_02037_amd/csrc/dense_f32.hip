@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256, 2) void dense_f32_dma_kernel(DenseP p) {
   static_assert(RING * STAGE >= 4 * epi_wave_bytes(W) && 2 * RING * STAGE <= 163840, "epilogue; two work-groups a compute unit");
   __shared__ __attribute__((aligned(256))) unsigned char lds[RING * STAGE];
 
-  const int job = xcd_order(p.ntiles * p.splits);
+  const int job = dense_job(p);
   if (job < 0) return;
   const int split = job / p.ntiles, tile = job - split * p.ntiles;
   int tm = tile % p.ntm, tn = tile / p.ntm, src = 0;
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256, FM == 128 ? 2 : 4) void dense_f32_kernel(Dense
   static_assert(16 * F_TILE >= 4 * epi_wave_bytes(W) && (FM == 128 ? 2 : 4) * 16 * F_TILE <= 163840, "two stages of two operands; epilogue; work-groups of a compute unit");
   __shared__ __attribute__((aligned(16))) float lds[4 * F_TILE];
 
-  const int job = xcd_order(p.ntiles * p.splits);
+  const int job = dense_job(p);
   if (job < 0) return;
   const int split = job / p.ntiles, tile = job - split * p.ntiles;
   int tm = tile % p.ntm, tn = tile / p.ntm, src = 0;
@@ -391,8 +391,7 @@ hipError_t launch_f32(Kernel kernel, DenseP& p, hipStream_t s) {
   p.ntm = (int)tm;
   p.ntn = (int)tn;
   p.ntiles = (int)(tm * tn);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(256), 0, s, p);
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = launch_jobs<256>(p, [&](dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p); });
   return e == hipSuccess && p.splits > 1 ? dense_join(MODE, true, p, s) : e;
 }
 

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(FT) void dense_few_kernel(DenseP p) {
   constexpr int S = MODE == DENSE_GATED ? 2 : 1, LC = CB / 8, KG = FT / LC;
   constexpr int KU = S * R * sizeof(T) >= 32 ? 4 : 8;             // registers
   __shared__ float sums[FT / 64][S][R][CB];
-  const int job = xcd_order(p.ntiles * p.splits);
+  const int job = dense_job(p);
   if (job < 0) return;
   const int split = job / p.ntiles;
   const int tid = threadIdx.x, c = (tid % LC) * 8, n = (job - split * p.ntiles) * CB + c, cnt = p.N - n < 8 ? p.N - n : 8;
@@ -134,8 +134,7 @@ hipError_t few_rows(DenseP& p, hipStream_t s) {
   auto launch = [&](auto cb) {
     constexpr int CB = decltype(cb)::value;
     p.ntiles = (p.N + CB - 1) / CB;
-    hipLaunchKernelGGL((dense_few_kernel<T, MODE, R, CB>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(FT), 0, s, p);
-    return hipGetLastError();
+    return launch_jobs<FT>(p, [&](dim3 grid) { hipLaunchKernelGGL((dense_few_kernel<T, MODE, R, CB>), grid, dim3(FT), 0, s, p); });
   };
   if (p.splits > 1) {
     const hipError_t e = launch(std::integral_constant<int, 128>{});

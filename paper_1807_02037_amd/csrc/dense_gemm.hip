@@ -388,7 +388,7 @@ __device__ __forceinline__ void dense_tile(const DenseP& p, int job) {
 
 template <typename T, int MODE, bool DMA>
 __global__ __launch_bounds__(T::NT, T::OCC) void dense_kernel(DenseP p) {
-  const int job = xcd_order(p.ntiles * p.splits);
+  const int job = dense_job(p);
   if (job >= 0) dense_tile<T, MODE, DMA>(p, job);
 }
 // Both products of a backward pass in one launch: of few tiles each, one after the other they leave most compute units idle twice.
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(DenseP p) {
   typedef Operand<BN, B_FAST, SUB, DK> OpB;
   extern __shared__ __attribute__((aligned(256))) unsigned char dense_smem[];
 
-  const int job = xcd_order(p.ntiles * p.splits);
+  const int job = dense_job(p);
   if (job < 0) return;
   const int split = job / p.ntiles;
   int tm, tn, src = 0;
@@ -579,7 +579,7 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(DenseP p) {
   dense_epilogue<uint16_t, MODE, 128, 2>(p, acc, dense_smem + wave * epi_wave_bytes(128), wm0, wn0, src, split, beside);
 }
 
-// Tiles and stages of a launch; false: more than a grid holds.
+// Tiles and stages of a product; false: more than an int numbers.
 template <typename T, int MODE>
 bool dense_grid(DenseP& p) {
   p.stages = (int)((p.red + T::DK - 1) / T::DK) * p.segs;
@@ -600,8 +600,7 @@ hipError_t launch_large(DenseP& p, hipStream_t s) {
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(dense_large_kernel<MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
   if (attr != hipSuccess) return attr;
   if (!dense_grid<T, MODE>(p)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((dense_large_kernel<MODE>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(T::NT), T::LDS_BYTES, s, p);
-  return hipGetLastError();
+  return launch_jobs<T::NT>(p, [&](dim3 grid) { hipLaunchKernelGGL((dense_large_kernel<MODE>), grid, dim3(T::NT), T::LDS_BYTES, s, p); });
 }
 
 template <typename T, int MODE, bool DMA>
@@ -609,8 +608,7 @@ hipError_t launch_dense(DenseP& p, hipStream_t s) {
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(dense_kernel<T, MODE, DMA>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
   if (attr != hipSuccess) return attr;
   if (!dense_grid<T, MODE>(p)) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((dense_kernel<T, MODE, DMA>), dim3((unsigned)xcd_grid((long long)p.ntiles * p.splits)), dim3(T::NT), T::LDS_BYTES, s, p);
-  return hipGetLastError();
+  return launch_jobs<T::NT>(p, [&](dim3 grid) { hipLaunchKernelGGL((dense_kernel<T, MODE, DMA>), grid, dim3(T::NT), T::LDS_BYTES, s, p); });
 }
 
 // Deep rings hide what a stage takes to arrive where there is one work-group on a compute unit; two work-groups hide each other's.
@@ -708,6 +706,7 @@ hipError_t dense_bf16_pair(DenseP& dx, DenseP& dw, bool& taken, hipStream_t s) {
   if (attr != hipSuccess) return attr;
   dx.splits = dw.splits = 1;
   if (!dense_grid<T, DENSE_DX>(dx) || !dense_grid<T, DENSE_DW>(dw)) return hipErrorInvalidValue;
+  if ((long long)dx.ntiles + dw.ntiles > (1LL << 31) / T::NT) return hipSuccess;     // more than one grid holds
   taken = true;
   hipLaunchKernelGGL((dense_pair_kernel<T>), dim3((unsigned)xcd_grid((long long)dx.ntiles + dw.ntiles)), dim3(T::NT), T::LDS_BYTES, s, dx, dw);
   return hipGetLastError();

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(64) void dense_join_kernel(DenseP p) {
 template <typename T, int MODE>
 hipError_t launch_join(DenseP& p, hipStream_t s) {
   const long long vectors = (long long)((p.N + 7) / 8) * p.M * (MODE == DENSE_DW ? p.srcs : 1);
-  if ((vectors + 63) / 64 > 0x7fffffffLL) return hipErrorInvalidValue;
+  if (vectors > 0xffffff00LL) return hipErrorInvalidValue;        // a grid holds less than 2^32 threads; results this large are not split
   hipLaunchKernelGGL((dense_join_kernel<T, MODE>), dim3((unsigned)((vectors + 63) / 64)), dim3(64), 0, s, p);
   return hipGetLastError();
 }

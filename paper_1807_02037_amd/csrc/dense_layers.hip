@@ -89,10 +89,10 @@ __global__ __launch_bounds__(PT) void act_grad_kernel(GradP p) {
     }
 }
 
-// out[n] = sum over the chunks of part[chunk][n], in order
-__global__ __launch_bounds__(PT) void sum_rows_kernel(const float* part, long long chunks, int N, float* out) {
+// out[n] = sum over the chunks of part[chunk][n], in order, for the columns from n0 on
+__global__ __launch_bounds__(PT) void sum_rows_kernel(const float* part, long long chunks, int N, int n0, float* out) {
   __shared__ float sums[8][32];
-  const int c = threadIdx.x & 31, way = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
+  const int c = threadIdx.x & 31, way = threadIdx.x >> 5, n = n0 + (int)blockIdx.x * 32 + c;
   float t = 0.f;
   if (n < N) {
     long long i = way;
@@ -114,25 +114,27 @@ __global__ __launch_bounds__(PT) void sum_rows_kernel(const float* part, long lo
 }
 
 __global__ __launch_bounds__(PT) void zero_kernel(uint16_t* p, long long ld, int N, long long rows, int halves) {
-  const long long i = (long long)blockIdx.x * PT + threadIdx.x, row = i / N;
-  if (row < rows)
-    for (int h = 0; h < halves; ++h) p[(row * ld + i % N) * halves + h] = 0;
+  for (long long i = (long long)blockIdx.x * PT + threadIdx.x; i < rows * N; i += (long long)gridDim.x * PT)
+    for (int h = 0; h < halves; ++h) p[(i / N * ld + i % N) * halves + h] = 0;
 }
 
 hipError_t act_grad(bool f32, GradP& p, float* sums, hipStream_t s) {
   p.rows = chunk_rows(p.M);
   const long long chunks = (p.M + p.rows - 1) / p.rows;
   const long long groups = chunks * ((p.N + PC - 1) / PC);
-  if (groups > 0x7fffffffLL) return hipErrorInvalidValue;
+  if (groups >= (1LL << 32) / PT) return hipErrorInvalidValue;    // a grid holds less than 2^32 threads; this many have more rows and columns than fit the device's memory
   const dim3 grid((unsigned)groups);
   if (f32) hipLaunchKernelGGL(act_grad_kernel<float>, grid, dim3(PT), 0, s, p);
   else hipLaunchKernelGGL(act_grad_kernel<uint16_t>, grid, dim3(PT), 0, s, p);
-  if (sums) hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((p.N + 31) / 32)), dim3(PT), 0, s, p.part, chunks, p.N, sums);
+  if (sums)
+    for (int n0 = 0; n0 < p.N; n0 += 1 << 28)                     // 2^23 work-groups
+      hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)(((p.N - n0 < 1 << 28 ? p.N - n0 : 1 << 28) + 31) / 32)), dim3(PT), 0, s, p.part, chunks, p.N, n0, sums);
   return hipGetLastError();
 }
 
 hipError_t fill_zero(void* out, long long rows, int N, long long ld, bool f32, hipStream_t s) {
-  hipLaunchKernelGGL(zero_kernel, dim3((unsigned)((rows * N + PT - 1) / PT)), dim3(PT), 0, s, (uint16_t*)out, ld, N, rows, f32 ? 2 : 1);
+  const long long groups = (rows * N + PT - 1) / PT;
+  hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20)), dim3(PT), 0, s, (uint16_t*)out, ld, N, rows, f32 ? 2 : 1);
   return hipGetLastError();
 }
 

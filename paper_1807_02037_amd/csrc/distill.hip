@@ -27,6 +27,7 @@ struct DistillP {
   float* part;                 // weight * row loss, or null
   void* dz;                    // or null
   long long rows, ldz;
+  long long row0;              // first row of this launch
   int classes, k, table;       // table: a power of two, at least 2 k
   float temp, scale;
 };
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillP p) {
   const auto larger = [](float a, float b) { return fmaxf(a, b); };
   const float inf = __builtin_inff();
   const int tid = threadIdx.x;
-  const long long row = blockIdx.x;
+  const long long row = p.row0 + blockIdx.x;
   const T* z = (const T*)p.z + row * p.ldz;
   T* dz = (T*)p.dz + (p.dz ? row * p.ldz : 0);
   const float weight = p.weight ? p.weight[row] : 1.f;
@@ -259,13 +260,21 @@ __global__ __launch_bounds__(512) void distill_loss_kernel(const float* part, lo
   }
 }
 
-// The fewest threads and vectors that hold a row; rows beyond 98304 classes (fp32: 65536) are read again for the gradient.
+// The fewest threads and vectors that hold a row; rows beyond 98304 classes (fp32: 65536) are read again for the gradient.  A grid holds less than 2^32
+// threads: more rows go in several launches.
 template <typename T>
-void launch_rows(const DistillP& p, hipStream_t s) {
+hipError_t launch_rows(DistillP& p, hipStream_t s) {
   constexpr bool wide = sizeof(T) == 4;
   auto go = [&](auto nt, auto nv) {
     constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-    hipLaunchKernelGGL((distill_kernel<T, NT, NV>), dim3((unsigned)p.rows), dim3(NT), (3 * p.k + (p.dz ? p.table : 0)) * 4, s, p);
+    constexpr long long most = (1LL << 31) / NT;
+    for (p.row0 = 0; p.row0 < p.rows; p.row0 += most) {
+      const long long take = p.rows - p.row0 < most ? p.rows - p.row0 : most;
+      hipLaunchKernelGGL((distill_kernel<T, NT, NV>), dim3((unsigned)take), dim3(NT), (3 * p.k + (p.dz ? p.table : 0)) * 4, s, p);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   };
 #define ROWS(NT, NV) if (p.classes <= NT * 8 * NV) return go(std::integral_constant<int, NT>{}, std::integral_constant<int, NV>{})
   ROWS(64, 1);
@@ -277,14 +286,12 @@ void launch_rows(const DistillP& p, hipStream_t s) {
   ROWS(1024, 8);
   if constexpr (!wide) ROWS(1024, 12);
 #undef ROWS
-  go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
+  return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
 
-hipError_t launch_distill(bool f32, const DistillP& p, float* loss, hipStream_t s) {
-  if (p.rows > 0) {
-    if (f32) launch_rows<float>(p, s);
-    else launch_rows<uint16_t>(p, s);
-  }
+hipError_t launch_distill(bool f32, DistillP& p, float* loss, hipStream_t s) {
+  const hipError_t e = f32 ? launch_rows<float>(p, s) : launch_rows<uint16_t>(p, s);
+  if (e != hipSuccess) return e;
   if (loss) hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(512), 0, s, p.part, p.rows, p.scale, loss);
   return hipGetLastError();
 }
