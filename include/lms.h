@@ -438,7 +438,7 @@ lms_status lms_swap_decode_staged(void* dst, const void* src_host, uint64_t nume
  * else it is at least the row's length.  bf16 matrices may start at any even address and have any pitch; those whose addresses are multiples of 16
  * bytes and whose lengths and pitches are multiples of 8 elements are faster.  fp32 pointers are 4-byte aligned.  Outputs must not
  * overlap inputs, unless said so.  The elements between the end of a row and the next one are neither read into a result nor written.
- * Calls with m = 0 write what does not depend on rows (weight and bias gradients: zeros).
+ * Calls with m = 0 (rows = 0) write what does not depend on rows (weight and bias gradients and the loss: zeros); tensors of as many rows may then be NULL.
  * Widths are at most 2^30.  workspace: device memory of at least the bytes that *_workspace_bytes says, 16-byte aligned, may be NULL for 0; what it holds before and after means nothing.
  * LMS_EINVAL with a message for bad arguments, before anything is launched. */
 typedef enum { LMS_ACT_NONE = 0, LMS_ACT_RELU = 1, LMS_ACT_SILU = 2, LMS_ACT_GELU = 3 /* by erf */, LMS_ACT_GELU_TANH = 4 } lms_act;

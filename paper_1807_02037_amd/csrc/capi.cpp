@@ -338,12 +338,12 @@ lms_status lms_linear_workspace_bytes(const lms_linear_desc* d, int32_t which, u
 }
 lms_status lms_linear_fwd(const lms_linear_desc* d, const void* x, const void* w, const float* bias, const void* res, void* y, void* pre, void* workspace,
                           void* stream) {
-  NEED(d && x && w && y, "lms_linear_fwd: null argument");
+  NEED(d && w && (d->m == 0 || (x && y)), "lms_linear_fwd: null argument");
   return lms::linear_fwd(d, x, w, bias, res, y, pre, workspace, stream);
 }
 lms_status lms_linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, const void* w, const void* pre, void* dx, void* dw, float* dbias,
                           void* workspace, void* stream) {
-  NEED(d && dy, "lms_linear_bwd: null argument");
+  NEED(d && (d->m == 0 || dy), "lms_linear_bwd: null argument");
   return lms::linear_bwd(d, dy, x, w, pre, dx, dw, dbias, workspace, stream);
 }
 lms_status lms_gated_workspace_bytes(const lms_gated_desc* d, int32_t which, uint64_t* bytes) {
@@ -351,12 +351,12 @@ lms_status lms_gated_workspace_bytes(const lms_gated_desc* d, int32_t which, uin
   return lms::gated_workspace(d, which, bytes);
 }
 lms_status lms_gated_fwd(const lms_gated_desc* d, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, void* stream) {
-  NEED(d && x && wg && wu && h, "lms_gated_fwd: null argument");
+  NEED(d && wg && wu && (d->m == 0 || (x && h)), "lms_gated_fwd: null argument");
   return lms::gated_fwd(d, x, wg, wu, h, g, u, workspace, stream);
 }
 lms_status lms_gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, const void* wg, const void* wu, const void* g, const void* u, void* dx,
                          void* dwg, void* dwu, void* workspace, void* stream) {
-  NEED(d && dh, "lms_gated_bwd: null argument");
+  NEED(d && (d->m == 0 || dh), "lms_gated_bwd: null argument");
   return lms::gated_bwd(d, dh, x, wg, wu, g, u, dx, dwg, dwu, workspace, stream);
 }
 lms_status lms_distill_workspace_bytes(const lms_distill_desc* d, int32_t which, uint64_t* bytes) {
@@ -365,17 +365,17 @@ lms_status lms_distill_workspace_bytes(const lms_distill_desc* d, int32_t which,
 }
 lms_status lms_distill_fwd(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, float* loss, float* row_loss,
                            float* lse, void* workspace, void* stream) {
-  NEED(d && z && t && ids, "lms_distill_fwd: null argument");
+  NEED(d && (d->rows == 0 || (z && t && ids)), "lms_distill_fwd: null argument");
   return lms::distill(d, LMS_DISTILL_FWD, z, t, ids, weight, nullptr, loss, row_loss, lse, nullptr, workspace, stream);
 }
 lms_status lms_distill_bwd(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, const float* lse, void* dz,
                            void* workspace, void* stream) {
-  NEED(d && z && t && ids && lse && dz, "lms_distill_bwd: null argument");
+  NEED(d && (d->rows == 0 || (z && t && ids && lse && dz)), "lms_distill_bwd: null argument");
   return lms::distill(d, LMS_DISTILL_BWD, z, t, ids, weight, lse, nullptr, nullptr, nullptr, dz, workspace, stream);
 }
 lms_status lms_distill_loss_grad(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, float* loss, void* dz,
                                  void* workspace, void* stream) {
-  NEED(d && z && t && ids && loss && dz, "lms_distill_loss_grad: null argument");
+  NEED(d && loss && (d->rows == 0 || (z && t && ids && dz)), "lms_distill_loss_grad: null argument");
   return lms::distill(d, LMS_DISTILL_LOSS_GRAD, z, t, ids, weight, nullptr, loss, nullptr, nullptr, dz, workspace, stream);
 }
 

@@ -281,8 +281,8 @@ lms_status linear_bwd(const lms_linear_desc* d, const void* dy, const void* x, c
                       void* stream) {
   Layer l;
   if (const lms_status st = linear_layer(d, l)) return st;
-  NEED((!dx || w) && (!dw || x), "lms_linear_bwd: dx needs w, dw needs x");
-  NEED(l.act == LMS_ACT_NONE || pre, "lms_linear_bwd: a layer with an activation needs pre");
+  NEED(l.m == 0 || ((!dx || w) && (!dw || x)), "lms_linear_bwd: dx needs w, dw needs x");
+  NEED(l.m == 0 || l.act == LMS_ACT_NONE || pre, "lms_linear_bwd: a layer with an activation needs pre");
   const void* all[] = {dy, x, w, pre, dx, dw};
   if (const lms_status st = aligned("lms_linear_bwd", l, all, 6)) return st;
   NEED((((uintptr_t)db | (l.w32 ? (uintptr_t)dw : 0)) & 3) == 0, "lms_linear_bwd: dw or dbias is not aligned to its elements");
@@ -358,8 +358,8 @@ lms_status gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, con
   if (const lms_status st = gated_layer(d, l)) return st;
   NEED(!g == !u, "lms_gated_bwd: g and u are both given or both NULL");
   NEED(!dwg == !dwu, "lms_gated_bwd: dwg and dwu are both given or both NULL");
-  NEED((wg && wu) || (g && !dx), "lms_gated_bwd: wg and wu are needed for dx, and where g and u are not given");
-  NEED(x || (g && !dwg), "lms_gated_bwd: x is needed for dwg and dwu, and where g and u are not given");
+  NEED(l.m == 0 || (wg && wu) || (g && !dx), "lms_gated_bwd: wg and wu are needed for dx, and where g and u are not given");
+  NEED(l.m == 0 || x || (g && !dwg), "lms_gated_bwd: x is needed for dwg and dwu, and where g and u are not given");
   const void* all[] = {dh, x, wg, wu, g, u, dx, dwg, dwu};
   if (const lms_status st = aligned("lms_gated_bwd", l, all, 9)) return st;
   NEED(!l.w32 || (((uintptr_t)dwg | (uintptr_t)dwu) & 3) == 0, "lms_gated_bwd: dwg or dwu is not aligned to its elements");

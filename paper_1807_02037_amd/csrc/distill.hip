@@ -291,8 +291,8 @@ hipError_t launch_rows(DistillP& p, hipStream_t s) {
 
 hipError_t launch_distill(bool f32, DistillP& p, float* loss, hipStream_t s) {
   const hipError_t e = f32 ? launch_rows<float>(p, s) : launch_rows<uint16_t>(p, s);
-  if (e != hipSuccess) return e;
-  if (loss) hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(512), 0, s, p.part, p.rows, p.scale, loss);
+  if (e != hipSuccess || !loss) return e;
+  hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(512), 0, s, p.part, p.rows, p.scale, loss);
   return hipGetLastError();
 }
 
