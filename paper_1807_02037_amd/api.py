@@ -286,12 +286,18 @@ def swap_moved_bytes(host, numel):
     return b.value
 
 
+def _fill(d, **fields):
+    """Sets a descriptor's fields; a number that its field cannot hold is an error (ctypes would cut it to the low bits)."""
+    for name, value in fields.items():
+        setattr(d, name, value)
+        if isinstance(value, int) and isinstance(getattr(d, name), int) and getattr(d, name) != value:
+            raise LmsError(A.EINVAL, f"{type(d).__name__}.{name}: {value} does not fit")
+    return d
+
+
 def linear_desc(m, n, k, act=A.ACT_NONE, dtype=A.BF16, wgrad_dtype=A.F32, ldx=0, ldw=0, ldy=0, ldr=0):
     """m rows, n outputs, k inputs; ld*: row pitches in elements, 0 = dense."""
-    d = A.LinearDesc()
-    d.m, d.n, d.k, d.act, d.dtype, d.wgrad_dtype = m, n, k, act, dtype, wgrad_dtype
-    d.ldx, d.ldw, d.ldy, d.ldr = ldx, ldw, ldy, ldr
-    return d
+    return _fill(A.LinearDesc(), m=m, n=n, k=k, act=act, dtype=dtype, wgrad_dtype=wgrad_dtype, ldx=ldx, ldw=ldw, ldy=ldy, ldr=ldr)
 
 
 def linear_workspace_bytes(desc, which):
@@ -310,10 +316,7 @@ def linear_bwd(desc, dy, x, w, pre, dx, dw, dbias, workspace, stream):
 
 def gated_desc(m, f, k, act=A.ACT_SILU, dtype=A.BF16, wgrad_dtype=A.F32, ldx=0, ldw=0, ldh=0):
     """m rows, f hidden units, k inputs."""
-    d = A.GatedDesc()
-    d.m, d.f, d.k, d.act, d.dtype, d.wgrad_dtype = m, f, k, act, dtype, wgrad_dtype
-    d.ldx, d.ldw, d.ldh = ldx, ldw, ldh
-    return d
+    return _fill(A.GatedDesc(), m=m, f=f, k=k, act=act, dtype=dtype, wgrad_dtype=wgrad_dtype, ldx=ldx, ldw=ldw, ldh=ldh)
 
 
 def gated_workspace_bytes(desc, which):
@@ -332,9 +335,7 @@ def gated_bwd(desc, dh, x, wg, wu, g, u, dx, dwg, dwu, workspace, stream):
 
 def distill_desc(rows, classes, k, temperature=1.0, scale=1.0, dtype=A.BF16, ldz=0):
     """rows of logits over classes, k teacher entries a row."""
-    d = A.DistillDesc()
-    d.rows, d.classes, d.k, d.dtype, d.ldz, d.temperature, d.scale = rows, classes, k, dtype, ldz, temperature, scale
-    return d
+    return _fill(A.DistillDesc(), rows=rows, classes=classes, k=k, dtype=dtype, ldz=ldz, temperature=temperature, scale=scale)
 
 
 def distill_workspace_bytes(desc, which):

@@ -1,4 +1,7 @@
-"""Arguments of the language-model layers at their edges, without a GPU: calls without rows take the null pointers that empty tensors have."""
+"""Arguments of the language-model layers at their edges, without a GPU: calls without rows take the null pointers that empty tensors have; numbers that a field of a
+descriptor cannot hold are refused and not cut."""
+import pytest
+
 import paper_1807_02037_amd as L
 from paper_1807_02037_amd import abi as A
 from test_lib_layers_host import PTR, distill, gated, linear, refused
@@ -27,3 +30,13 @@ def test_with_rows_every_pointer_is_needed():
     refused(L.linear_bwd, linear(m=1), None, PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, match="null argument")
     refused(L.gated_bwd, gated(m=1), None, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, match="null argument")
     refused(L.distill_bwd, distill(rows=1), None, PTR, PTR, None, PTR, PTR, None, None, match="null argument")
+
+
+@pytest.mark.parametrize("make,kw", [(linear, dict(n=(1 << 32) + 8)), (linear, dict(k=(1 << 32) + 16)), (linear, dict(m=(1 << 64) + 4)), (linear, dict(act=1 << 32)),
+                                     (linear, dict(ldx=1 << 64)), (gated, dict(f=(1 << 32) + 8)), (gated, dict(k=-(1 << 32) + 16)), (gated, dict(ldh=(1 << 64) + 8)),
+                                     (distill, dict(rows=1 << 64)), (distill, dict(classes=(1 << 32) + 100)), (distill, dict(k=(1 << 32) + 5)),
+                                     (distill, dict(ldz=1 << 64))])
+def test_numbers_that_do_not_fit(make, kw):
+    with pytest.raises(L.LmsError, match=next(iter(kw))) as e:
+        make(**kw)
+    assert e.value.status == A.EINVAL
