@@ -25,6 +25,12 @@ def _bf16(*shape, scale, gen):
     return (torch.randn(*shape, generator=gen, device="cuda") * scale).to(torch.bfloat16)
 
 
+def _expect(what, t, shape, dtype):
+    """The layers take addresses: a tensor of another size, type or place would be read beyond its end."""
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of {shape} on the GPU is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
 class Student:
     """Weights, the buffers of a batch of `rows` positions, and the calls on them.  keep: the forward pass keeps g and u for the backward pass (else it computes
     them again)."""
@@ -71,17 +77,23 @@ class Student:
 
     def logits(self, x):
         """Logits of the batch (the student's own buffer)."""
+        _expect("x", x, (self.rows, self.width), torch.bfloat16)
         self._forward((self.gated, self.down, self.head), x, self.h, self.g, self.u, self.y, self.z, torch.cuda.current_stream().cuda_stream)
         return self.z
 
     def answer(self, x):
         """Logits of one position: x is (1, width)."""
+        _expect("x", x, (1, self.width), torch.bfloat16)
         h, y, z = (torch.empty(1, c, dtype=torch.bfloat16, device="cuda") for c in (self.hidden, self.width, self.classes))
         self._forward(self._descs(1), x, h, None, None, y, z, torch.cuda.current_stream().cuda_stream)
         return z
 
     def step(self, x, t, ids, weight=None):
         """Forward, loss and gradients of a batch; t, ids: the teacher's top logits and their classes.  Returns the loss (a tensor, not waited for)."""
+        _expect("t", t, (self.rows, self.top), torch.float32)
+        _expect("ids", ids, (self.rows, self.top), torch.int32)
+        if weight is not None:
+            _expect("weight", weight, (self.rows,), torch.float32)
         s, w, g, ws = torch.cuda.current_stream().cuda_stream, self.weights, self.grads, self.ws.data_ptr()
         self.logits(x)
         L.distill_loss_grad(self.loss_desc, self.z.data_ptr(), t.data_ptr(), ids.data_ptr(), None if weight is None else weight.data_ptr(),
