@@ -441,7 +441,7 @@ lms_status lms_swap_decode_staged(void* dst, const void* src_host, uint64_t nume
  * Calls with m = 0 (rows = 0) write what does not depend on rows (weight and bias gradients and the loss: zeros); tensors of as many rows may then be NULL.
  * Widths are at most 2^30.  workspace: device memory of at least the bytes that *_workspace_bytes says, 16-byte aligned, may be NULL for 0; what it holds before and after means nothing.
  * LMS_EINVAL with a message for bad arguments, before anything is launched. */
-typedef enum { LMS_ACT_NONE = 0, LMS_ACT_RELU = 1, LMS_ACT_SILU = 2, LMS_ACT_GELU = 3 /* by erf */, LMS_ACT_GELU_TANH = 4 } lms_act;
+typedef enum { LMS_ACT_NONE = 0, LMS_ACT_RELU = 1 /* 0 for NaN */, LMS_ACT_SILU = 2, LMS_ACT_GELU = 3 /* by erf */, LMS_ACT_GELU_TANH = 4 } lms_act;
 
 /* Linear layer of m rows, k inputs, n outputs: y = act(x w + bias) + res. */
 typedef struct {

@@ -1,13 +1,14 @@
 // Matrix products of language-model layers in bf16 on the matrix cores (see DenseP for what a launch computes).
 //
-// A work-group of four waves computes BM x BN outputs; the reduction runs 64 at a time through two buffers in LDS.  Every operand lies in
+// A work-group of four waves computes BM x BN outputs; the reduction runs 64 at a time through a ring of two to five stages in LDS.  Every operand lies in
 // LDS as it lies in memory: where the reduction index is contiguous (rows of x, of the gradients, and of w for the data gradient) rows of 64 of it, read as
 // they are; where it is not (w for the forward pass, both operands of the weight gradient) rows of 128 columns, or of 64, read with the gfx950 LDS transpose
 // read.  So no operand is ever transposed in memory.  Products are taken transposed (the operand of the columns first): a lane then holds four consecutive
 // columns of a row, and the epilogue turns 32 rows at a time through LDS into vectors of eight columns.
 //
 // Two ways into LDS: buffer loads that write LDS, for operands on 16-byte boundaries, where offsets beyond the descriptor read zeros and so
-// ragged tiles need no branches; and through registers, at any address and for any length, element by element only where a vector crosses the end of a row.
+// ragged tiles need no branches; and through registers and two stages, at any address and for any length: a vector of columns across the end of a row is the row's last eight,
+// shifted; only a partial last stage and rows of fewer than eight columns go element by element.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -678,6 +679,7 @@ bool dma_ok(int mode, const DenseP& p) {
   return (at & 15) == 0 && ((p.lda | p.ldb | a_len | b_len) & 7) == 0 && p.lda < (1 << 21) && p.ldb < (1 << 21);
 }
 
+// What cannot go by those loads takes the plan's splits, for which the workspace was sized, on one of two tiles through registers: the plan's costs are not theirs.
 template <int MODE>
 hipError_t dense_mode(DenseP& p, hipStream_t s) {
   const DensePlan plan = dense_plan(MODE, p.M, p.N, p.red, p.segs, p.srcs);

@@ -13,6 +13,8 @@ namespace {
 //
 // A work-group takes a chunk of 32 rows (more where there are many, so that the chunks' sums stay small) of 512 columns, eight columns a thread: each input is read once, the gradient is written once in the storage type, and
 // the columns' sums over the work-group's rows, of the values before rounding, go to part[chunk of rows][n].  sum_rows adds the chunks in order.
+// The rounding to bf16 is the price of products on the bf16 matrix cores: dx and dw of a layer with an activation are 0.0023 from the exact result (relative norm) where
+// their own rounding alone is 0.0017.  Carrying the rest of each value as a second bf16 operand would restore that and double the products (8192 x 4096 x 4096: 435 of 483 us).
 constexpr int PT = 256, PC = 512, LANES = PC / 8, WAYS = PT / LANES;
 int chunk_rows(long long m) {
   int rows = 32;
