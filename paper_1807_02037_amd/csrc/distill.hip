@@ -123,7 +123,8 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillP p) {
   };
 
   // ---- the teacher: p, and the logits of its classes (before any of them is written over: dz may be z) ----
-  const float c2 = LOG2E / p.temp;                                // e^((a - b) / T) = 2^((a - b) c2); the difference first: the type's lowest value times c2 is -inf
+  // e^((a - b) / T) = 2^((a - b) c2); the difference first: the type's lowest value times c2 is -inf.  A T below the least normal number would make c2 inf and the largest class 0 inf.
+  const float c2 = fminf(LOG2E / p.temp, 3.4028235e38f);
   float top = -inf;
   if (p.dz) {
     for (int i = tid; i < p.table; i += NT) s_set[i] = -1;

@@ -46,3 +46,20 @@ def test_very_large_temperatures():
     ws, loss, dz = torch.empty(256, dtype=torch.uint8, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(z)
     L.distill_loss_grad(d, z.data_ptr(), t.data_ptr(), ids.data_ptr(), None, loss.data_ptr(), dz.data_ptr(), ws.data_ptr(), torch.cuda.current_stream().cuda_stream)
     assert loss.item() == 0.0 and not dz.any() and not math.isnan(loss.item())
+
+
+@pytest.mark.parametrize("temp", [1e-30, 1e-37, 1e-40, 1.5e-45])
+def test_very_small_temperatures(temp):
+    """The limit: all probability on the largest logit.  Teacher and student agree on it, so neither loss nor gradient is left, and no NaN."""
+    import torch
+    import paper_1807_02037_amd as L
+    A = L.abi
+    z = torch.zeros(2, 40, device="cuda")
+    z[:, 3] = 1.0
+    ids = torch.tensor([[3, 4], [-1, 3]], dtype=torch.int32, device="cuda")
+    t = torch.tensor([[2.0, 1.0], [0.0, 5.0]], device="cuda")
+    d = L.distill_desc(2, 40, 2, temperature=temp, dtype=A.F32)
+    ws, loss, dz = torch.empty(256, dtype=torch.uint8, device="cuda"), torch.full((1,), 9.0, device="cuda"), torch.full_like(z, 9.0)
+    L.distill_loss_grad(d, z.data_ptr(), t.data_ptr(), ids.data_ptr(), None, loss.data_ptr(), dz.data_ptr(), ws.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert loss.item() == 0.0 and not dz.any()
