@@ -510,6 +510,38 @@ lms_status lms_distill_bwd(const lms_distill_desc* d, const void* z, const float
 lms_status lms_distill_loss_grad(const lms_distill_desc* d, const void* z, const float* t, const int32_t* ids, const float* weight, float* loss,
                                  void* dz, void* workspace, void* stream);
 
+/* ------------------------------------------------------------------ sequences
+ * Layers that mix the positions of a sequence or normalise it, and what serves them token by token.  Conventions of the language-model layers above: raw device pointers,
+ * row-major matrices of LMS_BF16 or LMS_F32 with row pitches in elements (0 = dense), sums and states in fp32, a workspace the caller owns, nothing allocated or waited for. */
+
+/* Gated recurrence of `channels` independent channels over sequences that lie one after the other in `rows` rows:
+ *   a = sigmoid(g), h_t = a_t h_{t-1} + (1 - a_t) x_t, y_t = h_t act(o_t), or h_t where o is NULL. */
+typedef struct {
+  int64_t rows;             /* positions of all sequences, 0 .. 2^31 - 65 */
+  int32_t seqs;             /* sequences (lms_recur_step: slots), 1 .. 2^30 */
+  int32_t channels;         /* 1 .. 2^26 */
+  int32_t act;              /* lms_act of the output gate */
+  int32_t dtype;            /* of x, g, o, y and their gradients */
+  int64_t ldx, ldy;         /* row pitches of x, g, o and their gradients (they may be columns of one matrix); of y and dy */
+} lms_recur_desc;
+typedef enum { LMS_RECUR_FWD = 0, LMS_RECUR_BWD = 1 } lms_recur_which;
+lms_status lms_recur_workspace_bytes(const lms_recur_desc* d, int32_t which, uint64_t* bytes);
+/* Bytes of `kept`, what the forward pass leaves for the backward pass (16-byte aligned; may be NULL where this is 0): a state in fp32 for every 64 rows. */
+lms_status lms_recur_kept_bytes(const lms_recur_desc* d, uint64_t* bytes);
+/* offsets: seqs + 1 row numbers that do not fall, sequence s has the rows offsets[s] .. offsets[s+1]-1 (none where they are equal); rows before the first and behind the last are neither read into
+ * a result nor written.  NULL: all have rows / seqs rows.  h0, last: seqs x channels fp32, dense, the states before and after each sequence (last: h0 for one without
+ * rows); either may be NULL (h0: zeros), and they must not overlap.  kept: NULL where no backward pass follows. */
+lms_status lms_recur_fwd(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, void* y, float* last, void* kept,
+                         void* workspace, void* stream);
+/* dlast: gradient of last, or NULL for zeros.  With e = dy act(o): dh_t = e_t + a_{t+1} dh_{t+1}, at a sequence's end e_t + dlast; dx = (1 - a) dh, dg = dh (h_{t-1} - x) a (1 - a),
+ * dout = dy h act'(o), dh0 = a dh of the first position.  h is computed again from kept.  dx, dg, dout and dh0 may each be NULL.  Deterministic. */
+lms_status lms_recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, const void* kept,
+                         const float* dlast, void* dx, void* dg, void* dout, float* dh0, void* workspace, void* stream);
+/* One position of each of `rows` requests (at most 65536): row i goes on from state[slots[i]] and leaves next[slots[i]]; state and next: seqs x channels fp32, the same or apart.
+ * Slots that no row has stay as they are, in next too.  Rows whose slot is outside 0 .. seqs-1, as -1, are left alone.  Rows of the same slot are consecutive positions of one request. */
+lms_status lms_recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream);
+
+
 
 #ifdef __cplusplus
 }

@@ -11,5 +11,6 @@ from .api import (  # noqa: F401
     swap_encoded_bytes, swap_encode, swap_decode, swap_moved_bytes,
     linear_desc, linear_workspace_bytes, linear_fwd, linear_bwd, gated_desc, gated_workspace_bytes, gated_fwd, gated_bwd,
     distill_desc, distill_workspace_bytes, distill_fwd, distill_bwd, distill_loss_grad,
+    recur_desc, recur_workspace_bytes, recur_kept_bytes, recur_fwd, recur_bwd, recur_step,
 )
 from .models import build_graph  # noqa: F401

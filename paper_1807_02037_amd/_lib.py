@@ -21,6 +21,7 @@ ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
 LINEAR_FWD, LINEAR_BWD = 0, 1
 GATED_FWD, GATED_BWD, GATED_BWD_RECOMPUTE = 0, 1, 2
 DISTILL_FWD, DISTILL_BWD, DISTILL_LOSS_GRAD = 0, 1, 2
+RECUR_FWD, RECUR_BWD = 0, 1
 CONV_FWD, CONV_DGRAD, CONV_WGRAD, CONV_WGRAD_BIAS = 0, 1, 2, 3
 
 
@@ -83,6 +84,11 @@ class DistillDesc(C.Structure):
                 ("temperature", C.c_float), ("scale", C.c_float)]
 
 
+class RecurDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("seqs", C.c_int32), ("channels", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32),
+                ("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
 P = C.POINTER
 VP = C.c_void_p
 _SIGS = {
@@ -143,6 +149,11 @@ _SIGS = {
     "lms_distill_fwd": (C.c_int, [P(DistillDesc)] + [VP] * 9),
     "lms_distill_bwd": (C.c_int, [P(DistillDesc)] + [VP] * 8),
     "lms_distill_loss_grad": (C.c_int, [P(DistillDesc)] + [VP] * 8),
+    "lms_recur_workspace_bytes": (C.c_int, [P(RecurDesc), C.c_int32, P(C.c_uint64)]),
+    "lms_recur_kept_bytes": (C.c_int, [P(RecurDesc), P(C.c_uint64)]),
+    "lms_recur_fwd": (C.c_int, [P(RecurDesc)] + [VP] * 10),
+    "lms_recur_bwd": (C.c_int, [P(RecurDesc)] + [VP] * 14),
+    "lms_recur_step": (C.c_int, [P(RecurDesc)] + [VP] * 8),
 }
 EXPORTS = sorted(_SIGS)
 

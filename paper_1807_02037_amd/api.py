@@ -354,3 +354,32 @@ def distill_bwd(desc, z, t, ids, weight, lse, dz, workspace, stream):
 
 def distill_loss_grad(desc, z, t, ids, weight, loss, dz, workspace, stream):
     _ck(A.lib().lms_distill_loss_grad(C.byref(desc), z, t, ids, weight, loss, dz, workspace, stream))
+
+
+def recur_desc(rows, channels, seqs=1, act=A.ACT_NONE, dtype=A.BF16, ldx=0, ldy=0):
+    """rows positions of seqs sequences (of a step: seqs slots)."""
+    return _fill(A.RecurDesc(), rows=rows, seqs=seqs, channels=channels, act=act, dtype=dtype, ldx=ldx, ldy=ldy)
+
+
+def recur_workspace_bytes(desc, which):
+    b = C.c_uint64()
+    _ck(A.lib().lms_recur_workspace_bytes(C.byref(desc), which, C.byref(b)))
+    return b.value
+
+
+def recur_kept_bytes(desc):
+    b = C.c_uint64()
+    _ck(A.lib().lms_recur_kept_bytes(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def recur_fwd(desc, x, g, o, offsets, h0, y, last, kept, workspace, stream):
+    _ck(A.lib().lms_recur_fwd(C.byref(desc), x, g, o, offsets, h0, y, last, kept, workspace, stream))
+
+
+def recur_bwd(desc, dy, x, g, o, offsets, h0, kept, dlast, dx, dg, dout, dh0, workspace, stream):
+    _ck(A.lib().lms_recur_bwd(C.byref(desc), dy, x, g, o, offsets, h0, kept, dlast, dx, dg, dout, dh0, workspace, stream))
+
+
+def recur_step(desc, x, g, o, slots, state, next_state, y, stream):
+    _ck(A.lib().lms_recur_step(C.byref(desc), x, g, o, slots, state, next_state, y, stream))

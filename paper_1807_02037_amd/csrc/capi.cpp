@@ -40,6 +40,13 @@ lms_status gated_bwd(const lms_gated_desc* d, const void* dh, const void* x, con
 lms_status distill_workspace(const lms_distill_desc* d, int which, uint64_t* bytes);
 lms_status distill(const lms_distill_desc* d, int which, const void* z, const float* t, const int32_t* ids, const float* weight, const float* lse_in, float* loss,
                    float* row_loss, float* lse, void* dz, void* ws, void* stream);
+lms_status recur_workspace(const lms_recur_desc* d, int which, uint64_t* bytes);
+lms_status recur_kept(const lms_recur_desc* d, uint64_t* bytes);
+lms_status recur_fwd(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, void* y, float* last, void* kept, void* ws,
+                     void* stream);
+lms_status recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, const void* kept, const float* dlast,
+                     void* dx, void* dg, void* dout, float* dh0, void* ws, void* stream);
+lms_status recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream);
 }  // namespace lms
 
 using lms::set_error;
@@ -377,6 +384,29 @@ lms_status lms_distill_loss_grad(const lms_distill_desc* d, const void* z, const
                                  void* workspace, void* stream) {
   NEED(d && loss && (d->rows == 0 || (z && t && ids && dz)), "lms_distill_loss_grad: null argument");
   return lms::distill(d, LMS_DISTILL_LOSS_GRAD, z, t, ids, weight, nullptr, loss, nullptr, nullptr, dz, workspace, stream);
+}
+
+lms_status lms_recur_workspace_bytes(const lms_recur_desc* d, int32_t which, uint64_t* bytes) {
+  NEED(d && bytes, "lms_recur_workspace_bytes: null argument");
+  return lms::recur_workspace(d, which, bytes);
+}
+lms_status lms_recur_kept_bytes(const lms_recur_desc* d, uint64_t* bytes) {
+  NEED(d && bytes, "lms_recur_kept_bytes: null argument");
+  return lms::recur_kept(d, bytes);
+}
+lms_status lms_recur_fwd(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, void* y, float* last, void* kept,
+                         void* workspace, void* stream) {
+  NEED(d && (d->rows == 0 || (x && g && y)), "lms_recur_fwd: null argument");
+  return lms::recur_fwd(d, x, g, o, offsets, h0, y, last, kept, workspace, stream);
+}
+lms_status lms_recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, const void* kept,
+                         const float* dlast, void* dx, void* dg, void* dout, float* dh0, void* workspace, void* stream) {
+  NEED(d && (d->rows == 0 || (dy && x && g)), "lms_recur_bwd: null argument");
+  return lms::recur_bwd(d, dy, x, g, o, offsets, h0, kept, dlast, dx, dg, dout, dh0, workspace, stream);
+}
+lms_status lms_recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream) {
+  NEED(d && (d->rows == 0 || (x && g && slots && state && next && y)), "lms_recur_step: null argument");
+  return lms::recur_step(d, x, g, o, slots, state, next, y, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,564 @@
+// Gated recurrence over packed sequences, its backward pass and its single-token form (include/lms.h has the formulas).
+//
+// A span of rows maps the state h that enters it to A h + H, A the product of its a, or 0 where a sequence begins in it.  Backwards, with r = a dh, what a row passes to the one before it
+// (dh = e + r of the row behind), it maps r to A r + R, A = 0 where a sequence ends in it.  Those zeros are negative, which no product is: behind them what enters does not count, were it NaN.
+// Spans compose, so rows need not wait for one another:
+// a wave takes a few rows of 256 channels and holds what it has read of them in registers; the waves of a work-group, one after the other in time, exchange their spans in LDS: a chunk.
+// Where chunks depend on each other, a first launch leaves each chunk's (A, H), a second composes them into the state that enters each chunk, and the third computes the
+// results.  The first and the third run over the same rows soon after one another, a part of the line at a time, so that the second read comes from the last-level cache.
+#include <hip/hip_runtime.h>
+
+#include <initializer_list>
+
+#include "dense.hpp"
+#include "graph.hpp"
+#include "kernels.hpp"
+
+namespace lms {
+
+namespace {
+
+constexpr int V = 4;                   // channels of a thread
+constexpr int BLOCK = 64 * V;          // of a wave and of a work-group
+constexpr int CHUNK = 64;              // rows of a work-group
+constexpr long long PART_BYTES = 96LL << 20;                      // inputs of a part of the line
+
+struct RecurP {
+  const void *x, *g, *o, *dy;
+  const int32_t* offsets;
+  const float *h0, *dlast;
+  void *y, *dx, *dg, *dout;
+  float *last, *dh0;
+  float* sums;                 // [chunk of the part][2][channels]: A and H, or null
+  float* in;                   // [chunk][channels]: state that enters a chunk (backward: r from the chunk behind), or null: none does
+  const float* kept;           // backward: what the forward pass had in `in`
+  long long rows, ldx, ldy, each;      // each: rows of a sequence where there are no offsets
+  int seqs, channels, act;
+  int chunk0, chunks, all_chunks;      // chunks of this launch
+};
+
+// Rows of a wave: which begin a sequence, which end one, which belong to one; lane r holds the sequence of row r.
+struct Marks {
+  unsigned first, last, live;
+  int seq;
+};
+template <int ROWS>
+__device__ __forceinline__ Marks marks(const RecurP& p, long long r0) {
+  const int lane = threadIdx.x & 63;
+  const long long row = r0 + lane;
+  bool first = false, last = false, live = lane < ROWS && row < p.rows;
+  int s = 0;
+  if (live) {
+    if (p.offsets) {                                              // the last sequence that begins at or before the row; of several at the same place all but the last are empty
+      int lo = -1, hi = p.seqs + 1;                               // offsets[lo] <= row < offsets[hi]
+      while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (p.offsets[mid] <= row) lo = mid;
+        else hi = mid;
+      }
+      s = lo;
+      live = s >= 0 && s < p.seqs;
+      if (live) {
+        first = p.offsets[s] == row;
+        last = p.offsets[s + 1] == row + 1;
+      }
+    } else {
+      s = (int)(row / p.each);
+      const long long at = row - s * p.each;
+      first = at == 0;
+      last = at == p.each - 1;
+    }
+  }
+  return Marks{(unsigned)__ballot(first), (unsigned)__ballot(last), (unsigned)__ballot(live), s};
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int cnt, const float (&v)[V]) {
+  if constexpr (sizeof(T) == 2) {
+    const v2u q = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    if (cnt >= V) { __builtin_memcpy(p, &q, 8); return; }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < cnt) p[e] = (T)(q[e >> 1] >> ((e & 1) * 16));
+  } else {
+    if (cnt >= V) { __builtin_memcpy(p, v, 16); return; }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e < cnt) p[e] = v[e];
+  }
+}
+__device__ __forceinline__ void load4(const float* p, int cnt, float (&v)[V]) {
+  if (cnt >= V) { __builtin_memcpy(v, p, 16); return; }
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = e < cnt ? p[e] : 0.f;
+}
+
+// a = sigmoid(g); rest = 1 - a without its cancellation.  Beyond 2^100 the exponential is cut: a is then nothing against any state, and rest 1.
+__device__ __forceinline__ void gate(float g, float& a, float& rest) {
+  const float e = __builtin_fminf(__builtin_amdgcn_exp2f(g * -1.44269504f), 0x1p100f);
+  a = __builtin_amdgcn_rcpf(1.f + e);
+  rest = e * a;
+}
+
+// a h + (1 - a) x: a difference that is exact from a = 1/2 on, so that a state no gate touches stays what it is.
+__device__ __forceinline__ float mix(float a, float h, float x) { return __builtin_fmaf(a, h, (1.f - a) * x); }
+
+// What leaves a span (a, h) that v enters, and the a of two spans, the one of `second` behind.
+__device__ __forceinline__ float through(float a, float v, float h) { return __builtin_signbitf(a) ? h : __builtin_fmaf(a, v, h); }
+__device__ __forceinline__ float product(float a, float second) { return __builtin_signbitf(second) ? -0.f : a * second; }
+
+enum { SUM_FWD, APPLY_FWD, SUM_BWD, APPLY_BWD };
+
+template <int WAY>
+struct Shape {
+  static constexpr int ROWS = WAY == APPLY_BWD ? 4 : 8, WAVES = CHUNK / ROWS, NT = WAVES * 64;
+};
+
+template <typename T, int WAY>
+__global__ __launch_bounds__((Shape<WAY>::NT)) void recur_kernel(RecurP p) {
+  constexpr int ROWS = Shape<WAY>::ROWS, WAVES = Shape<WAY>::WAVES;
+  constexpr bool BWD = WAY == SUM_BWD || WAY == APPLY_BWD, STATE = WAY != SUM_BWD;       // STATE: h is computed
+  __shared__ float s_a[STATE ? WAVES : 1][BLOCK], s_h[STATE ? WAVES : 1][BLOCK], s_b[BWD ? WAVES : 1][BLOCK], s_r[BWD ? WAVES : 1][BLOCK];
+  const int blocks = (p.channels + BLOCK - 1) / BLOCK, job = blockIdx.x;
+  const int chunk = job / blocks, at = (threadIdx.x & 63) * V, c = (job - chunk * blocks) * BLOCK + at, cnt = p.channels - c;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long r0 = (long long)(p.chunk0 + chunk) * CHUNK + wave * ROWS;
+  const bool there = cnt > 0 && r0 < p.rows, gated = p.o != nullptr;
+
+  // all that is read of the rows, in flight at once; rows beyond the last: the last, for nothing
+  Raw<T, V> x[STATE ? ROWS : 1], g[ROWS], o[WAY == SUM_FWD ? 1 : ROWS], dy[BWD ? ROWS : 1];
+  if (there) {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const long long row = r0 + r < p.rows ? r0 + r : p.rows - 1;
+      g[r] = raw<V>((const T*)p.g + row * p.ldx + c, cnt);
+      if constexpr (STATE) x[r] = raw<V>((const T*)p.x + row * p.ldx + c, cnt);
+      if constexpr (BWD) dy[r] = raw<V>((const T*)p.dy + row * p.ldy + c, cnt);
+    }
+    if constexpr (WAY != SUM_FWD)
+      if (gated)
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) o[r] = raw<V>((const T*)p.o + (r0 + r < p.rows ? r0 + r : p.rows - 1) * p.ldx + c, cnt);
+  }
+  float state[V] = {}, behind[V] = {};                            // h that enters the chunk; r that enters it from behind
+  if (cnt > 0) {
+    const long long entry = (long long)(p.chunk0 + chunk) * p.channels + c;
+    if (WAY == APPLY_FWD && p.in) load4(p.in + entry, cnt, state);
+    if (WAY == APPLY_BWD && p.kept) load4(p.kept + entry, cnt, state);
+    if (WAY == APPLY_BWD && p.in) load4(p.in + entry + p.channels, cnt, behind);
+  }
+  const Marks m = marks<ROWS>(p, r0);
+  auto of_sequence = [&](const float* t, int r, float (&v)[V]) {  // the values of row r's sequence, zeros where there are none
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+    if (t && cnt > 0) load4(t + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, v);
+  };
+
+  // ---- the wave's spans ----
+  // Backwards R = sum over rows of e times the product of a up to the row, which needs no order from behind.
+  float a[ROWS][V], rest[WAY == APPLY_BWD ? ROWS : 1][V], value[WAY == SUM_FWD ? 1 : ROWS][V], slope[WAY == APPLY_BWD ? ROWS : 1][V];      // value: act(o), backwards e = dy act(o); slope: dy act'(o)
+  if constexpr (WAY != SUM_FWD) {
+    if (gated && there) with_act(p.act, [&](auto act) {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float val, sl;
+          act_one<decltype(act)::value>(o[r].get(e), val, sl);
+          value[r][e] = BWD ? val * dy[BWD ? r : 0].get(e) : val;
+          if constexpr (WAY == APPLY_BWD) slope[r][e] = sl * dy[r].get(e);
+        }
+    });
+    else
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) value[r][e] = BWD && there ? dy[BWD ? r : 0].get(e) : 1.f;
+  }
+  float A[V], H[V], B[V], R[V];                                   // B: A of the way backwards
+#pragma unroll
+  for (int e = 0; e < V; ++e) { A[e] = B[e] = 1.f; H[e] = R[e] = 0.f; }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (STATE && (m.first >> r & 1)) {
+      of_sequence(p.h0, r, H);
+#pragma unroll
+      for (int e = 0; e < V; ++e) A[e] = -0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float s, sr;
+      gate(there ? g[r].get(e) : 0.f, s, sr);
+      a[r][e] = s;
+      if constexpr (WAY == APPLY_BWD) rest[r][e] = sr;
+      if constexpr (STATE) {
+        const float xv = there ? x[r].get(e) : 0.f;
+        A[e] *= s;
+        H[e] = mix(s, H[e], xv);
+      }
+    }
+    if constexpr (BWD)
+      if (!(m.last & ((1u << r) - 1))) {                          // rows behind a sequence's end pass nothing on
+        float d[V] = {};
+        const bool end = m.last >> r & 1;
+        if (end) of_sequence(p.dlast, r, d);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          B[e] *= a[r][e];
+          R[e] = __builtin_fmaf(B[e], value[r][e] + d[e], R[e]);
+          if (end) B[e] = -0.f;
+        }
+      }
+  }
+  auto put = [&](float (&t)[BLOCK], const float (&v)[V]) { *reinterpret_cast<float4*>(&t[at]) = make_float4(v[0], v[1], v[2], v[3]); };
+  if constexpr (STATE) { put(s_a[wave], A); put(s_h[wave], H); }
+  if constexpr (BWD) { put(s_b[wave], B); put(s_r[wave], R); }
+  __syncthreads();
+  auto compose = [&](const float (&sa)[BLOCK], const float (&sh)[BLOCK], float (&v)[V]) {
+    const float4 k = *reinterpret_cast<const float4*>(&sa[at]), d = *reinterpret_cast<const float4*>(&sh[at]);
+    v[0] = through(k.x, v[0], d.x); v[1] = through(k.y, v[1], d.y); v[2] = through(k.z, v[2], d.z); v[3] = through(k.w, v[3], d.w);
+  };
+  if constexpr (WAY == SUM_FWD || WAY == SUM_BWD) {
+    if (wave != 0 || cnt <= 0) return;
+    float k[V] = {1.f, 1.f, 1.f, 1.f}, d[V] = {};
+    for (int i = 0; i < WAVES; ++i) {
+      const int w = WAY == SUM_FWD ? i : WAVES - 1 - i;
+      const float (&sa)[BLOCK] = WAY == SUM_FWD ? s_a[STATE ? w : 0] : s_b[BWD ? w : 0];
+      compose(sa, WAY == SUM_FWD ? s_h[STATE ? w : 0] : s_r[BWD ? w : 0], d);
+#pragma unroll
+      for (int e = 0; e < V; ++e) k[e] = product(k[e], sa[at + e]);
+    }
+    float* to = p.sums + (long long)chunk * 2 * p.channels + c;
+    store4(to, cnt, k);
+    store4(to + p.channels, cnt, d);
+    return;
+  }
+  if constexpr (WAY == APPLY_FWD || WAY == APPLY_BWD) {
+    // sequences without a row keep their states
+    if (p.chunk0 + chunk == 0) {                                  // all lanes: they look through the sequences
+      float* to = BWD ? p.dh0 : p.last;
+      const float* from = BWD ? p.dlast : p.h0;
+      if (to && (p.offsets || p.rows == 0))
+        for (int s0 = wave * 64; s0 < p.seqs; s0 += Shape<WAY>::NT) {
+          const int s = s0 + (threadIdx.x & 63);
+          unsigned long long empty = __ballot(s < p.seqs && (!p.offsets || p.offsets[s] == p.offsets[s + 1]));
+          for (; empty; empty &= empty - 1) {
+            const long long entry = (long long)(s0 + __builtin_ctzll(empty)) * p.channels + c;
+            float v[V] = {};
+            if (from && cnt > 0) load4(from + entry, cnt, v);
+            store4(to + entry, cnt, v);
+          }
+        }
+    }
+    if (!there) return;
+    for (int w = 0; w < wave; ++w) compose(s_a[w], s_h[w], state);
+    float h[BWD ? ROWS : 1][V], now[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) now[e] = state[e];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (m.first >> r & 1) of_sequence(p.h0, r, now);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float xv = x[r].get(e);
+        now[e] = mix(a[r][e], now[e], xv);
+        if constexpr (BWD) h[r][e] = now[e];
+      }
+      if constexpr (WAY == APPLY_FWD) {
+        if (!(m.live >> r & 1)) continue;
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = now[e] * value[r][e];
+        store4((T*)p.y + (r0 + r) * p.ldy + c, cnt, y);
+        if ((m.last >> r & 1) && p.last) store4(p.last + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, now);
+      }
+    }
+    if constexpr (WAY == APPLY_BWD) {
+      for (int w = WAVES - 1; w > wave; --w) compose(s_b[w], s_r[w], behind);
+#pragma unroll
+      for (int r = ROWS - 1; r >= 0; --r) {
+        if (!(m.live >> r & 1)) continue;
+        const bool first = m.first >> r & 1;
+        if (m.last >> r & 1) of_sequence(p.dlast, r, behind);
+        float before[V], dx[V], dg[V], dout[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) before[e] = r > 0 ? h[r > 0 ? r - 1 : 0][e] : state[e];
+        if (first) of_sequence(p.h0, r, before);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float dh = value[r][e] + behind[e];
+          dx[e] = rest[r][e] * dh;
+          behind[e] = a[r][e] * dh;
+          dg[e] = behind[e] * rest[r][e] * (before[e] - x[r].get(e));
+          dout[e] = slope[r][e] * h[r][e];
+        }
+        const long long to = (r0 + r) * p.ldx + c;
+        if (p.dx) store4((T*)p.dx + to, cnt, dx);
+        if (p.dg) store4((T*)p.dg + to, cnt, dg);
+        if (p.dout) store4((T*)p.dout + to, cnt, dout);
+        if (first && p.dh0) store4(p.dh0 + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, behind);
+      }
+    }
+  }
+}
+
+// The states that enter the chunks chunk0 .. chunk0 + chunks of the line from that which enters the first (backwards: r from behind, from that which enters the last): 64 channels, 16 spans of chunks.
+constexpr int JOIN_SPANS = 16;
+template <bool BWD>
+__global__ __launch_bounds__(64 * JOIN_SPANS) void recur_join_kernel(RecurP p) {
+  __shared__ float s_a[JOIN_SPANS][64], s_h[JOIN_SPANS][64];
+  const int lane = threadIdx.x & 63, span = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  const int per = (p.chunks + JOIN_SPANS - 1) / JOIN_SPANS, first = span * per, end = first + per < p.chunks ? first + per : p.chunks;
+  const bool there = c < p.channels;
+  auto index = [&](int i) { return BWD ? p.chunks - 1 - i : i; };   // i: in the order of composition
+  constexpr int U = 8;
+  auto walk = [&](float& a, float& h, bool write) {
+    for (int i0 = first; i0 < end; i0 += U) {
+      float ka[U], kh[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float* from = p.sums + (long long)index(i0 + u < end ? i0 + u : i0) * 2 * p.channels + c;
+        ka[u] = from[0];
+        kh[u] = from[p.channels];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i0 + u < end) {
+          a = product(a, ka[u]);
+          h = through(ka[u], h, kh[u]);
+          if (write) p.in[(long long)(p.chunk0 + (BWD ? index(i0 + u) : i0 + u + 1)) * p.channels + c] = h;
+        }
+    }
+  };
+  float a = 1.f, h = 0.f;
+  if (there) walk(a, h, false);
+  s_a[span][lane] = a;
+  s_h[span][lane] = h;
+  __syncthreads();
+  if (!there) return;
+  const bool outer = BWD ? p.chunk0 + p.chunks == p.all_chunks : p.chunk0 == 0;     // nothing enters the line
+  float* const edge = p.in + (long long)(BWD ? p.chunk0 + p.chunks : p.chunk0) * p.channels + c;
+  float in = outer ? 0.f : *edge;
+  if (outer && span == 0) *edge = 0.f;
+  for (int s = 0; s < span; ++s) in = through(s_a[s][lane], in, s_h[s][lane]);
+  walk(a, in, true);
+}
+
+// One position of each request, its state in a slot.  Rows of the same slot are consecutive positions of one request: the first of them takes them all, in order.
+template <typename T>
+__global__ __launch_bounds__(256) void recur_step_kernel(RecurP p, const int32_t* slots, const float* from, float* to, int n) {
+  const int blocks = (p.channels + 4 * BLOCK - 1) / (4 * BLOCK), lane = threadIdx.x & 63;
+  const int row = blockIdx.x / blocks, c = (blockIdx.x - row * blocks) * 4 * BLOCK + threadIdx.x * V, cnt = p.channels - c;
+  const int slot = slots[row];
+  if (slot < 0 || slot >= p.seqs) return;
+  float h[V] = {};
+  if (cnt > 0) load4(from + (long long)slot * p.channels + c, cnt, h);
+  auto position = [&](int at) {
+    if (cnt <= 0) return;
+    const long long i = at * p.ldx + c;
+    const Raw<T, V> x = raw<V>((const T*)p.x + i, cnt), g = raw<V>((const T*)p.g + i, cnt);
+    Raw<T, V> o;
+    if (p.o) o = raw<V>((const T*)p.o + i, cnt);
+    float y[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float a, rest;
+      gate(g.get(e), a, rest);
+      const float xv = x.get(e);
+      y[e] = h[e] = mix(a, h[e], xv);
+    }
+    if (p.o) with_act(p.act, [&](auto act) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float value, slope;
+        act_one<decltype(act)::value>(o.get(e), value, slope);
+        y[e] *= value;
+      }
+    });
+    store4((T*)p.y + at * p.ldy + c, cnt, y);
+  };
+  for (int i0 = 0; i0 < row; i0 += 64)                            // an earlier row of the slot takes this one
+    if (__ballot(i0 + lane < row && slots[i0 + lane < row ? i0 + lane : row] == slot)) return;
+  position(row);
+  for (int i0 = row + 1; i0 < n; i0 += 64) {
+    unsigned long long more = __ballot(i0 + lane < n && slots[i0 + lane < n ? i0 + lane : row] == slot);
+    for (; more; more &= more - 1) position(i0 + __builtin_ctzll(more));
+  }
+  if (cnt > 0) store4(to + (long long)slot * p.channels + c, cnt, h);
+}
+
+#define NEED(cond, ...)        \
+  do {                         \
+    if (!(cond)) {             \
+      set_error(__VA_ARGS__);  \
+      return LMS_EINVAL;       \
+    }                          \
+  } while (0)
+
+long long chunks_of(long long rows) { return rows <= CHUNK ? 1 : (rows + CHUNK - 1) / CHUNK; }
+uint64_t up(uint64_t b) { return (b + 255) / 256 * 256; }
+// Chunks of a part of the line: the rows of its inputs take PART_BYTES at most.
+long long part_chunks(const lms_recur_desc* d) {
+  const long long bytes = (long long)CHUNK * d->channels * (d->dtype == LMS_F32 ? 4 : 2) * 3, fit = PART_BYTES / bytes, blocks = (d->channels + BLOCK - 1) / BLOCK;
+  const long long most = (1LL << 21) / blocks;                    // 2^21 work-groups of up to 1024 threads are a grid
+  return fit < 1 ? 1 : fit < most ? fit : most;
+}
+uint64_t sums_bytes(const lms_recur_desc* d) {
+  const long long part = part_chunks(d), all = chunks_of(d->rows);
+  return up((uint64_t)(part < all ? part : all) * 2 * d->channels * 4);
+}
+uint64_t in_bytes(const lms_recur_desc* d) { return up((uint64_t)(chunks_of(d->rows) + 1) * d->channels * 4); }
+
+lms_status check(const char* what, const lms_recur_desc* d, bool step) {
+  NEED(d->rows >= 0 && d->channels >= 1 && d->seqs >= 1, "%s: rows must be >= 0, channels and sequences >= 1", what);
+  NEED(d->rows <= 0x7fffffffLL - CHUNK, "%s: more than 2^31 - 65 rows", what);
+  NEED(d->channels <= 1 << 26 && d->seqs <= 1 << 30, "%s: more than 2^26 channels, or 2^30 sequences", what);
+  NEED(d->act >= LMS_ACT_NONE && d->act <= LMS_ACT_GELU_TANH, "%s: unknown activation %d", what, d->act);
+  NEED(d->dtype == LMS_BF16 || d->dtype == LMS_F32, "%s: dtype must be LMS_BF16 or LMS_F32", what);
+  const long long most = 1LL << 40;
+  NEED((d->ldx == 0 || (d->ldx >= d->channels && d->ldx <= most)) && (d->ldy == 0 || (d->ldy >= d->channels && d->ldy <= most)),
+       "%s: a row pitch is shorter than the row, or above 2^40", what);
+  NEED(!step || d->rows <= 65536, "%s: more than 65536 rows of a step", what);
+  return LMS_OK;
+}
+lms_status lined(const char* what, const lms_recur_desc* d, const int32_t* offsets) {
+  NEED(offsets || d->rows % d->seqs == 0, "%s: without offsets the rows must be a multiple of the sequences", what);
+  return LMS_OK;
+}
+// Elements of the storage type, then of 32 bits.
+lms_status aligned(const char* what, const lms_recur_desc* d, std::initializer_list<const void*> rows, std::initializer_list<const void*> words) {
+  uintptr_t a = 0, b = 0;
+  for (const void* q : rows) a |= (uintptr_t)q;
+  for (const void* q : words) b |= (uintptr_t)q;
+  NEED((a & (d->dtype == LMS_F32 ? 3 : 1)) == 0 && (b & 3) == 0, "%s: a pointer is not aligned to its elements", what);
+  return LMS_OK;
+}
+bool overlap(const lms_recur_desc* d, const float* a, const float* b) {
+  const uintptr_t n = (uintptr_t)d->seqs * d->channels * 4, x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && x < y + n && y < x + n;
+}
+RecurP params(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0) {
+  RecurP p{};
+  p.x = x; p.g = g; p.o = o; p.offsets = offsets; p.h0 = h0;
+  p.rows = d->rows; p.ldx = d->ldx ? d->ldx : d->channels; p.ldy = d->ldy ? d->ldy : d->channels;
+  p.each = d->rows / d->seqs > 0 ? d->rows / d->seqs : 1;
+  p.seqs = d->seqs; p.channels = d->channels; p.act = d->act;
+  p.all_chunks = (int)chunks_of(d->rows);
+  return p;
+}
+// No chunk needs what another leaves: one chunk, or whole sequences in each.
+bool alone(const lms_recur_desc* d, const int32_t* offsets) { return d->rows <= CHUNK || (!offsets && CHUNK % (d->rows / d->seqs) == 0); }
+
+template <typename T, int WAY>
+hipError_t launch(const RecurP& p, hipStream_t s) {
+  const int blocks = (p.channels + BLOCK - 1) / BLOCK;
+  hipLaunchKernelGGL((recur_kernel<T, WAY>), dim3((unsigned)(blocks * p.chunks)), dim3(Shape<WAY>::NT), 0, s, p);
+  return hipGetLastError();
+}
+
+// in: entries of the states between chunks, sums: of a part.
+template <typename T, bool BWD>
+hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
+  const int parts = (int)((p.all_chunks + part - 1) / part);
+  float* const in = p.in;
+  if (alone) p.in = nullptr;
+  for (int i = 0; i < parts; ++i) {
+    p.chunk0 = (int)((BWD ? parts - 1 - i : i) * part);
+    p.chunks = (int)(p.all_chunks - p.chunk0 < part ? p.all_chunks - p.chunk0 : part);
+    hipError_t e = hipSuccess;
+    if (!alone) {
+      e = launch<T, BWD ? SUM_BWD : SUM_FWD>(p, s);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(recur_join_kernel<BWD>, dim3((unsigned)((p.channels + 63) / 64)), dim3(64 * JOIN_SPANS), 0, s, p);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    e = launch<T, BWD ? APPLY_BWD : APPLY_FWD>(p, s);
+    if (e != hipSuccess) return e;
+  }
+  p.in = in;
+  return hipSuccess;
+}
+
+lms_status done(const char* what, hipError_t e) {
+  if (e == hipSuccess) return LMS_OK;
+  set_error("%s: %s", what, hipGetErrorString(e));
+  return LMS_EHIP;
+}
+
+}  // namespace
+
+lms_status recur_kept(const lms_recur_desc* d, uint64_t* bytes) {
+  if (const lms_status st = check("lms_recur_kept_bytes", d, false)) return st;
+  *bytes = d->rows <= CHUNK ? 0 : in_bytes(d);
+  return LMS_OK;
+}
+
+lms_status recur_workspace(const lms_recur_desc* d, int which, uint64_t* bytes) {
+  if (const lms_status st = check("lms_recur_workspace_bytes", d, false)) return st;
+  NEED(which == LMS_RECUR_FWD || which == LMS_RECUR_BWD, "lms_recur_workspace_bytes: unknown call %d", which);
+  *bytes = d->rows <= CHUNK ? 0 : sums_bytes(d) + in_bytes(d);
+  return LMS_OK;
+}
+
+lms_status recur_fwd(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, void* y, float* last, void* kept, void* ws,
+                     void* stream) {
+  const char* what = "lms_recur_fwd";
+  if (const lms_status st = check(what, d, false)) return st;
+  if (const lms_status st = lined(what, d, offsets)) return st;
+  if (const lms_status st = aligned(what, d, {x, g, o, y}, {offsets, h0, last})) return st;
+  NEED(!overlap(d, h0, last), "%s: the last states must not overlap the initial ones", what);
+  uint64_t need = 0;
+  recur_workspace(d, LMS_RECUR_FWD, &need);
+  NEED(!need || ws, "%s: workspace of %llu bytes required", what, (unsigned long long)need);
+  NEED((((uintptr_t)ws | (uintptr_t)kept) & 15) == 0, "%s: the workspace is not aligned", what);
+  RecurP p = params(d, x, g, o, offsets, h0);
+  p.y = y; p.last = last;
+  p.sums = (float*)ws;
+  p.in = kept ? (float*)kept : (float*)((char*)ws + sums_bytes(d));
+  const bool whole = alone(d, offsets);
+  hipStream_t s = (hipStream_t)stream;
+  return done(what, d->dtype == LMS_F32 ? line<float, false>(p, whole, part_chunks(d), s) : line<uint16_t, false>(p, whole, part_chunks(d), s));
+}
+
+lms_status recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, const void* kept, const float* dlast,
+                     void* dx, void* dg, void* dout, float* dh0, void* ws, void* stream) {
+  const char* what = "lms_recur_bwd";
+  if (const lms_status st = check(what, d, false)) return st;
+  if (const lms_status st = lined(what, d, offsets)) return st;
+  if (const lms_status st = aligned(what, d, {dy, x, g, o, dx, dg, dout}, {offsets, h0, dlast, dh0})) return st;
+  NEED(o || !dout, "%s: the gradient of o needs o", what);
+  NEED(!overlap(d, dlast, dh0) && !overlap(d, h0, dh0), "%s: the gradient of the initial states must not overlap the states or the gradient of the last ones", what);
+  const bool whole = alone(d, offsets);
+  NEED(whole || kept, "%s: what the forward pass kept is needed", what);
+  uint64_t need = 0;
+  recur_workspace(d, LMS_RECUR_BWD, &need);
+  NEED(!need || ws, "%s: workspace of %llu bytes required", what, (unsigned long long)need);
+  NEED((((uintptr_t)ws | (uintptr_t)kept) & 15) == 0, "%s: the workspace is not aligned", what);
+  RecurP p = params(d, x, g, o, offsets, h0);
+  p.dy = dy; p.dlast = dlast;
+  p.dx = dx; p.dg = dg; p.dout = dout; p.dh0 = dh0;
+  p.kept = whole ? nullptr : (const float*)kept;
+  p.sums = (float*)ws;
+  p.in = (float*)((char*)ws + sums_bytes(d));
+  hipStream_t s = (hipStream_t)stream;
+  return done(what, d->dtype == LMS_F32 ? line<float, true>(p, whole, part_chunks(d), s) : line<uint16_t, true>(p, whole, part_chunks(d), s));
+}
+
+lms_status recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream) {
+  const char* what = "lms_recur_step";
+  if (const lms_status st = check(what, d, true)) return st;
+  if (const lms_status st = aligned(what, d, {x, g, o, y}, {slots, state, next})) return st;
+  NEED(state == next || !overlap(d, state, next), "%s: the new states are the old ones or apart from them", what);
+  if (d->rows == 0) return LMS_OK;
+  RecurP p = params(d, x, g, o, nullptr, nullptr);
+  p.y = y;
+  const long long groups = d->rows * ((d->channels + 4 * BLOCK - 1) / (4 * BLOCK));
+  NEED(groups < 1 << 24, "%s: rows times channels above 2^34", what);
+  const dim3 grid((unsigned)groups);
+  if (d->dtype == LMS_F32) hipLaunchKernelGGL(recur_step_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, p, slots, state, next, (int)d->rows);
+  else hipLaunchKernelGGL(recur_step_kernel<uint16_t>, grid, dim3(256), 0, (hipStream_t)stream, p, slots, state, next, (int)d->rows);
+  return done(what, hipGetLastError());
+}
+
+}  // namespace lms

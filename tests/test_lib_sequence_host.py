@@ -1,0 +1,66 @@
+"""Refusals, workspace sizes and calls without rows of the sequence operators (no GPU: every refusal comes before anything is launched)."""
+import pytest
+
+import paper_1807_02037_amd as L
+from paper_1807_02037_amd import abi as A
+
+PTR = 1 << 20        # never dereferenced
+
+
+def refused(call, *args, match):
+    with pytest.raises(L.LmsError, match=match) as e:
+        call(*args)
+    assert e.value.status == A.EINVAL
+
+
+def recur(**kw):
+    return L.recur_desc(**{**dict(rows=200, channels=12, seqs=4), **kw})
+
+
+BAD_RECUR = [(dict(rows=-1), "rows must be"), (dict(channels=0), "channels"), (dict(seqs=0), "sequences"), (dict(rows=(1 << 31) - 1), "rows"), (dict(channels=(1 << 26) + 1), "channels"),
+             (dict(seqs=(1 << 30) + 1), "sequences"), (dict(act=5), "activation"), (dict(dtype=A.I32), "dtype"), (dict(ldx=11), "pitch"), (dict(ldy=11), "pitch"),
+             (dict(ldy=(1 << 40) + 1), "pitch")]
+
+
+@pytest.mark.parametrize("kw,match", BAD_RECUR)
+def test_recur_descriptors(kw, match):
+    d = recur(**kw)
+    refused(L.recur_workspace_bytes, d, A.RECUR_FWD, match=match)
+    refused(L.recur_kept_bytes, d, match=match)
+    refused(L.recur_fwd, d, PTR, PTR, None, PTR, None, PTR, None, PTR, PTR, None, match=match)
+    refused(L.recur_bwd, d, PTR, PTR, PTR, PTR, PTR, None, PTR, None, PTR, PTR, PTR, None, PTR, None, match=match)
+    refused(L.recur_step, d, PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, match=match)
+
+
+def test_recur_calls():
+    d = recur()
+    n = 4 * 12 * 4
+    refused(L.recur_workspace_bytes, d, 2, match="unknown call")
+    refused(L.recur_fwd, d, None, PTR, None, PTR, None, PTR, None, PTR, PTR, None, match="null argument")
+    refused(L.recur_fwd, d, PTR, PTR, None, PTR, None, PTR, None, PTR, None, None, match="workspace of")
+    refused(L.recur_fwd, d, PTR, PTR, None, PTR, None, PTR, None, PTR, PTR + 8, None, match="workspace is not aligned")
+    refused(L.recur_fwd, d, PTR, PTR, None, PTR, None, PTR, None, PTR + 8, PTR, None, match="workspace is not aligned")
+    refused(L.recur_fwd, recur(seqs=3), PTR, PTR, None, None, None, PTR, None, PTR, PTR, None, match="multiple of the sequences")
+    refused(L.recur_fwd, d, PTR, PTR, None, PTR, PTR, PTR, PTR, PTR, PTR, None, match="overlap")
+    refused(L.recur_fwd, d, PTR, PTR, None, PTR, PTR + n - 4, PTR, PTR, PTR, PTR, None, match="overlap")
+    refused(L.recur_fwd, d, PTR + 1, PTR, None, PTR, None, PTR, None, PTR, PTR, None, match="aligned")
+    refused(L.recur_fwd, d, PTR, PTR, None, PTR + 2, None, PTR, None, PTR, PTR, None, match="aligned")
+    refused(L.recur_fwd, recur(dtype=A.F32), PTR, PTR, PTR + 2, PTR, None, PTR, None, PTR, PTR, None, match="aligned")
+    refused(L.recur_bwd, d, PTR, PTR, PTR, PTR, PTR, None, None, None, PTR, PTR, PTR, None, PTR, None, match="kept is needed")
+    refused(L.recur_bwd, d, PTR, PTR, PTR, None, PTR, None, PTR, None, PTR, PTR, PTR, None, PTR, None, match="needs o")
+    refused(L.recur_bwd, d, PTR, PTR, PTR, PTR, PTR, None, PTR, PTR, PTR, PTR, PTR, PTR + n - 4, PTR, None, match="overlap")
+    refused(L.recur_bwd, d, PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, PTR, PTR, PTR, PTR, PTR, None, match="overlap")
+    refused(L.recur_bwd, d, PTR, PTR, PTR, PTR, PTR, None, PTR, None, PTR, PTR, PTR, None, None, None, match="workspace of")
+    refused(L.recur_step, d, PTR, PTR, PTR, None, PTR, PTR, PTR, None, match="null argument")
+    refused(L.recur_step, d, PTR, PTR, PTR, PTR, PTR, PTR + 4, PTR, None, match="apart")
+    refused(L.recur_step, recur(rows=65537), PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, match="65536 rows")
+    L.recur_step(recur(rows=0), None, None, None, None, None, None, None, None)
+
+
+def test_recur_sizes():
+    assert L.recur_kept_bytes(recur(rows=64)) == 0 and L.recur_workspace_bytes(recur(rows=64), A.RECUR_FWD) == 0
+    assert L.recur_kept_bytes(recur(rows=65)) >= 3 * 12 * 4
+    small, large = (L.recur_workspace_bytes(recur(rows=r, channels=1000), A.RECUR_BWD) for r in (1000, 1000000))
+    assert small < large < 1000000 * 1000 * 2 // 8
+    # sizes of 64 bits
+    assert L.recur_kept_bytes(recur(rows=1 << 30, channels=1 << 20)) > 1 << 45
