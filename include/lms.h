@@ -541,6 +541,24 @@ lms_status lms_recur_bwd(const lms_recur_desc* d, const void* dy, const void* x,
  * Slots that no row has stay as they are, in next too.  Rows whose slot is outside 0 .. seqs-1, as -1, are left alone.  Rows of the same slot are consecutive positions of one request. */
 lms_status lms_recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream);
 
+/* Group normalisation with an activation, channels last: n samples of s positions (n * s rows of c channels), `groups` groups of c / groups neighbouring channels.  Over a sample's positions and
+ * a group's channels xhat = (x - mean) / sqrt(variance + eps), variance = mean of the squared deviations; y = act(gamma xhat + beta).  s = 1: each token by itself; groups = 1: all its channels. */
+typedef struct {
+  int64_t n, s;             /* samples, >= 0; positions of a sample, >= 1 */
+  int32_t c, groups;        /* channels, a multiple of the groups, at most 2^20 */
+  int32_t act, dtype;       /* as in lms_linear_desc */
+  float eps;                /* > 0 */
+  int64_t ldx, ldy;         /* row pitches of x and dx; y and dy */
+} lms_group_norm_desc;
+typedef enum { LMS_GROUP_NORM_FWD = 0, LMS_GROUP_NORM_BWD = 1 } lms_group_norm_which;
+lms_status lms_group_norm_workspace_bytes(const lms_group_norm_desc* d, int32_t which, uint64_t* bytes);
+/* gamma, beta: c fp32 values each, or NULL for ones and zeros.  mean, rstd = 1 / sqrt(variance + eps): n x groups fp32, for the backward pass; may be NULL. */
+lms_status lms_group_norm_fwd(const lms_group_norm_desc* d, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, void* workspace, void* stream);
+/* With dv = dy act'(gamma xhat + beta): dgamma = sum over rows of dv xhat, dbeta = sum of dv, dx = rstd (gamma dv - mean of gamma dv - xhat * mean of gamma dv xhat), the means over the group.
+ * mean, rstd: what the forward pass wrote.  dx, dgamma and dbeta may each be NULL.  Deterministic. */
+lms_status lms_group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, void* dx,
+                              float* dgamma, float* dbeta, void* workspace, void* stream);
+
 
 
 #ifdef __cplusplus

@@ -12,5 +12,6 @@ from .api import (  # noqa: F401
     linear_desc, linear_workspace_bytes, linear_fwd, linear_bwd, gated_desc, gated_workspace_bytes, gated_fwd, gated_bwd,
     distill_desc, distill_workspace_bytes, distill_fwd, distill_bwd, distill_loss_grad,
     recur_desc, recur_workspace_bytes, recur_kept_bytes, recur_fwd, recur_bwd, recur_step,
+    group_norm_desc, group_norm_workspace_bytes, group_norm_fwd, group_norm_bwd,
 )
 from .models import build_graph  # noqa: F401

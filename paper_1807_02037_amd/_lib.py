@@ -22,6 +22,7 @@ LINEAR_FWD, LINEAR_BWD = 0, 1
 GATED_FWD, GATED_BWD, GATED_BWD_RECOMPUTE = 0, 1, 2
 DISTILL_FWD, DISTILL_BWD, DISTILL_LOSS_GRAD = 0, 1, 2
 RECUR_FWD, RECUR_BWD = 0, 1
+GROUP_NORM_FWD, GROUP_NORM_BWD = 0, 1
 CONV_FWD, CONV_DGRAD, CONV_WGRAD, CONV_WGRAD_BIAS = 0, 1, 2, 3
 
 
@@ -86,6 +87,11 @@ class DistillDesc(C.Structure):
 
 class RecurDesc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("seqs", C.c_int32), ("channels", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32),
+                ("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
+class GroupNormDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("s", C.c_int64), ("c", C.c_int32), ("groups", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float),
                 ("ldx", C.c_int64), ("ldy", C.c_int64)]
 
 
@@ -154,6 +160,9 @@ _SIGS = {
     "lms_recur_fwd": (C.c_int, [P(RecurDesc)] + [VP] * 10),
     "lms_recur_bwd": (C.c_int, [P(RecurDesc)] + [VP] * 14),
     "lms_recur_step": (C.c_int, [P(RecurDesc)] + [VP] * 8),
+    "lms_group_norm_workspace_bytes": (C.c_int, [P(GroupNormDesc), C.c_int32, P(C.c_uint64)]),
+    "lms_group_norm_fwd": (C.c_int, [P(GroupNormDesc)] + [VP] * 8),
+    "lms_group_norm_bwd": (C.c_int, [P(GroupNormDesc)] + [VP] * 11),
 }
 EXPORTS = sorted(_SIGS)
 

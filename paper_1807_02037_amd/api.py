@@ -383,3 +383,22 @@ def recur_bwd(desc, dy, x, g, o, offsets, h0, kept, dlast, dx, dg, dout, dh0, wo
 
 def recur_step(desc, x, g, o, slots, state, next_state, y, stream):
     _ck(A.lib().lms_recur_step(C.byref(desc), x, g, o, slots, state, next_state, y, stream))
+
+
+def group_norm_desc(n, s, c, groups, act=A.ACT_NONE, dtype=A.BF16, eps=1e-5, ldx=0, ldy=0):
+    """n samples of s positions of c channels."""
+    return _fill(A.GroupNormDesc(), n=n, s=s, c=c, groups=groups, act=act, dtype=dtype, eps=eps, ldx=ldx, ldy=ldy)
+
+
+def group_norm_workspace_bytes(desc, which):
+    b = C.c_uint64()
+    _ck(A.lib().lms_group_norm_workspace_bytes(C.byref(desc), which, C.byref(b)))
+    return b.value
+
+
+def group_norm_fwd(desc, x, gamma, beta, y, mean, rstd, workspace, stream):
+    _ck(A.lib().lms_group_norm_fwd(C.byref(desc), x, gamma, beta, y, mean, rstd, workspace, stream))
+
+
+def group_norm_bwd(desc, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, stream):
+    _ck(A.lib().lms_group_norm_bwd(C.byref(desc), dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, stream))

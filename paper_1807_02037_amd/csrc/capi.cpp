@@ -47,6 +47,10 @@ lms_status recur_fwd(const lms_recur_desc* d, const void* x, const void* g, cons
 lms_status recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, const void* kept, const float* dlast,
                      void* dx, void* dg, void* dout, float* dh0, void* ws, void* stream);
 lms_status recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream);
+lms_status group_norm_workspace(const lms_group_norm_desc* d, int which, uint64_t* bytes);
+lms_status group_norm_fwd(const lms_group_norm_desc* d, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, void* ws, void* stream);
+lms_status group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, void* dx,
+                          float* dgamma, float* dbeta, void* ws, void* stream);
 }  // namespace lms
 
 using lms::set_error;
@@ -407,6 +411,20 @@ lms_status lms_recur_bwd(const lms_recur_desc* d, const void* dy, const void* x,
 lms_status lms_recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream) {
   NEED(d && (d->rows == 0 || (x && g && slots && state && next && y)), "lms_recur_step: null argument");
   return lms::recur_step(d, x, g, o, slots, state, next, y, stream);
+}
+
+lms_status lms_group_norm_workspace_bytes(const lms_group_norm_desc* d, int32_t which, uint64_t* bytes) {
+  NEED(d && bytes, "lms_group_norm_workspace_bytes: null argument");
+  return lms::group_norm_workspace(d, which, bytes);
+}
+lms_status lms_group_norm_fwd(const lms_group_norm_desc* d, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, void* workspace, void* stream) {
+  NEED(d && (d->n == 0 || (x && y)), "lms_group_norm_fwd: null argument");
+  return lms::group_norm_fwd(d, x, gamma, beta, y, mean, rstd, workspace, stream);
+}
+lms_status lms_group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, void* dx,
+                              float* dgamma, float* dbeta, void* workspace, void* stream) {
+  NEED(d && (d->n == 0 || (dy && x && mean && rstd)), "lms_group_norm_bwd: null argument");
+  return lms::group_norm_bwd(d, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, stream);
 }
 
 }  // extern "C"

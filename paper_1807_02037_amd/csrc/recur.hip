@@ -13,12 +13,12 @@
 #include "dense.hpp"
 #include "graph.hpp"
 #include "kernels.hpp"
+#include "rows4.hpp"
 
 namespace lms {
 
 namespace {
 
-constexpr int V = 4;                   // channels of a thread
 constexpr int BLOCK = 64 * V;          // of a wave and of a work-group
 constexpr int CHUNK = 64;              // rows of a work-group
 constexpr long long PART_BYTES = 96LL << 20;                      // inputs of a part of the line
@@ -70,27 +70,6 @@ __device__ __forceinline__ Marks marks(const RecurP& p, long long r0) {
     }
   }
   return Marks{(unsigned)__ballot(first), (unsigned)__ballot(last), (unsigned)__ballot(live), s};
-}
-
-template <typename T>
-__device__ __forceinline__ void store4(T* p, int cnt, const float (&v)[V]) {
-  if constexpr (sizeof(T) == 2) {
-    const v2u q = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    if (cnt >= V) { __builtin_memcpy(p, &q, 8); return; }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < cnt) p[e] = (T)(q[e >> 1] >> ((e & 1) * 16));
-  } else {
-    if (cnt >= V) { __builtin_memcpy(p, v, 16); return; }
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < cnt) p[e] = v[e];
-  }
-}
-__device__ __forceinline__ void load4(const float* p, int cnt, float (&v)[V]) {
-  if (cnt >= V) { __builtin_memcpy(v, p, 16); return; }
-#pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = e < cnt ? p[e] : 0.f;
 }
 
 // a = sigmoid(g); rest = 1 - a without its cancellation.  Beyond 2^100 the exponential is cut: a is then nothing against any state, and rest 1.
@@ -387,16 +366,7 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurP p, const int32_t
   if (cnt > 0) store4(to + (long long)slot * p.channels + c, cnt, h);
 }
 
-#define NEED(cond, ...)        \
-  do {                         \
-    if (!(cond)) {             \
-      set_error(__VA_ARGS__);  \
-      return LMS_EINVAL;       \
-    }                          \
-  } while (0)
-
 long long chunks_of(long long rows) { return rows <= CHUNK ? 1 : (rows + CHUNK - 1) / CHUNK; }
-uint64_t up(uint64_t b) { return (b + 255) / 256 * 256; }
 // Chunks of a part of the line: the rows of its inputs take PART_BYTES at most.
 long long part_chunks(const lms_recur_desc* d) {
   const long long bytes = (long long)CHUNK * d->channels * (d->dtype == LMS_F32 ? 4 : 2) * 3, fit = PART_BYTES / bytes, blocks = (d->channels + BLOCK - 1) / BLOCK;
@@ -405,9 +375,9 @@ long long part_chunks(const lms_recur_desc* d) {
 }
 uint64_t sums_bytes(const lms_recur_desc* d) {
   const long long part = part_chunks(d), all = chunks_of(d->rows);
-  return up((uint64_t)(part < all ? part : all) * 2 * d->channels * 4);
+  return up256((uint64_t)(part < all ? part : all) * 2 * d->channels * 4);
 }
-uint64_t in_bytes(const lms_recur_desc* d) { return up((uint64_t)(chunks_of(d->rows) + 1) * d->channels * 4); }
+uint64_t in_bytes(const lms_recur_desc* d) { return up256((uint64_t)(chunks_of(d->rows) + 1) * d->channels * 4); }
 
 lms_status check(const char* what, const lms_recur_desc* d, bool step) {
   NEED(d->rows >= 0 && d->channels >= 1 && d->seqs >= 1, "%s: rows must be >= 0, channels and sequences >= 1", what);
@@ -478,12 +448,6 @@ hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
   }
   p.in = in;
   return hipSuccess;
-}
-
-lms_status done(const char* what, hipError_t e) {
-  if (e == hipSuccess) return LMS_OK;
-  set_error("%s: %s", what, hipGetErrorString(e));
-  return LMS_EHIP;
 }
 
 }  // namespace

@@ -68,3 +68,68 @@ def recur(x, g, o, act_name, borders, h0, dy=None, dlast=None, dtype=torch.bfloa
         out[name] = (v, U[dtype] * np.abs(v) + b)
     out["dh0"] = (dh0, e_dh0 + U32 * np.abs(dh0))
     return out
+
+
+def _grouped(t, n, s, groups):
+    return t.reshape(n, s, groups, -1)
+
+
+def norm_terms(n, s, cg):
+    """Roundings that follow one another in a sum over a group at most: rows of a thread, threads of a column, chunks and channels by 256 threads, the tree."""
+    return 24 + min(s, 560 + s / 512) + s * cg / 4096
+
+
+def group_norm_fwd(x, n, s, groups, gamma, beta, act_name, eps, dtype):
+    """y, mean, rstd and their bounds.  Means are joined from rows and channels: each join rounds values no larger than the largest |x| (with K joins, K u of it), and deviations are off by
+    as much; in the variance that error meets a deviation, or itself."""
+    v = _grouped(x, n, s, groups)
+    ax = (1, 3)
+    k = 3 * norm_terms(n, s, v.shape[3]) * U32
+    mean, var = v.mean(ax, keepdims=True), v.var(ax, keepdims=True)
+    most = np.abs(v).max(ax, keepdims=True)
+    e_mean = k * most
+    e_var = 2 * k * (var + np.sqrt(var) * most) + e_mean ** 2
+    rstd = 1 / np.sqrt(var + eps)
+    e_rstd = rstd * (np.minimum(1, 0.5 * e_var / (var + eps) * (1 + e_var / (var + eps))) + 6 * U32)
+    y, e_y = _norm_out(v, mean, rstd, e_mean, e_rstd, gamma, beta, act_name)[:2]
+    y = y.reshape(x.shape)
+    return (y, e_y.reshape(x.shape) + U[dtype] * np.abs(y)), (mean.reshape(n, groups), e_mean.reshape(n, groups)), (rstd.reshape(n, groups), e_rstd.reshape(n, groups))
+
+
+def _norm_out(v, mean, rstd, e_mean, e_rstd, gamma, beta, act_name):
+    from layer_oracle import SLOPE
+    groups = v.shape[2]
+    ga, be = gamma.reshape(groups, -1), beta.reshape(groups, -1)
+    hat = (v - mean) * rstd
+    e_hat = rstd * (e_mean + U32 * (np.abs(v) + np.abs(mean))) + np.abs(v - mean) * e_rstd + 3 * U32 * np.abs(hat)
+    pre = ga * hat + be
+    e_pre = np.abs(ga) * e_hat + 3 * U32 * (np.abs(pre) + np.abs(be))
+    y, slope = act(act_name, pre)
+    return y, SLOPE[act_name] * e_pre + (act_err(pre) if act_name not in ("none", "relu") else 0), hat, e_hat, pre, e_pre, slope
+
+
+def group_norm_bwd(dy, x, n, s, groups, gamma, beta, mean, rstd, act_name, dtype):
+    """dx, dgamma, dbeta and their bounds; mean and rstd as given."""
+    from layer_oracle import CURVE
+    v, d = _grouped(x, n, s, groups), _grouped(dy, n, s, groups)
+    mean, rstd, ga = mean.reshape(n, 1, groups, 1), rstd.reshape(n, 1, groups, 1), gamma.reshape(groups, -1)
+    _, _, hat, e_hat, pre, e_pre, slope = _norm_out(v, mean, rstd, 0, 0, gamma, beta, act_name)
+    e_slope = CURVE[act_name] * e_pre + (act_err(pre) if act_name not in ("none", "relu") else 0)
+    if act_name == "relu":
+        e_slope = (np.abs(pre) <= e_pre) * 1.0                     # either side of the border
+    dv = d * slope
+    e_dv = np.abs(d) * e_slope + U32 * np.abs(dv)
+    k = (norm_terms(n, s, v.shape[3]) + n) * U32
+    ax = (1, 3)
+    u, w = ga * dv, ga * dv * hat
+    m1, m2 = u.mean(ax, keepdims=True), w.mean(ax, keepdims=True)
+    e_w = np.abs(ga) * (e_dv * np.abs(hat) + np.abs(dv) * e_hat)
+    e_m1 = (np.abs(ga) * e_dv).mean(ax, keepdims=True) + k * np.abs(u).mean(ax, keepdims=True)
+    e_m2 = e_w.mean(ax, keepdims=True) + k * np.abs(w).mean(ax, keepdims=True)
+    dx = rstd * (u - m1 - hat * m2)
+    e_dx = rstd * (np.abs(ga) * e_dv + e_m1 + np.abs(hat) * e_m2 + np.abs(m2) * e_hat + 4 * U32 * (np.abs(u) + np.abs(m1) + np.abs(hat * m2)))
+    dx, e_dx = dx.reshape(x.shape), e_dx.reshape(x.shape)
+    db, dg = dv.sum((0, 1)).ravel(), (dv * hat).sum((0, 1)).ravel()
+    e_db = (e_dv + k * np.abs(dv)).sum((0, 1)).ravel()
+    e_dg = (e_dv * np.abs(hat) + np.abs(dv) * e_hat + k * np.abs(dv * hat)).sum((0, 1)).ravel()
+    return (dx, e_dx + U[dtype] * np.abs(dx)), (dg, e_dg + U32 * np.abs(dg)), (db, e_db + U32 * np.abs(db))

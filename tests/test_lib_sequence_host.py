@@ -64,3 +64,31 @@ def test_recur_sizes():
     assert small < large < 1000000 * 1000 * 2 // 8
     # sizes of 64 bits
     assert L.recur_kept_bytes(recur(rows=1 << 30, channels=1 << 20)) > 1 << 45
+
+
+def norm(**kw):
+    return L.group_norm_desc(**{**dict(n=3, s=10, c=12, groups=4), **kw})
+
+
+@pytest.mark.parametrize("kw,match", [(dict(n=-1), "samples"), (dict(s=0), "positions"), (dict(c=0), "channels"), (dict(groups=5), "multiple of the groups"), (dict(groups=0), "multiple"),
+                                      (dict(n=1 << 20, s=1 << 12), "rows"), (dict(n=1 << 62, s=4), "rows"), (dict(c=(1 << 20) + 4), "channels"), (dict(act=-1), "activation"),
+                                      (dict(dtype=A.I32), "dtype"), (dict(eps=0.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"), (dict(ldx=11), "pitch"),
+                                      (dict(ldy=-12), "pitch")])
+def test_norm_descriptors(kw, match):
+    d = norm(**kw)
+    refused(L.group_norm_workspace_bytes, d, A.GROUP_NORM_FWD, match=match)
+    refused(L.group_norm_fwd, d, PTR, None, None, PTR, PTR, PTR, PTR, None, match=match)
+    refused(L.group_norm_bwd, d, PTR, PTR, None, None, PTR, PTR, PTR, None, None, PTR, None, match=match)
+
+
+def test_norm_calls():
+    d = norm()
+    refused(L.group_norm_workspace_bytes, d, 2, match="unknown call")
+    refused(L.group_norm_fwd, d, None, None, None, PTR, PTR, PTR, PTR, None, match="null argument")
+    refused(L.group_norm_bwd, d, PTR, PTR, None, None, None, PTR, PTR, None, None, PTR, None, match="null argument")
+    refused(L.group_norm_fwd, d, PTR, None, None, PTR, PTR, PTR, None, None, match="workspace")
+    refused(L.group_norm_fwd, d, PTR, None, None, PTR, PTR, PTR, PTR + 8, None, match="workspace is not aligned")
+    refused(L.group_norm_fwd, d, PTR + 1, None, None, PTR, PTR, PTR, PTR, None, match="aligned")
+    refused(L.group_norm_fwd, d, PTR, PTR + 2, None, PTR, PTR, PTR, PTR, None, match="aligned")
+    refused(L.group_norm_bwd, d, PTR, PTR, None, None, PTR, PTR, PTR, PTR + 1, None, PTR, None, match="aligned")
+    assert L.group_norm_workspace_bytes(norm(n=0), A.GROUP_NORM_BWD) == 0
