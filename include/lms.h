@@ -559,6 +559,41 @@ lms_status lms_group_norm_fwd(const lms_group_norm_desc* d, const void* x, const
 lms_status lms_group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, void* dx,
                               float* dgamma, float* dbeta, void* workspace, void* stream);
 
+/* Linear layer in 8-bit integers, for serving: y = act((xq wq) sx sw + bias) + res, where a row of x stands as xq = 127 x / max |x| rounded to the nearest whole number, ties to even, times
+ * sx = max |x| / 127, and each column of w alike with sw; sums are exact.  A row or column of zeros has the scale 0; one that is not finite everywhere has the scale NaN, and so have the results. */
+typedef struct {
+  int64_t m;                /* rows (tokens), >= 0 */
+  int32_t n, k;             /* outputs; inputs, at most 2^17 */
+  int32_t act, dtype;       /* dtype of x, w, res and y */
+  int64_t ldx, ldw, ldy, ldr; /* row pitches of x, w, y and res */
+} lms_linear_q8_desc;
+/* wq: the n columns of w, one after the other, each of k bytes followed by zeros up to a multiple of 16; 16-byte aligned.  sw: n fp32 values.  A program does this once (the row count does not matter). */
+lms_status lms_linear_q8_weight_bytes(const lms_linear_q8_desc* d, uint64_t* bytes);
+lms_status lms_linear_q8_weight(const lms_linear_q8_desc* d, const void* w, void* wq, float* sw, void* stream);
+lms_status lms_linear_q8_workspace_bytes(const lms_linear_q8_desc* d, uint64_t* bytes);
+/* bias: n fp32 values, or NULL; res: m x n, may be y itself if ldr = ldy, or NULL. */
+lms_status lms_linear_q8_fwd(const lms_linear_q8_desc* d, const void* x, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* workspace, void* stream);
+/* The two halves of lms_linear_q8_fwd, for several layers of one x: its rows (xq: m rows laid out as the columns in wq; sx: m fp32 values), and the product, whose results are the same. */
+lms_status lms_linear_q8_rows(const lms_linear_q8_desc* d, const void* x, void* xq, float* sx, void* stream);
+lms_status lms_linear_q8_product(const lms_linear_q8_desc* d, const void* xq, const float* sx, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* workspace,
+                                 void* stream);
+
+/* Verification of drafted tokens against the target's probabilities.  For each request: p, drafts + 1 rows of probabilities of the target, and q, drafts rows of those that the tokens
+ * were drawn from (fp32, rows of a request one after the other).  Draft i is accepted if all before it are and u[i] q_i[token] < p_i[token] (products in fp64).  The next token is drawn from max(p_i - q_i, 0) at
+ * the first draft i that is not accepted (from p_i where that is 0 everywhere), from the row of p behind the last draft where all are: the first class whose running sum is above v times the
+ * whole (the last class with a share, if rounding leaves none; -1 if no class has one).  What is NaN or below 0 has no share; drafted tokens that are no class are not accepted. */
+typedef struct {
+  int32_t requests;         /* 0 .. 2^20 */
+  int32_t drafts;           /* places for drafts of a request, 0 .. 1024 */
+  int32_t classes;          /* >= 1 */
+  int64_t ldp, ldq;         /* row pitches of p and q */
+} lms_verify_desc;
+lms_status lms_verify_workspace_bytes(const lms_verify_desc* d, uint64_t* bytes);
+/* drafted, u: requests x drafts; counts: drafts that each request has (the first ones; cut to 0 .. drafts), or NULL for all; v: requests values in 0 .. 1.  accepted: requests counts;
+ * tokens: requests x (drafts + 1): the accepted ones, the next one, then -1.  q, drafted and u may be NULL where drafts is 0. */
+lms_status lms_verify(const lms_verify_desc* d, const float* p, const float* q, const int32_t* drafted, const int32_t* counts, const float* u, const float* v, int32_t* accepted,
+                      int32_t* tokens, void* workspace, void* stream);
+
 
 
 #ifdef __cplusplus

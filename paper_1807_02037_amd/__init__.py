@@ -13,5 +13,7 @@ from .api import (  # noqa: F401
     distill_desc, distill_workspace_bytes, distill_fwd, distill_bwd, distill_loss_grad,
     recur_desc, recur_workspace_bytes, recur_kept_bytes, recur_fwd, recur_bwd, recur_step,
     group_norm_desc, group_norm_workspace_bytes, group_norm_fwd, group_norm_bwd,
+    linear_q8_desc, linear_q8_weight_bytes, linear_q8_workspace_bytes, linear_q8_weight, linear_q8_rows, linear_q8_product, linear_q8_fwd,
+    verify_desc, verify_workspace_bytes, verify,
 )
 from .models import build_graph  # noqa: F401

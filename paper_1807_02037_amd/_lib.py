@@ -95,6 +95,15 @@ class GroupNormDesc(C.Structure):
                 ("ldx", C.c_int64), ("ldy", C.c_int64)]
 
 
+class LinearQ8Desc(C.Structure):
+    _fields_ = [("m", C.c_int64), ("n", C.c_int32), ("k", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32),
+                ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldy", C.c_int64), ("ldr", C.c_int64)]
+
+
+class VerifyDesc(C.Structure):
+    _fields_ = [("requests", C.c_int32), ("drafts", C.c_int32), ("classes", C.c_int32), ("ldp", C.c_int64), ("ldq", C.c_int64)]
+
+
 P = C.POINTER
 VP = C.c_void_p
 _SIGS = {
@@ -163,6 +172,14 @@ _SIGS = {
     "lms_group_norm_workspace_bytes": (C.c_int, [P(GroupNormDesc), C.c_int32, P(C.c_uint64)]),
     "lms_group_norm_fwd": (C.c_int, [P(GroupNormDesc)] + [VP] * 8),
     "lms_group_norm_bwd": (C.c_int, [P(GroupNormDesc)] + [VP] * 11),
+    "lms_linear_q8_weight_bytes": (C.c_int, [P(LinearQ8Desc), P(C.c_uint64)]),
+    "lms_linear_q8_workspace_bytes": (C.c_int, [P(LinearQ8Desc), P(C.c_uint64)]),
+    "lms_linear_q8_weight": (C.c_int, [P(LinearQ8Desc)] + [VP] * 4),
+    "lms_linear_q8_rows": (C.c_int, [P(LinearQ8Desc)] + [VP] * 4),
+    "lms_linear_q8_product": (C.c_int, [P(LinearQ8Desc)] + [VP] * 9),
+    "lms_linear_q8_fwd": (C.c_int, [P(LinearQ8Desc)] + [VP] * 8),
+    "lms_verify_workspace_bytes": (C.c_int, [P(VerifyDesc), P(C.c_uint64)]),
+    "lms_verify": (C.c_int, [P(VerifyDesc)] + [VP] * 10),
 }
 EXPORTS = sorted(_SIGS)
 

@@ -402,3 +402,51 @@ def group_norm_fwd(desc, x, gamma, beta, y, mean, rstd, workspace, stream):
 
 def group_norm_bwd(desc, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, stream):
     _ck(A.lib().lms_group_norm_bwd(C.byref(desc), dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, stream))
+
+
+def linear_q8_desc(m, n, k, act=A.ACT_NONE, dtype=A.BF16, ldx=0, ldw=0, ldy=0, ldr=0):
+    """m rows, n outputs, k inputs."""
+    return _fill(A.LinearQ8Desc(), m=m, n=n, k=k, act=act, dtype=dtype, ldx=ldx, ldw=ldw, ldy=ldy, ldr=ldr)
+
+
+def linear_q8_weight_bytes(desc):
+    b = C.c_uint64()
+    _ck(A.lib().lms_linear_q8_weight_bytes(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def linear_q8_workspace_bytes(desc):
+    b = C.c_uint64()
+    _ck(A.lib().lms_linear_q8_workspace_bytes(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def linear_q8_weight(desc, w, wq, sw, stream):
+    _ck(A.lib().lms_linear_q8_weight(C.byref(desc), w, wq, sw, stream))
+
+
+def linear_q8_rows(desc, x, xq, sx, stream):
+    _ck(A.lib().lms_linear_q8_rows(C.byref(desc), x, xq, sx, stream))
+
+
+def linear_q8_product(desc, xq, sx, wq, sw, bias, res, y, workspace, stream):
+    _ck(A.lib().lms_linear_q8_product(C.byref(desc), xq, sx, wq, sw, bias, res, y, workspace, stream))
+
+
+def linear_q8_fwd(desc, x, wq, sw, bias, res, y, workspace, stream):
+    _ck(A.lib().lms_linear_q8_fwd(C.byref(desc), x, wq, sw, bias, res, y, workspace, stream))
+
+
+def verify_desc(requests, drafts, classes, ldp=0, ldq=0):
+    """requests with places for `drafts` drafted tokens each."""
+    return _fill(A.VerifyDesc(), requests=requests, drafts=drafts, classes=classes, ldp=ldp, ldq=ldq)
+
+
+def verify_workspace_bytes(desc):
+    b = C.c_uint64()
+    _ck(A.lib().lms_verify_workspace_bytes(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def verify(desc, p, q, drafted, counts, u, v, accepted, tokens, workspace, stream):
+    _ck(A.lib().lms_verify(C.byref(desc), p, q, drafted, counts, u, v, accepted, tokens, workspace, stream))

@@ -51,6 +51,16 @@ lms_status group_norm_workspace(const lms_group_norm_desc* d, int which, uint64_
 lms_status group_norm_fwd(const lms_group_norm_desc* d, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, void* ws, void* stream);
 lms_status group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, void* dx,
                           float* dgamma, float* dbeta, void* ws, void* stream);
+lms_status linear_q8_weight_size(const lms_linear_q8_desc* d, uint64_t* bytes);
+lms_status linear_q8_workspace(const lms_linear_q8_desc* d, uint64_t* bytes);
+lms_status linear_q8_weight(const lms_linear_q8_desc* d, const void* w, void* wq, float* sw, void* stream);
+lms_status linear_q8_rows(const lms_linear_q8_desc* d, const void* x, void* xq, float* sx, void* stream);
+lms_status linear_q8_product(const lms_linear_q8_desc* d, const void* xq, const float* sx, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* ws,
+                             void* stream);
+lms_status linear_q8_fwd(const lms_linear_q8_desc* d, const void* x, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* ws, void* stream);
+lms_status verify_workspace(const lms_verify_desc* d, uint64_t* bytes);
+lms_status verify(const lms_verify_desc* d, const float* p, const float* q, const int32_t* drafted, const int32_t* counts, const float* u, const float* v, int32_t* accepted, int32_t* tokens,
+                  void* ws, void* stream);
 }  // namespace lms
 
 using lms::set_error;
@@ -425,6 +435,42 @@ lms_status lms_group_norm_bwd(const lms_group_norm_desc* d, const void* dy, cons
                               float* dgamma, float* dbeta, void* workspace, void* stream) {
   NEED(d && (d->n == 0 || (dy && x && mean && rstd)), "lms_group_norm_bwd: null argument");
   return lms::group_norm_bwd(d, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta, workspace, stream);
+}
+
+lms_status lms_linear_q8_weight_bytes(const lms_linear_q8_desc* d, uint64_t* bytes) {
+  NEED(d && bytes, "lms_linear_q8_weight_bytes: null argument");
+  return lms::linear_q8_weight_size(d, bytes);
+}
+lms_status lms_linear_q8_workspace_bytes(const lms_linear_q8_desc* d, uint64_t* bytes) {
+  NEED(d && bytes, "lms_linear_q8_workspace_bytes: null argument");
+  return lms::linear_q8_workspace(d, bytes);
+}
+lms_status lms_linear_q8_weight(const lms_linear_q8_desc* d, const void* w, void* wq, float* sw, void* stream) {
+  NEED(d && w && wq && sw, "lms_linear_q8_weight: null argument");
+  return lms::linear_q8_weight(d, w, wq, sw, stream);
+}
+lms_status lms_linear_q8_rows(const lms_linear_q8_desc* d, const void* x, void* xq, float* sx, void* stream) {
+  NEED(d && (d->m == 0 || (x && xq && sx)), "lms_linear_q8_rows: null argument");
+  return lms::linear_q8_rows(d, x, xq, sx, stream);
+}
+lms_status lms_linear_q8_product(const lms_linear_q8_desc* d, const void* xq, const float* sx, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* workspace,
+                                 void* stream) {
+  NEED(d && wq && sw && (d->m == 0 || (xq && sx && y)), "lms_linear_q8_product: null argument");
+  return lms::linear_q8_product(d, xq, sx, wq, sw, bias, res, y, workspace, stream);
+}
+lms_status lms_linear_q8_fwd(const lms_linear_q8_desc* d, const void* x, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* workspace, void* stream) {
+  NEED(d && wq && sw && (d->m == 0 || (x && y)), "lms_linear_q8_fwd: null argument");
+  return lms::linear_q8_fwd(d, x, wq, sw, bias, res, y, workspace, stream);
+}
+
+lms_status lms_verify_workspace_bytes(const lms_verify_desc* d, uint64_t* bytes) {
+  NEED(d && bytes, "lms_verify_workspace_bytes: null argument");
+  return lms::verify_workspace(d, bytes);
+}
+lms_status lms_verify(const lms_verify_desc* d, const float* p, const float* q, const int32_t* drafted, const int32_t* counts, const float* u, const float* v, int32_t* accepted,
+                      int32_t* tokens, void* workspace, void* stream) {
+  NEED(d && (d->requests == 0 || (p && v && accepted && tokens)), "lms_verify: null argument");
+  return lms::verify(d, p, q, drafted, counts, u, v, accepted, tokens, workspace, stream);
 }
 
 }  // extern "C"

@@ -15,13 +15,17 @@ namespace lms {
 //                With dh: out, pre1 = dh u act'(g), dh act(g) instead (the gradients of g and u)
 //   DENSE_DX     out[i][j] = sum over segments and r of a_s[i][r] b_s[j][r]
 //   DENSE_DW     out_s[i][j] = sum_r a[r][i] b_s[r][j] for each source s
-enum { DENSE_FWD = 0, DENSE_GATED = 1, DENSE_DX = 2, DENSE_DW = 3 };
+//   DENSE_Q8     DENSE_FWD of 8-bit integers: the sum times sx[i] sw[j] in its place.  Both operands have the reduction in rows, two elements in each of the
+//                "elements" that lda, ldb and red count; DENSE_Q8_F32: out and res are fp32.  The sums are whole numbers of 32 bits, kept as such in part
+enum { DENSE_FWD = 0, DENSE_GATED = 1, DENSE_DX = 2, DENSE_DW = 3, DENSE_Q8 = 4, DENSE_Q8_F32 = 5 };
+constexpr bool dense_q8(int mode) { return mode == DENSE_Q8 || mode == DENSE_Q8_F32; }
 
 struct DenseP {
   const void* a[2];            // operands of the segments (DX), or a[0]
   const void* b[2];            // of the segments (DX) or the sources (GATED, DW)
   void* out[2];                // of the sources (DW), or out[0]
   const float* bias;
+  const float *sx, *sw;        // Q8: what one step of a row of a, and of a row of b, stands for
   const void* res;
   const void* dh;
   void *pre, *pre1;
@@ -207,11 +211,27 @@ __device__ __forceinline__ Raw<T, N> raw(const T* p, int cnt) {
 template <typename T, int MODE>
 __device__ __forceinline__ void dense_beside8(const DenseP& p, long long i, int n, int cnt, float (&r)[8]) {
   const T* q = (const T*)(MODE == DENSE_GATED ? p.dh : p.res);
-  if ((MODE == DENSE_FWD || MODE == DENSE_GATED) && q) load8(q + i * p.ldr + n, cnt, r);
+  if ((MODE == DENSE_FWD || MODE == DENSE_GATED || dense_q8(MODE)) && q) load8(q + i * p.ldr + n, cnt, r);
 }
 template <int MODE>
 __device__ __forceinline__ void dense_bias8(const DenseP& p, int n, int cnt, float (&b)[8]) {
-  if (MODE == DENSE_FWD && p.bias) load8(p.bias + n, cnt, b);
+  if ((MODE == DENSE_FWD || dense_q8(MODE)) && p.bias) load8(p.bias + n, cnt, b);
+}
+// Sums of 8-bit integers into what they stand for; s = sx of the row.  Rounded to 24 bits before the product, once.
+template <int MODE>
+__device__ __forceinline__ void dense_scales8(const DenseP& p, int n, int cnt, float (&w)[8]) {
+  if constexpr (dense_q8(MODE)) load8(p.sw + n, cnt, w);
+}
+template <int MODE>
+__device__ __forceinline__ float dense_scale(const DenseP& p, long long i) {
+  if constexpr (dense_q8(MODE)) return p.sx[i];
+  else return 1.f;
+}
+template <int MODE>
+__device__ __forceinline__ void dense_scaled8(float s, const float (&w)[8], float (&v)[8]) {
+  if constexpr (dense_q8(MODE))
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)__float_as_int(v[e]) * (s * w[e]);
 }
 
 // What is done with eight sums (DENSE_GATED: of g and of u) at row i, columns n .. n+7 (cnt of them exist).  T: storage type.
@@ -224,7 +244,7 @@ __device__ __forceinline__ void dense_finish8(const DenseP& p, int src, long lon
     if (p.out_f32) store8<true>((float*)p.out[src] + o, cnt, v);
     else store8<true>((T*)p.out[src] + o, cnt, v);
   }
-  if constexpr (MODE == DENSE_FWD) {
+  if constexpr (MODE == DENSE_FWD || dense_q8(MODE)) {
     if (p.bias)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += b[e];
@@ -268,7 +288,7 @@ struct EpiShape {
 // Residuals (or dh) of a wave's first PRE x 32 rows, asked for before the main loop, whose length hides them.
 template <int MODE, int WTN, int PRE>
 struct Beside {
-  static constexpr bool ON = MODE == DENSE_FWD || MODE == DENSE_GATED;
+  static constexpr bool ON = MODE == DENSE_FWD || MODE == DENSE_GATED || MODE == DENSE_Q8;
   typedef EpiShape<MODE, WTN> E;
   v4u q[ON && PRE ? PRE : 1][ON && PRE ? E::QV : 1];
   __device__ __forceinline__ void ask(const DenseP& p, long long m0, int n0, bool whole) {
@@ -290,23 +310,27 @@ __device__ __forceinline__ bool epilogue_whole(const DenseP& p, long long m0, in
   return p.splits <= 1 && m0 + TM * 32 <= p.M && n0 + EpiShape<MODE, WTN>::COLS <= p.N;
 }
 
-template <typename T, int MODE, int WTN, int PRE, int TM, int TN>
-__device__ __forceinline__ void dense_epilogue(const DenseP& p, const f32x16 (&acc)[TM][TN], unsigned char* lds, long long m0, int n0, int src, int split,
+template <typename T, int MODE, int WTN, int PRE, int TM, int TN, typename Acc>
+__device__ __forceinline__ void dense_epilogue(const DenseP& p, const Acc (&acc)[TM][TN], unsigned char* lds, long long m0, int n0, int src, int split,
                                                const Beside<MODE, WTN, PRE>& pre) {
   typedef EpiShape<MODE, WTN> E;
   constexpr int LDC = WTN + 4, COLS = E::COLS, LPR = E::LPR, RPI = E::RPI, QV = E::QV;
   const int lane = threadIdx.x & 63, half = lane >> 5, cg = (lane % LPR) * 8;
   const int n = n0 + cg, cnt = p.N - n < 8 ? p.N - n : 8;
   float* sC = reinterpret_cast<float*>(lds);
-  float b[8];
-  if (p.splits <= 1 && cnt > 0) dense_bias8<MODE>(p, n, cnt, b);
+  float b[8], w[8];
+  if (p.splits <= 1 && cnt > 0) {
+    dense_bias8<MODE>(p, n, cnt, b);
+    dense_scales8<MODE>(p, n, cnt, w);
+  }
+  auto bits = [](auto v) { return __builtin_bit_cast(float, v); };
   auto turn = [&](int i) {                                        // 32 rows into LDS
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
         *reinterpret_cast<float4*>(sC + (lane & 31) * LDC + j * 32 + 8 * v + 4 * half) =
-            make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
+            make_float4(bits(acc[i][j][4 * v]), bits(acc[i][j][4 * v + 1]), bits(acc[i][j][4 * v + 2]), bits(acc[i][j][4 * v + 3]));
   };
   auto get = [&](int lr, int at, float (&d)[8]) {
     const float* s = sC + lr * LDC + cg + at;
@@ -316,9 +340,10 @@ __device__ __forceinline__ void dense_epilogue(const DenseP& p, const f32x16 (&a
   if (epilogue_whole<MODE, WTN, TM>(p, m0, n0)) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      float r[QV][8];
+      float r[QV][8], s[QV];
 #pragma unroll
       for (int q = 0; q < QV; ++q) {
+        s[q] = dense_scale<MODE>(p, m0 + i * 32 + lane / LPR + q * RPI);
         if constexpr (Beside<MODE, WTN, PRE>::ON && PRE > 0) {
           if (i < PRE) {
 #pragma unroll
@@ -335,6 +360,7 @@ __device__ __forceinline__ void dense_epilogue(const DenseP& p, const f32x16 (&a
         float v[8], u[8];
         get(lr, 0, v);
         if constexpr (MODE == DENSE_GATED) get(lr, COLS, u);
+        dense_scaled8<MODE>(s[q], w, v);
         dense_finish8<T, MODE>(p, src, m0 + i * 32 + lr, n, 8, v, u, b, r[q]);
       }
       __builtin_amdgcn_sched_barrier(0);                          // 32 rows after the other: together they are more than the registers hold
@@ -356,6 +382,7 @@ __device__ __forceinline__ void dense_epilogue(const DenseP& p, const f32x16 (&a
         if constexpr (MODE == DENSE_GATED) dense_part8(p, split, 1, row, n, cnt, u);
       } else {
         dense_beside8<T, MODE>(p, row, n, cnt, r);
+        dense_scaled8<MODE>(dense_scale<MODE>(p, row), w, v);
         dense_finish8<T, MODE>(p, src, row, n, cnt, v, u, b, r);
       }
     }

@@ -91,8 +91,24 @@ struct Operand {
   }
 };
 
+// The reduction lies in rows of b.
+template <int MODE>
+constexpr bool dense_b_fast() { return MODE == DENSE_DX || dense_q8(MODE); }
 template <int MODE, int BN>
 constexpr int dense_sub() { return MODE == DENSE_GATED ? BN / 2 : (BN < 128 ? BN : 128); }
+
+// Accumulators, what they leave as, and one product of fragments of 16 bytes a lane: 32 x 32 x 16 in bf16, 32 x 32 x 32 in 8-bit integers, in the same time.
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+template <int MODE>
+struct DenseKind {
+  typedef std::conditional_t<dense_q8(MODE), i32x16, f32x16> Acc;
+  typedef std::conditional_t<MODE == DENSE_Q8_F32, float, uint16_t> Out;
+  __device__ static __forceinline__ Acc product(const bf16x8& b, const bf16x8& a, const Acc& c) {
+    if constexpr (dense_q8(MODE)) return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(v4i, b), __builtin_bit_cast(v4i, a), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
+  }
+};
 
 // Order of the tiles: neighbours in the grid's order share operands in the L2 of an XCD, so a run of tiles covers GROUP rows of tiles by some columns.
 constexpr int GROUP = 8;
@@ -104,7 +120,7 @@ __device__ __forceinline__ void tile_at(const DenseP& p, int tile, int& tm, int&
 
 template <typename T, int MODE, bool DMA>
 __device__ __forceinline__ void dense_tile(const DenseP& p, int job) {
-  constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = MODE == DENSE_DX;
+  constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = dense_b_fast<MODE>();
   constexpr int BM = T::BM, BN = T::BN, TM = T::TM, TN = T::TN, AV = T::AV, BV = T::BV, SUB = dense_sub<MODE, BN>();
   constexpr int OUT_N = MODE == DENSE_GATED ? BN / 2 : BN;       // output columns of a tile
   constexpr int DK = T::DK, NKS = DK / 16;
@@ -290,13 +306,13 @@ __device__ __forceinline__ void dense_tile(const DenseP& p, int job) {
   const int wn0 = n0 + wn * (MODE == DENSE_GATED ? T::WTN / 2 : T::WTN);
   constexpr int PRE = !DMA ? 0 : TM < 2 ? TM : 2;
   Beside<MODE, T::WTN, PRE> beside;
-  f32x16 acc[TM][TN];
+  typename DenseKind<MODE>::Acc acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
   bf16x8 af[2][TM], bf[2][TN];                                    // operands are read one step ahead of their products
   auto read = [&](const unsigned char* t, int ks, int f) {        // fragment f of step ks
     if (f < TN) bf[ks & 1][f] = OpB::fragment(t + T::A_BYTES + OpB::address(b_rd, f, ks));
@@ -304,7 +320,7 @@ __device__ __forceinline__ void dense_tile(const DenseP& p, int job) {
   };
   auto product = [&](int ks, int q) {
     const int i = q / TN, j = q % TN;
-    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][j], af[ks & 1][i], acc[i][j], 0, 0, 0);
+    acc[i][j] = DenseKind<MODE>::product(bf[ks & 1][j], af[ks & 1][i], acc[i][j]);
   };
   auto multiply = [&](int buf) {
     const unsigned char* t = dense_smem + buf * T::STAGE;
@@ -384,7 +400,7 @@ __device__ __forceinline__ void dense_tile(const DenseP& p, int job) {
     }
   }
   __syncthreads();                                                // the buffers are free for the epilogue
-  dense_epilogue<uint16_t, MODE, T::WTN, PRE>(p, acc, dense_smem + wave * T::EPI_WAVE, wm0, wn0, src, split, beside);
+  dense_epilogue<typename DenseKind<MODE>::Out, MODE, T::WTN, PRE>(p, acc, dense_smem + wave * T::EPI_WAVE, wm0, wn0, src, split, beside);
 }
 
 template <typename T, int MODE, bool DMA>
@@ -418,7 +434,7 @@ struct Tile256 {
 template <int MODE>
 __global__ __launch_bounds__(256, 1) void dense_large_kernel(DenseP p) {
   typedef Tile256 T;
-  constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = MODE == DENSE_DX;
+  constexpr bool A_FAST = MODE != DENSE_DW, B_FAST = dense_b_fast<MODE>();
   constexpr int DK = T::DK, BM = T::BM, BN = T::BN, TM = 4, TN = 4, NP = TM * TN, SUB = 128, OUT_N = MODE == DENSE_GATED ? 128 : 256;
   constexpr int V = T::UNIT / (16 * T::NT), B_AT = T::A_RING * T::UNIT;     // loads of a unit per thread; where B's ring begins
   typedef Operand<BM, A_FAST, SUB, DK> OpA;
@@ -506,13 +522,13 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(DenseP p) {
   const long long wm0 = m0 + wm * 128;                            // the wave's first row and column
   const int wn0 = n0 + wn * (OUT_N / 2);
   Beside<MODE, 128, 2> beside;
-  f32x16 acc[TM][TN];
+  typename DenseKind<MODE>::Acc acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
   bf16x8 af[2][TM], bf[2][TN];                                    // operands are read one step ahead of their products
   auto read = [&](unsigned a, unsigned b, int ks, int f) {        // fragment f of step ks; a, b: the units
     if (f < TN) bf[ks & 1][f] = OpB::fragment(dense_smem + B_AT + b + OpB::address(b_rd, f, ks));
@@ -523,7 +539,7 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(DenseP p) {
     constexpr int ks = decltype(ks_c)::value, l = decltype(l_c)::value;
 #pragma unroll
     for (int q = 0; q < NP; ++q) {
-      acc[q / TN][q % TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[ks & 1][q % TN], af[ks & 1][q / TN], acc[q / TN][q % TN], 0, 0, 0);
+      acc[q / TN][q % TN] = DenseKind<MODE>::product(bf[ks & 1][q % TN], af[ks & 1][q / TN], acc[q / TN][q % TN]);
       if (q < TM + TN) read(a, b, (ks + 1) % 4, q);
       if (q % 4 == 0) load(l + q / 4);
       __builtin_amdgcn_sched_barrier(0);
@@ -577,7 +593,7 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(DenseP p) {
   } while (--left > 0);
   wait_loads();
   __syncthreads();                                                // the rings are free for the epilogue
-  dense_epilogue<uint16_t, MODE, 128, 2>(p, acc, dense_smem + wave * epi_wave_bytes(128), wm0, wn0, src, split, beside);
+  dense_epilogue<typename DenseKind<MODE>::Out, MODE, 128, 2>(p, acc, dense_smem + wave * epi_wave_bytes(128), wm0, wn0, src, split, beside);
 }
 
 // Tiles and stages of a product; false: more than an int numbers.
@@ -645,7 +661,7 @@ struct TileCost { int tile, bm, bn, per_cu; double alone, full, fixed; };
 constexpr TileCost COSTS[] = {{TILE_256, 256, 256, 1, 1.62, 1.62, 0.0}, {TILE_128, 128, 128, 2, 0.86, 1.10, 2.0}, {TILE_128D, 128, 128, 1, 0.50, 0.65, 2.0},
                               {TILE_64X128, 64, 128, 2, 0.48, 0.80, 1.0}, {TILE_64, 64, 64, 2, 0.33, 0.52, 1.0}, {TILE_32, 32, 128, 2, 0.38, 0.62, 1.0}};
 
-constexpr double LARGE_FIXED[] = {20.0, 15.0, 8.0, 5.0};           // DENSE_FWD, GATED, DX, DW
+constexpr double LARGE_FIXED[] = {20.0, 15.0, 8.0, 5.0, 20.0, 20.0};     // DENSE_FWD, GATED, DX, DW, Q8, Q8_F32
 
 constexpr int MAX_SPLITS = 48;
 
@@ -675,7 +691,7 @@ bool dma_ok(int mode, const DenseP& p) {
   uintptr_t at = (uintptr_t)p.a[0] | (uintptr_t)p.b[0];
   if (p.segs == 2) at |= (uintptr_t)p.a[1];
   if (p.segs == 2 || p.srcs == 2) at |= (uintptr_t)p.b[1];
-  const long long a_len = mode == DENSE_DW ? p.M : p.red, b_len = mode == DENSE_DX ? p.red : p.N;
+  const long long a_len = mode == DENSE_DW ? p.M : p.red, b_len = mode == DENSE_DX || dense_q8(mode) ? p.red : p.N;
   return (at & 15) == 0 && ((p.lda | p.ldb | a_len | b_len) & 7) == 0 && p.lda < (1 << 21) && p.ldb < (1 << 21);
 }
 
@@ -685,7 +701,11 @@ hipError_t dense_mode(DenseP& p, hipStream_t s) {
   const DensePlan plan = dense_plan(MODE, p.M, p.N, p.red, p.segs, p.srcs);
   p.splits = plan.splits;
   hipError_t e;
-  if (!dma_ok(MODE, p)) e = plan.tile <= TILE_128D ? launch_dense<Tile128, MODE, false>(p, s) : launch_dense<Tile64x128, MODE, false>(p, s);
+  const auto at_any_address = [&]() {
+    if constexpr (dense_q8(MODE)) return hipErrorInvalidValue;    // never: the layout of its operands is the library's
+    else return plan.tile <= TILE_128D ? launch_dense<Tile128, MODE, false>(p, s) : launch_dense<Tile64x128, MODE, false>(p, s);
+  };
+  if (!dma_ok(MODE, p)) e = at_any_address();
   else if (plan.tile == TILE_256) e = launch_large<MODE>(p, s);
   else if (plan.tile == TILE_128) e = launch_dense<Tile128, MODE, true>(p, s);
   else if (plan.tile == TILE_128D) e = launch_dense<Tile128D, MODE, true>(p, s);
@@ -719,6 +739,8 @@ hipError_t dense_bf16(int mode, DenseP& p, hipStream_t s) {
     case DENSE_FWD: return dense_mode<DENSE_FWD>(p, s);
     case DENSE_GATED: return dense_mode<DENSE_GATED>(p, s);
     case DENSE_DX: return dense_mode<DENSE_DX>(p, s);
+    case DENSE_Q8: return dense_mode<DENSE_Q8>(p, s);
+    case DENSE_Q8_F32: return dense_mode<DENSE_Q8_F32>(p, s);
     default: return dense_mode<DENSE_DW>(p, s);
   }
 }

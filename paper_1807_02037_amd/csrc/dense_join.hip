@@ -19,6 +19,10 @@ __global__ __launch_bounds__(64) void dense_join_kernel(DenseP p) {
   if (src >= (MODE == DENSE_DW ? p.srcs : 1) || row >= p.M) return;
   const long long plane = p.M * p.N, split = plane * p.srcs;
   const float* at = p.part + src * plane + row * p.N + n;
+  auto plus = [](float a, float c) {                              // Q8: sums of 32 bits in the place of floats
+    if constexpr (dense_q8(MODE)) return __int_as_float(__float_as_int(a) + __float_as_int(c));
+    else return a + c;
+  };
   auto add = [&](const float* q, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.f;
@@ -30,20 +34,23 @@ __global__ __launch_bounds__(64) void dense_join_kernel(DenseP p) {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += t[u][e];
+        for (int e = 0; e < 8; ++e) v[e] = plus(v[e], t[u][e]);
     }
     for (; s < p.splits; ++s) {
       float t[8];
       load8(q + s * split, cnt, t);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += t[e];
+      for (int e = 0; e < 8; ++e) v[e] = plus(v[e], t[e]);
     }
   };
-  float v[8], u[8], b[8], r[8];
+  float v[8], u[8], b[8], r[8], w[8];
   dense_bias8<MODE>(p, n, cnt, b);
+  dense_scales8<MODE>(p, n, cnt, w);
+  const float scale = dense_scale<MODE>(p, row);
   dense_beside8<T, MODE>(p, row, n, cnt, r);
   add(at, v);
   if constexpr (MODE == DENSE_GATED) add(at + plane, u);
+  dense_scaled8<MODE>(scale, w, v);
   dense_finish8<T, MODE>(p, src, row, n, cnt, v, u, b, r);
 }
 
@@ -62,6 +69,8 @@ hipError_t dense_join(int mode, bool f32, DenseP& p, hipStream_t s) {
     case DENSE_FWD: return f32 ? launch_join<float, DENSE_FWD>(p, s) : launch_join<uint16_t, DENSE_FWD>(p, s);
     case DENSE_GATED: return f32 ? launch_join<float, DENSE_GATED>(p, s) : launch_join<uint16_t, DENSE_GATED>(p, s);
     case DENSE_DX: return f32 ? launch_join<float, DENSE_DX>(p, s) : launch_join<uint16_t, DENSE_DX>(p, s);
+    case DENSE_Q8: return launch_join<uint16_t, DENSE_Q8>(p, s);
+    case DENSE_Q8_F32: return launch_join<float, DENSE_Q8_F32>(p, s);
     default: return f32 ? launch_join<float, DENSE_DW>(p, s) : launch_join<uint16_t, DENSE_DW>(p, s);
   }
 }

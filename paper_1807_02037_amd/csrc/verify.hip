@@ -1,0 +1,213 @@
+// Verification of drafted tokens (include/lms.h has the rule).
+//
+// Two launches.  The first sums, for each request, the chunks of the one distribution that its next token comes from; every work-group finds that out by itself, from a few reads of the drafts.
+// The second picks the chunk in which the running sum passes the drawn share of the whole, and the class in it.  Differences and sums are fp64: the token is that of exact sums but
+// where the drawn number lies within some 2^-50 of a border, and whole numbers have no tolerance.
+#include <hip/hip_runtime.h>
+
+#include <initializer_list>
+
+#include "kernels.hpp"
+#include "rows4.hpp"
+
+namespace lms {
+
+namespace {
+
+constexpr int NT = 256, MAX_CHUNKS = 64, STEP = NT * 4;            // classes of a work-group at a time
+
+struct VerifyP {
+  const float *p, *q;
+  const int32_t *drafted, *counts;
+  const float *u, *v;
+  int32_t *accepted, *tokens;
+  double* sums;                // [request][chunk][2]: of max(p - q, 0) and of p
+  long long ldp, ldq;
+  int requests, drafts, classes, chunks, chunk;      // chunk: classes of one, a multiple of STEP
+};
+
+// Drafts of a request that are accepted: those before the first that is not.  The whole wave takes part.
+__device__ __forceinline__ int accepted_drafts(const VerifyP& p, int b, int& count) {
+  const int lane = threadIdx.x & 63;
+  count = p.counts ? p.counts[b] : p.drafts;
+  count = count < 0 ? 0 : count > p.drafts ? p.drafts : count;
+  for (int i0 = 0; i0 < count; i0 += 64) {
+    const int i = i0 + lane;
+    bool good = false;
+    if (i < count) {
+      const int t = p.drafted[(long long)b * p.drafts + i];
+      if (t >= 0 && t < p.classes)
+        good = (double)p.u[(long long)b * p.drafts + i] * (double)p.q[((long long)b * p.drafts + i) * p.ldq + t] < (double)p.p[((long long)b * (p.drafts + 1) + i) * p.ldp + t];
+    }
+    const unsigned long long bad = __ballot(i < count && !good);
+    if (bad) return i0 + __builtin_ctzll(bad);
+  }
+  return count;
+}
+
+// Four classes from c on: max(p - q, 0) where there is a q, and p where it is above 0; nothing beyond the last, nothing for NaN.
+__device__ __forceinline__ void masses(const VerifyP& p, const float* pr, const float* qr, int c, double (&r)[4], double (&w)[4]) {
+  float a[4], b[4] = {0.f, 0.f, 0.f, 0.f};
+  load4(pr + c, p.classes - c, a);
+  if (qr) load4(qr + c, p.classes - c, b);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const double d = (double)a[e] - (double)b[e];
+    r[e] = d > 0.0 ? d : 0.0;
+    w[e] = a[e] > 0.f ? (double)a[e] : 0.0;
+  }
+}
+
+__global__ __launch_bounds__(NT) void verify_sums_kernel(VerifyP p) {
+  __shared__ double lds[NT / 64][2];
+  const int b = blockIdx.x / p.chunks, chunk = blockIdx.x - b * p.chunks;
+  int count;
+  const int at = accepted_drafts(p, b, count);
+  const float* pr = p.p + ((long long)b * (p.drafts + 1) + at) * p.ldp;
+  const float* qr = at < count ? p.q + ((long long)b * p.drafts + at) * p.ldq : nullptr;
+  const int begin = chunk * p.chunk, end = begin + p.chunk < p.classes ? begin + p.chunk : p.classes;
+  double sr = 0.0, sp = 0.0;
+  for (int c = begin + (int)threadIdx.x * 4; c < end; c += STEP) {
+    double r[4], w[4];
+    masses(p, pr, qr, c, r, w);
+    sr += (r[0] + r[1]) + (r[2] + r[3]);
+    sp += (w[0] + w[1]) + (w[2] + w[3]);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    sr += __shfl_xor(sr, d);
+    sp += __shfl_xor(sp, d);
+  }
+  if ((threadIdx.x & 63) == 0) { lds[threadIdx.x >> 6][0] = sr; lds[threadIdx.x >> 6][1] = sp; }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    double t = lds[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) t += lds[w][threadIdx.x];
+    p.sums[(long long)blockIdx.x * 2 + threadIdx.x] = t;
+  }
+}
+
+// Sum of the lanes up to this one.
+__device__ __forceinline__ double running(double v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const double o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+__global__ __launch_bounds__(NT) void verify_pick_kernel(VerifyP p) {
+  __shared__ double lds[NT / 64];
+  __shared__ int s_first[NT / 64], s_last[NT / 64];
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int count;
+  const int at = accepted_drafts(p, b, count);
+  const float* pr = p.p + ((long long)b * (p.drafts + 1) + at) * p.ldp;
+  const float* qr = at < count ? p.q + ((long long)b * p.drafts + at) * p.ldq : nullptr;
+  // the chunk
+  const double sr = lane < p.chunks ? p.sums[((long long)b * p.chunks + lane) * 2] : 0.0, sp = lane < p.chunks ? p.sums[((long long)b * p.chunks + lane) * 2 + 1] : 0.0;
+  const bool rest = __ballot(sr > 0.0) != 0;                      // else p, which has no more than q anywhere, itself
+  const double mine = rest ? sr : sp, upto = running(mine), whole = __shfl(upto, 63), target = (double)p.v[b] * whole;
+  const unsigned long long any = __ballot(mine > 0.0), beyond = __ballot(mine > 0.0 && upto > target);
+  int token = -1;
+  if (any) {                                                      // else there is no class to take
+    const int chunk = beyond ? __builtin_ctzll(beyond) : 63 - __builtin_clzll(any);
+    double base = __shfl(upto - mine, chunk);
+    const int begin = chunk * p.chunk, end = begin + p.chunk < p.classes ? begin + p.chunk : p.classes;
+    int last = -1;                                                // the last class with a share so far
+    for (int c0 = begin; c0 < end && token < 0; c0 += STEP) {
+      const int c = c0 + (int)threadIdx.x * 4;
+      double r[4] = {0.0, 0.0, 0.0, 0.0}, w[4] = {0.0, 0.0, 0.0, 0.0};
+      if (c < end) masses(p, pr, qr, c, r, w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = rest ? r[e] : w[e];
+      const double own = (r[0] + r[1]) + (r[2] + r[3]), before = running(own);
+      __syncthreads();
+      if (lane == 63) lds[wave] = before;
+      __syncthreads();
+      double sum = base + (before - own);
+      for (int i = 0; i < wave; ++i) sum += lds[i];
+      int first = 0x7fffffff, high = -1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum += r[e];
+        if (r[e] > 0.0) {
+          high = c + e;
+          if (sum > target && first == 0x7fffffff) first = c + e;
+        }
+      }
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) {
+        const int f = __shfl_xor(first, d), h = __shfl_xor(high, d);
+        first = first < f ? first : f;
+        high = high > h ? high : h;
+      }
+      if (lane == 0) { s_first[wave] = first; s_last[wave] = high; }
+      __syncthreads();
+      for (int i = 0; i < NT / 64; ++i) {
+        first = first < s_first[i] ? first : s_first[i];
+        last = last > s_last[i] ? last : s_last[i];
+        base += lds[i];
+      }
+      if (first != 0x7fffffff) token = first;
+    }
+    if (token < 0) token = last;
+  }
+  int32_t* out = p.tokens + (long long)b * (p.drafts + 1);
+  for (int i = threadIdx.x; i <= p.drafts; i += NT) out[i] = i < at ? p.drafted[(long long)b * p.drafts + i] : i == at ? token : -1;
+  if (threadIdx.x == 0) p.accepted[b] = at;
+}
+
+void chunks_of(const lms_verify_desc* d, int& chunks, int& chunk) {
+  const int steps = (d->classes + STEP - 1) / STEP, want = d->requests >= 512 ? 1 : (512 + d->requests - 1) / (d->requests ? d->requests : 1);
+  const int most = want < MAX_CHUNKS ? want : MAX_CHUNKS, per = (steps + most - 1) / most;
+  chunk = per * STEP;
+  chunks = (steps + per - 1) / per;
+}
+
+lms_status check(const char* what, const lms_verify_desc* d) {
+  NEED(d->requests >= 0 && d->drafts >= 0 && d->classes >= 1, "%s: requests and drafts must be >= 0, classes >= 1", what);
+  NEED(d->requests <= 1 << 20 && d->drafts <= 1 << 10, "%s: more than 2^20 requests, or 2^10 drafts", what);
+  NEED(d->classes <= 1 << 30, "%s: more than 2^30 classes", what);
+  const long long most = 1LL << 40;
+  NEED((d->ldp == 0 || (d->ldp >= d->classes && d->ldp <= most)) && (d->ldq == 0 || (d->ldq >= d->classes && d->ldq <= most)),
+       "%s: a row pitch is shorter than the row, or above 2^40", what);
+  return LMS_OK;
+}
+
+}  // namespace
+
+lms_status verify_workspace(const lms_verify_desc* d, uint64_t* bytes) {
+  if (const lms_status st = check("lms_verify_workspace_bytes", d)) return st;
+  int chunks, chunk;
+  chunks_of(d, chunks, chunk);
+  *bytes = up256((uint64_t)d->requests * chunks * 16);
+  return LMS_OK;
+}
+
+lms_status verify(const lms_verify_desc* d, const float* pr, const float* q, const int32_t* drafted, const int32_t* counts, const float* u, const float* v, int32_t* accepted, int32_t* tokens,
+                  void* ws, void* stream) {
+  const char* what = "lms_verify";
+  if (const lms_status st = check(what, d)) return st;
+  if (d->requests == 0) return LMS_OK;
+  NEED(d->drafts == 0 || (q && drafted && u), "%s: drafts need q, their tokens and u", what);
+  uintptr_t low = 0;
+  for (const void* a : {(const void*)pr, (const void*)q, (const void*)drafted, (const void*)counts, (const void*)u, (const void*)v, (const void*)accepted, (const void*)tokens}) low |= (uintptr_t)a;
+  NEED((low & 3) == 0, "%s: a pointer is not aligned to its elements", what);
+  NEED(ws && ((uintptr_t)ws & 15) == 0, "%s: the workspace is missing or not aligned", what);
+  VerifyP p{};
+  p.p = pr; p.q = q; p.drafted = drafted; p.counts = counts; p.u = u; p.v = v;
+  p.accepted = accepted; p.tokens = tokens; p.sums = (double*)ws;
+  p.ldp = d->ldp ? d->ldp : d->classes; p.ldq = d->ldq ? d->ldq : d->classes;
+  p.requests = d->requests; p.drafts = d->drafts; p.classes = d->classes;
+  chunks_of(d, p.chunks, p.chunk);
+  hipStream_t s = (hipStream_t)stream;
+  hipLaunchKernelGGL(verify_sums_kernel, dim3((unsigned)(d->requests * p.chunks)), dim3(NT), 0, s, p);
+  hipLaunchKernelGGL(verify_pick_kernel, dim3((unsigned)d->requests), dim3(NT), 0, s, p);
+  return done(what, hipGetLastError());
+}
+
+}  // namespace lms

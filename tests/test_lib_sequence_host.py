@@ -92,3 +92,70 @@ def test_norm_calls():
     refused(L.group_norm_fwd, d, PTR, PTR + 2, None, PTR, PTR, PTR, PTR, None, match="aligned")
     refused(L.group_norm_bwd, d, PTR, PTR, None, None, PTR, PTR, PTR, PTR + 1, None, PTR, None, match="aligned")
     assert L.group_norm_workspace_bytes(norm(n=0), A.GROUP_NORM_BWD) == 0
+
+
+def q8(**kw):
+    return L.linear_q8_desc(**{**dict(m=4, n=8, k=20), **kw})
+
+
+@pytest.mark.parametrize("kw,match", [(dict(m=-1), "rows must be"), (dict(k=0), "widths"), (dict(n=0), "widths"), (dict(m=1 << 31), "rows"), (dict(k=(1 << 17) + 1), "inputs"),
+                                      (dict(n=(1 << 30) + 1), "widths"), (dict(act=5), "activation"), (dict(dtype=A.I32), "dtype"), (dict(ldx=19), "pitch"), (dict(ldw=7), "pitch"),
+                                      (dict(ldy=7), "pitch"), (dict(ldr=7), "pitch"), (dict(ldx=(1 << 40) + 1), "pitch")])
+def test_q8_descriptors(kw, match):
+    d = q8(**kw)
+    refused(L.linear_q8_weight_bytes, d, match=match)
+    refused(L.linear_q8_workspace_bytes, d, match=match)
+    refused(L.linear_q8_weight, d, PTR, PTR, PTR, None, match=match)
+    refused(L.linear_q8_rows, d, PTR, PTR, PTR, None, match=match)
+    refused(L.linear_q8_product, d, PTR, PTR, PTR, PTR, None, None, PTR, PTR, None, match=match)
+    refused(L.linear_q8_fwd, d, PTR, PTR, PTR, None, None, PTR, PTR, None, match=match)
+
+
+def test_q8_calls():
+    d = q8()
+    assert L.linear_q8_weight_bytes(d) == 8 * 32
+    refused(L.linear_q8_weight, d, None, PTR, PTR, None, match="null argument")
+    refused(L.linear_q8_weight, d, PTR, PTR + 8, PTR, None, match="16 bytes")
+    refused(L.linear_q8_weight, d, PTR + 1, PTR, PTR, None, match="aligned")
+    refused(L.linear_q8_rows, d, PTR, PTR + 4, PTR, None, match="16 bytes")
+    refused(L.linear_q8_fwd, d, None, PTR, PTR, None, None, PTR, PTR, None, match="null argument")
+    refused(L.linear_q8_fwd, d, PTR, PTR + 1, PTR, None, None, PTR, PTR, None, match="16 bytes")
+    refused(L.linear_q8_fwd, d, PTR, PTR, PTR, None, None, PTR, None, None, match="workspace")
+    refused(L.linear_q8_fwd, d, PTR, PTR, PTR, PTR + 2, None, PTR, PTR, None, match="aligned")
+    refused(L.linear_q8_fwd, q8(ldr=9), PTR, PTR, PTR, None, PTR, PTR, PTR, None, match="same pitch")
+    refused(L.linear_q8_product, q8(ldr=9), PTR, PTR, PTR, PTR, None, PTR, PTR, PTR, None, match="same pitch")
+    L.linear_q8_fwd(q8(m=0), None, PTR, PTR, None, None, None, None, None)
+    L.linear_q8_rows(q8(m=0), None, None, None, None)
+    L.linear_q8_product(q8(m=0), None, None, PTR, PTR, None, None, None, None, None)
+    assert L.linear_q8_workspace_bytes(q8(m=0)) == 0
+
+
+def verify(**kw):
+    return L.verify_desc(**{**dict(requests=3, drafts=2, classes=50), **kw})
+
+
+@pytest.mark.parametrize("kw,match", [(dict(requests=-1), "requests"), (dict(drafts=-1), "drafts"), (dict(classes=0), "classes"), (dict(requests=(1 << 20) + 1), "requests"),
+                                      (dict(drafts=1025), "drafts"), (dict(classes=(1 << 30) + 1), "classes"), (dict(ldp=49), "pitch"), (dict(ldq=49), "pitch"),
+                                      (dict(ldq=1 << 41), "pitch")])
+def test_verify_descriptors(kw, match):
+    d = verify(**kw)
+    refused(L.verify_workspace_bytes, d, match=match)
+    refused(L.verify, d, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, PTR, None, match=match)
+
+
+def test_verify_calls():
+    d = verify()
+    refused(L.verify, d, None, PTR, PTR, None, PTR, PTR, PTR, PTR, PTR, None, match="null argument")
+    refused(L.verify, d, PTR, None, PTR, None, PTR, PTR, PTR, PTR, PTR, None, match="drafts need")
+    refused(L.verify, d, PTR, PTR, PTR, None, PTR, PTR, PTR, PTR, None, None, match="workspace")
+    refused(L.verify, d, PTR, PTR, PTR, None, PTR, PTR, PTR, PTR, PTR + 8, None, match="workspace")
+    refused(L.verify, d, PTR + 2, PTR, PTR, None, PTR, PTR, PTR, PTR, PTR, None, match="aligned")
+    L.verify(verify(requests=0), None, None, None, None, None, None, None, None, None, None)
+
+
+@pytest.mark.parametrize("make,kw", [(recur, dict(rows=1 << 64)), (recur, dict(channels=(1 << 32) + 12)), (recur, dict(seqs=(1 << 32) + 4)), (norm, dict(c=(1 << 32) + 12)),
+                                     (norm, dict(n=(1 << 64) + 3)), (q8, dict(k=(1 << 32) + 20)), (verify, dict(requests=(1 << 32) + 3)), (verify, dict(classes=1 << 32))])
+def test_numbers_that_do_not_fit(make, kw):
+    with pytest.raises(L.LmsError, match=next(iter(kw))) as e:
+        make(**kw)
+    assert e.value.status == A.EINVAL
