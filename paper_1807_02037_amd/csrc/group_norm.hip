@@ -323,6 +323,331 @@ __global__ __launch_bounds__(NT) void norm_dx_kernel(NormP p) {
   });
 }
 
+// ---- samples that a work-group holds ----
+//
+// Groups of whole vectors of eight channels.  A work-group keeps what it has read in registers from the one read to the one write.
+
+constexpr int W = 8;                   // channels of a vector here
+
+struct ResidentP {
+  NormP n;
+  long long samples;
+  int lanes;                           // tokens: lanes of a row, a power of two
+  int block, blocks;                   // images: vectors of a work-group's channels, and how many such blocks there are
+  int gv;                              // vectors of a group
+};
+
+// eight values of a vector
+template <int ACT, typename T>
+__device__ __forceinline__ void slope8(const float (&ga)[W], const float (&be)[W], float mean, float rstd, const Raw<T, W>& x, const Raw<T, W>& dy, float (&hat)[W], float (&dv)[W]) {
+#pragma unroll
+  for (int e = 0; e < W; ++e) {
+    float value, slope;
+    hat[e] = (x.get(e) - mean) * rstd;
+    act_one<ACT>(__builtin_fmaf(ga[e], hat[e], be[e]), value, slope);
+    dv[e] = dy.get(e) * slope;
+  }
+}
+__device__ __forceinline__ void weights8(const NormP& p, int c, bool there, float (&ga)[W], float (&be)[W]) {
+#pragma unroll
+  for (int e = 0; e < W; ++e) { ga[e] = 1.f; be[e] = 0.f; }
+  if (there && p.gamma) load8(p.gamma + c, W, ga);
+  if (there && p.beta) load8(p.beta + c, W, be);
+}
+
+// Tokens (s = 1).  A row takes `lanes` lanes of K vectors each; rows of a work-group run in parallel, and it goes on to others, the next row's loads out before this one is worked on.  Groups whose
+// vectors are a power of two of lanes of one wave meet by shuffles, others in LDS.  Backwards the sums for gamma and beta stay in registers until the work-group's last row.
+template <typename T, int NT, int K, bool BWD>
+__global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
+  __shared__ float s_part[2][NT * K], s_sum[2][NT * K];
+  const NormP& p = q.n;
+  const int tid = threadIdx.x, l = tid & (q.lanes - 1), sub = tid / q.lanes, rows = NT / q.lanes, nv = p.c / W;
+  const bool by_shuffles = (q.gv & (q.gv - 1)) == 0 && q.gv <= 64 && q.gv <= q.lanes;
+  auto vec = [&](int j) { return l + j * q.lanes; };
+  float ga[K][W], be[K][W], da[BWD ? K : 1][W] = {}, db[BWD ? K : 1][W] = {};
+#pragma unroll
+  for (int j = 0; j < K; ++j) weights8(p, vec(j) * W, vec(j) < nv, ga[j], be[j]);
+  Raw<T, W> x[K], dy[BWD ? K : 1], nx[K], ndy[BWD ? K : 1];
+  float mean[BWD ? K : 1], rstd[BWD ? K : 1], nmean[BWD ? K : 1], nrstd[BWD ? K : 1];
+  auto ask = [&](long long row) {
+    const bool there = row < q.samples;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int cnt = there && vec(j) < nv ? W : 0;
+      nx[j] = raw<W>((const T*)p.x + row * p.ldx + vec(j) * W, cnt);
+      if constexpr (BWD) {
+        ndy[j] = raw<W>((const T*)p.dy + row * p.ldy + vec(j) * W, cnt);
+        nmean[j] = cnt ? p.mean[row * p.groups + vec(j) / q.gv] : 0.f;
+        nrstd[j] = cnt ? p.rstd[row * p.groups + vec(j) / q.gv] : 0.f;
+      }
+    }
+  };
+  // a[j] and b[j] of each vector into the sums over its group
+  auto join = [&](float (&a)[K], float (&b)[K], bool two) {
+    if (by_shuffles) {
+      for (int d = 1; d < q.gv; d *= 2)
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+          a[j] += __shfl_xor(a[j], d);
+          if (two) b[j] += __shfl_xor(b[j], d);
+        }
+      return;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      s_part[0][sub * q.lanes * K + vec(j)] = a[j];
+      s_part[1][sub * q.lanes * K + vec(j)] = b[j];
+    }
+    __syncthreads();
+    int team = 1;
+    while (team < 64 && team < q.gv) team *= 2;
+    for (int i = tid / team; i < rows * p.groups; i += NT / team) {
+      const int at = i / p.groups * q.lanes * K + i % p.groups * q.gv;
+      float ta = 0.f, tb = 0.f;
+      for (int k = tid & (team - 1); k < q.gv; k += team) {
+        ta += s_part[0][at + k];
+        tb += s_part[1][at + k];
+      }
+      for (int d = 1; d < team; d *= 2) {
+        ta += __shfl_xor(ta, d);
+        tb += __shfl_xor(tb, d);
+      }
+      if ((tid & (team - 1)) == 0) { s_sum[0][i] = ta; s_sum[1][i] = tb; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+      if (vec(j) < nv) {
+        a[j] = s_sum[0][sub * p.groups + vec(j) / q.gv];
+        b[j] = s_sum[1][sub * p.groups + vec(j) / q.gv];
+      }
+  };
+  constexpr bool AHEAD = !BWD || NT < 1024;                       // registers
+  const float inv = 1.f / (float)p.cg;
+  const long long stride = (long long)gridDim.x * rows, first = (long long)blockIdx.x * rows;
+  if (AHEAD) ask(first + sub);
+  for (long long r0 = first; r0 < q.samples; r0 += stride) {      // the same for the whole work-group
+    const long long row = r0 + sub;
+    const bool there = row < q.samples;
+    if (!AHEAD) ask(row);
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      x[j] = nx[j];
+      if constexpr (BWD) { dy[j] = ndy[j]; mean[j] = nmean[j]; rstd[j] = nrstd[j]; }
+    }
+    if (AHEAD && r0 + stride < q.samples) ask(row + stride);
+    float a[K], b[K];
+    if constexpr (!BWD) {
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        a[j] = b[j] = 0.f;
+#pragma unroll
+        for (int e = 0; e < W; ++e) a[j] += x[j].get(e);
+      }
+      join(a, b, false);
+      float m[K], d2[K];
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        m[j] = a[j] * inv;
+        d2[j] = b[j] = 0.f;
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          const float d = x[j].get(e) - m[j];
+          b[j] += d;                                              // what the rounding of the mean left
+          d2[j] = __builtin_fmaf(d, d, d2[j]);
+        }
+      }
+      join(d2, b, true);
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        const float shift = b[j] * inv, var = d2[j] * inv - shift * shift, rs = 1.f / sqrtf((var > 0.f || var != var ? var : 0.f) + p.eps);
+        m[j] += shift;
+        if (!there || vec(j) >= nv) continue;
+        if (vec(j) % q.gv == 0) {
+          p.mean_out[row * p.groups + vec(j) / q.gv] = m[j];
+          p.rstd_out[row * p.groups + vec(j) / q.gv] = rs;
+        }
+        float y[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) y[e] = __builtin_fmaf((x[j].get(e) - m[j]) * rs, ga[j][e], be[j][e]);
+        act8(p.act, y);
+        store8((T*)p.out + row * p.ldo + vec(j) * W, W, y);
+      }
+    } else {
+      float hat[K][W], dv[K][W];
+      with_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < K; ++j) slope8<decltype(act)::value, T>(ga[j], be[j], mean[j], rstd[j], x[j], dy[j], hat[j], dv[j]);
+      });
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        a[j] = b[j] = 0.f;
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          db[j][e] += dv[j][e];
+          da[j][e] = __builtin_fmaf(dv[j][e], hat[j][e], da[j][e]);
+          dv[j][e] *= ga[j][e];
+          a[j] += dv[j][e];
+          b[j] = __builtin_fmaf(dv[j][e], hat[j][e], b[j]);
+        }
+      }
+      if (!p.out) continue;
+      join(a, b, true);
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (!there || vec(j) >= nv) continue;
+        float d[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) d[e] = rstd[j] * ((dv[j][e] - a[j] * inv) - hat[j][e] * (b[j] * inv));
+        store8((T*)p.out + row * p.ldo + vec(j) * W, W, d);
+      }
+    }
+  }
+  if constexpr (BWD)
+    if (p.part)
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (vec(j) < nv) {
+          float* to = p.part + ((long long)blockIdx.x * rows + sub) * 2 * p.c + vec(j) * W;
+          store8(to, W, db[j]);
+          store8(to + p.c, W, da[j]);
+        }
+}
+
+// Images: a sample's positions of one block of whole groups, K positions of a vector of channels a thread.
+template <typename T, int NT, int K, bool BWD>
+__global__ __launch_bounds__(NT) void norm_image_kernel(ResidentP q) {
+  __shared__ float s_part[2][NT], s_sum[2][64];
+  __shared__ float s_chan[BWD ? 2 : 1][BWD ? W : 1][BWD ? NT : 1];
+  const NormP& p = q.n;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nv = p.c / W;
+  const long long sample = blockIdx.x / q.blocks;
+  const int v0 = (int)(blockIdx.x % q.blocks) * q.block, mine = nv - v0 < q.block ? nv - v0 : q.block;       // vectors of this block
+  const int lanes = NT / q.block, pos = tid / q.block, col = tid - pos * q.block, group = col / q.gv, groups = mine / q.gv;
+  const bool there = pos < lanes && col < mine;
+  const int c = (v0 + col) * W;
+  const long long row0 = sample * p.s;
+  float ga[W], be[W];
+  weights8(p, c, there, ga, be);
+  Raw<T, W> x[K], dy[BWD ? K : 1];
+  float mean = 0.f, rstd = 0.f;
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    const long long at = pos + (long long)j * lanes;
+    const int cnt = there && at < p.s ? W : 0;
+    x[j] = raw<W>((const T*)p.x + (row0 + at) * p.ldx + c, cnt);
+    if constexpr (BWD) dy[j] = raw<W>((const T*)p.dy + (row0 + at) * p.ldy + c, cnt);
+  }
+  if (BWD && there) {
+    mean = p.mean[sample * p.groups + (v0 + col) / q.gv];
+    rstd = p.rstd[sample * p.groups + (v0 + col) / q.gv];
+  }
+  auto have = [&](int j) { return there && pos + (long long)j * lanes < p.s; };
+  auto join = [&](float& a, float& b) {                           // over the positions and a group's vectors
+    __syncthreads();
+    s_part[0][tid] = a;
+    s_part[1][tid] = b;
+    __syncthreads();
+    for (int g = wave; g < groups; g += NT / 64) {
+      float ta = 0.f, tb = 0.f;
+      for (int i = lane; i < lanes * q.gv; i += 64) {
+        const int at = i / q.gv * q.block + g * q.gv + i % q.gv;
+        ta += s_part[0][at];
+        tb += s_part[1][at];
+      }
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) {
+        ta += __shfl_xor(ta, d);
+        tb += __shfl_xor(tb, d);
+      }
+      if (lane == 0) { s_sum[0][g] = ta; s_sum[1][g] = tb; }
+    }
+    __syncthreads();
+    if (there) { a = s_sum[0][group]; b = s_sum[1][group]; }
+  };
+  const float inv = 1.f / ((float)p.s * (float)p.cg);
+  float a = 0.f, b = 0.f;
+  if constexpr (!BWD) {
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+      for (int e = 0; e < W; ++e) a += x[j].get(e);               // zeros where there is no position
+    join(a, b);
+    mean = a * inv;
+    a = b = 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+      if (have(j))
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          const float d = x[j].get(e) - mean;
+          b += d;
+          a = __builtin_fmaf(d, d, a);
+        }
+    join(a, b);
+    const float shift = b * inv, var = a * inv - shift * shift;
+    mean += shift;
+    rstd = 1.f / sqrtf((var > 0.f || var != var ? var : 0.f) + p.eps);
+    if (there && pos == 0 && col % q.gv == 0) {
+      p.mean_out[sample * p.groups + (v0 + col) / q.gv] = mean;
+      p.rstd_out[sample * p.groups + (v0 + col) / q.gv] = rstd;
+    }
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (have(j)) {
+          float y[W], slope;
+#pragma unroll
+          for (int e = 0; e < W; ++e) act_one<decltype(act)::value>(__builtin_fmaf((x[j].get(e) - mean) * rstd, ga[e], be[e]), y[e], slope);
+          store8((T*)p.out + (row0 + pos + (long long)j * lanes) * p.ldo + c, W, y);
+        }
+    });
+  } else {
+    float da[W] = {}, db[W] = {};
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        float hat[W], dv[W];
+        slope8<decltype(act)::value, T>(ga, be, mean, rstd, x[j], dy[j], hat, dv);
+        if (have(j))
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            db[e] += dv[e];
+            da[e] = __builtin_fmaf(dv[e], hat[e], da[e]);
+          }
+      }
+    });
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      a = __builtin_fmaf(ga[e], db[e], a);
+      b = __builtin_fmaf(ga[e], da[e], b);
+      s_chan[0][e][tid] = db[e];
+      s_chan[BWD ? 1 : 0][e][tid] = da[e];
+    }
+    join(a, b);
+    if (p.part)                                                   // 2 W mine sums over the positions' lanes
+      for (int i = tid; i < 2 * W * mine; i += NT) {
+        const int which = i / (W * mine), rest = i - which * W * mine, v = rest / W, e = rest - v * W;
+        float t = 0.f;
+        for (int k = 0; k < lanes; ++k) t += s_chan[BWD ? which : 0][e][k * q.block + v];
+        p.part[(sample * 2 + which) * p.c + (v0 + v) * W + e] = t;
+      }
+    if (!p.out) return;
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (have(j)) {
+          float hat[W], dv[W];
+          slope8<decltype(act)::value, T>(ga, be, mean, rstd, x[j], dy[j], hat, dv);
+#pragma unroll
+          for (int e = 0; e < W; ++e) dv[e] = rstd * (__builtin_fmaf(ga[e], dv[e], -a * inv) - hat[e] * (b * inv));
+          store8((T*)p.out + (row0 + pos + (long long)j * lanes) * p.ldo + c, W, dv);
+        }
+    });
+  }
+}
+
 // dbeta and dgamma from the sums of all samples' chunks, in order.
 __global__ __launch_bounds__(256) void norm_weights_kernel(const float* part, long long rows, int c, float* dgamma, float* dbeta) {
   __shared__ float sums[8][32];
@@ -372,6 +697,50 @@ long long part_samples(const lms_group_norm_desc* d, const Split& t, int tensors
   return n < d->n ? n : d->n;
 }
 
+// How a work-group holds samples, if it does: from the sizes and the type alone.
+enum { NOT_HELD, TOKENS, IMAGES };
+struct Held {
+  int kind, nt, k, lanes, block, blocks;
+  long long grid, rows;                // rows of sums for gamma and beta
+};
+constexpr int TOKEN_GROUPS = 512;      // work-groups that go through the tokens
+Held held_of(const lms_group_norm_desc* d) {
+  Held h{};
+  const int cg = d->c / d->groups, nv = d->c / W, gv = cg / W;
+  if (cg % W) return h;
+  if (d->s == 1) {
+    int lanes = 1;
+    while (lanes < nv) lanes *= 2;
+    if (lanes <= 256) h = Held{TOKENS, 256, 1, lanes, 0, 0, 0, 0};
+    else if (nv <= 512) h = Held{TOKENS, 512, 1, 512, 0, 0, 0, 0};
+    else if (nv <= 1024) h = Held{TOKENS, 512, 2, 512, 0, 0, 0, 0};
+    else if (nv <= 2048) h = Held{TOKENS, 1024, 2, 1024, 0, 0, 0, 0};
+    else return h;
+    const long long rows = h.nt / h.lanes, need = (d->n + rows - 1) / rows;
+    h.grid = need < TOKEN_GROUPS ? need : TOKEN_GROUPS;
+    h.rows = h.grid * rows;
+    return h;
+  }
+  // at least 64 channels of whole groups, whose rows are a cache line
+  const int each = gv >= 8 ? 1 : (8 + gv - 1) / gv, groups = each < d->groups ? each : d->groups;
+  h.block = groups * gv;
+  h.blocks = (nv + h.block - 1) / h.block;
+  if (h.block > 512) return Held{};
+  for (const int nt : {256, 512}) {
+    if (h.block > nt) continue;
+    const long long k = (d->s + nt / h.block - 1) / (nt / h.block);
+    if (k > 8) continue;
+    if (d->n * h.blocks > (1LL << 31) / nt) return Held{};
+    h.kind = IMAGES;
+    h.nt = nt;
+    h.k = k <= 2 ? 2 : k <= 4 ? 4 : 8;
+    h.grid = d->n * h.blocks;
+    h.rows = d->n;
+    return h;
+  }
+  return Held{};
+}
+
 lms_status check(const char* what, const lms_group_norm_desc* d) {
   NEED(d->n >= 0 && d->s >= 1 && d->c >= 1, "%s: samples must be >= 0, positions and channels >= 1", what);
   NEED(d->c <= 1 << 20, "%s: more than 2^20 channels", what);
@@ -400,6 +769,27 @@ NormP params(const lms_group_norm_desc* d, const Split& t) {
   return p;
 }
 
+template <typename T, bool BWD>
+hipError_t resident(const lms_group_norm_desc* d, const Held& h, const NormP& p, hipStream_t s) {
+  ResidentP q{p, d->n, h.lanes, h.block, h.blocks, p.cg / W};
+  const dim3 grid((unsigned)h.grid);
+#define TOKEN(NT, K) if (h.kind == TOKENS && h.nt == NT && h.k == K) hipLaunchKernelGGL((norm_tokens_kernel<T, NT, K, BWD>), grid, dim3(NT), 0, s, q)
+#define IMAGE(NT, K) if (h.kind == IMAGES && h.nt == NT && h.k == K) hipLaunchKernelGGL((norm_image_kernel<T, NT, K, BWD>), grid, dim3(NT), 0, s, q)
+  TOKEN(256, 1);
+  TOKEN(512, 1);
+  TOKEN(512, 2);
+  TOKEN(1024, 2);
+  IMAGE(256, 2);
+  IMAGE(256, 4);
+  IMAGE(256, 8);
+  IMAGE(512, 2);
+  IMAGE(512, 4);
+  IMAGE(512, 8);
+#undef TOKEN
+#undef IMAGE
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t forward(const lms_group_norm_desc* d, const Split& t, NormP& p, hipStream_t s) {
   const long long part = part_samples(d, t, 1);
@@ -413,6 +803,11 @@ hipError_t forward(const lms_group_norm_desc* d, const Split& t, NormP& p, hipSt
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+hipError_t sum_weights(const float* part, long long rows, int c, float* dgamma, float* dbeta, hipStream_t s) {
+  hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2LL * c + 31) / 32)), dim3(256), 0, s, part, rows, c, dgamma, dbeta);
+  return hipGetLastError();
 }
 
 template <typename T>
@@ -429,9 +824,7 @@ hipError_t backward(const lms_group_norm_desc* d, const Split& t, NormP& p, floa
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (!dgamma && !dbeta) return hipSuccess;
-  hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2LL * d->c + 31) / 32)), dim3(256), 0, s, p.part, d->n * t.chunks, d->c, dgamma, dbeta);
-  return hipGetLastError();
+  return !dgamma && !dbeta ? hipSuccess : sum_weights(p.part, d->n * t.chunks, d->c, dgamma, dbeta, s);
 }
 
 uint64_t stat_bytes(const lms_group_norm_desc* d) { return up256((uint64_t)d->n * d->groups * 4); }
@@ -443,7 +836,9 @@ lms_status group_norm_workspace(const lms_group_norm_desc* d, int which, uint64_
   if (const lms_status st = check("lms_group_norm_workspace_bytes", d)) return st;
   NEED(which == LMS_GROUP_NORM_FWD || which == LMS_GROUP_NORM_BWD, "lms_group_norm_workspace_bytes: unknown call %d", which);
   const Split t = split_of(d);
+  const Held h = held_of(d);
   if (d->n == 0) *bytes = 0;
+  else if (h.kind != NOT_HELD) *bytes = 2 * stat_bytes(d) + (which == LMS_GROUP_NORM_BWD ? up256((uint64_t)h.rows * 2 * d->c * 4) : 0);
   else if (which == LMS_GROUP_NORM_FWD) *bytes = part_bytes(d, t, part_samples(d, t, 1)) + 2 * stat_bytes(d);
   else *bytes = part_bytes(d, t, d->n) + 2 * stat_bytes(d);
   return LMS_OK;
@@ -465,6 +860,8 @@ lms_status group_norm_fwd(const lms_group_norm_desc* d, const void* x, const flo
   p.part = (float*)(at + 2 * stat_bytes(d));
   p.x = x; p.gamma = gamma; p.beta = beta; p.out = y; p.ldo = p.ldy;
   hipStream_t s = (hipStream_t)stream;
+  const Held h = held_of(d);
+  if (h.kind != NOT_HELD) return done(what, d->dtype == LMS_F32 ? resident<float, false>(d, h, p, s) : resident<uint16_t, false>(d, h, p, s));
   return done(what, d->dtype == LMS_F32 ? forward<float>(d, t, p, s) : forward<uint16_t>(d, t, p, s));
 }
 
@@ -481,6 +878,12 @@ lms_status group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const vo
   p.part = (float*)((char*)ws + 2 * stat_bytes(d));
   p.x = x; p.dy = dy; p.gamma = gamma; p.beta = beta; p.mean = mean; p.rstd = rstd; p.out = dx; p.ldo = p.ldx;
   hipStream_t s = (hipStream_t)stream;
+  const Held h = held_of(d);
+  if (h.kind != NOT_HELD && d->n > 0) {
+    if (!dgamma && !dbeta) p.part = nullptr;
+    const hipError_t e = d->dtype == LMS_F32 ? resident<float, true>(d, h, p, s) : resident<uint16_t, true>(d, h, p, s);
+    return done(what, e != hipSuccess || !p.part ? e : sum_weights(p.part, h.rows, d->c, dgamma, dbeta, s));
+  }
   return done(what, d->dtype == LMS_F32 ? backward<float>(d, t, p, dgamma, dbeta, s) : backward<uint16_t>(d, t, p, dgamma, dbeta, s));
 }
 
