@@ -526,7 +526,7 @@ typedef struct {
 } lms_recur_desc;
 typedef enum { LMS_RECUR_FWD = 0, LMS_RECUR_BWD = 1 } lms_recur_which;
 lms_status lms_recur_workspace_bytes(const lms_recur_desc* d, int32_t which, uint64_t* bytes);
-/* Bytes of `kept`, what the forward pass leaves for the backward pass (16-byte aligned; may be NULL where this is 0): a state in fp32 for every 64 rows. */
+/* Bytes of `kept`, what the forward pass leaves for the backward pass (16-byte aligned; may be NULL where this is 0): a state in fp32 for every 32 rows. */
 lms_status lms_recur_kept_bytes(const lms_recur_desc* d, uint64_t* bytes);
 /* offsets: seqs + 1 row numbers that do not fall, sequence s has the rows offsets[s] .. offsets[s+1]-1 (none where they are equal); rows before the first and behind the last are neither read into
  * a result nor written.  NULL: all have rows / seqs rows.  h0, last: seqs x channels fp32, dense, the states before and after each sequence (last: h0 for one without

@@ -20,7 +20,7 @@ namespace lms {
 namespace {
 
 constexpr int BLOCK = 64 * V;          // of a wave and of a work-group
-constexpr int CHUNK = 64;              // rows of a work-group
+constexpr int KEEP = 32;               // rows between the states that the forward pass keeps
 constexpr long long PART_BYTES = 96LL << 20;                      // inputs of a part of the line
 
 struct RecurP {
@@ -31,7 +31,7 @@ struct RecurP {
   float *last, *dh0;
   float* sums;                 // [chunk of the part][2][channels]: A and H, or null
   float* in;                   // [chunk][channels]: state that enters a chunk (backward: r from the chunk behind), or null: none does
-  const float* kept;           // backward: what the forward pass had in `in`
+  float* kept;                 // [KEEP rows][channels]: state that enters them, or null
   long long rows, ldx, ldy, each;      // each: rows of a sequence where there are no offsets
   int seqs, channels, act;
   int chunk0, chunks, all_chunks;      // chunks of this launch
@@ -72,11 +72,10 @@ __device__ __forceinline__ Marks marks(const RecurP& p, long long r0) {
   return Marks{(unsigned)__ballot(first), (unsigned)__ballot(last), (unsigned)__ballot(live), s};
 }
 
-// a = sigmoid(g); rest = 1 - a without its cancellation.  Beyond 2^100 the exponential is cut: a is then nothing against any state, and rest 1.
-__device__ __forceinline__ void gate(float g, float& a, float& rest) {
-  const float e = __builtin_fminf(__builtin_amdgcn_exp2f(g * -1.44269504f), 0x1p100f);
-  a = __builtin_amdgcn_rcpf(1.f + e);
-  rest = e * a;
+// 1 - a for a = sigmoid(g), without its cancellation: the exponential that a has below its line, times a.  Beyond 2^100 it is cut: a is then nothing against any state, and the rest 1.
+__device__ __forceinline__ float rest_of(float g, float a) {
+  const float e = __builtin_amdgcn_exp2f(g * -1.44269504f);
+  return e < 0x1p100f ? e * a : 1.f;
 }
 
 // a h + (1 - a) x: a difference that is exact from a = 1/2 on, so that a state no gate touches stays what it is.
@@ -88,21 +87,31 @@ __device__ __forceinline__ float product(float a, float second) { return __built
 
 enum { SUM_FWD, APPLY_FWD, SUM_BWD, APPLY_BWD };
 
-template <int WAY>
+constexpr int CHUNK_FWD = 64, CHUNK_BWD = 32;                      // rows of a work-group
+static_assert(CHUNK_BWD == KEEP, "a chunk of the backward pass begins where a state is kept");
+
+// Rows of a wave: forward eight, whose raw inputs and gates leave registers for sixteen waves on a compute unit; backward, with twice the tensors, four; in fp32 half of that.
+template <typename T, int WAY>
 struct Shape {
-  static constexpr int ROWS = WAY == APPLY_BWD ? 4 : 8, WAVES = CHUNK / ROWS, NT = WAVES * 64;
+  static constexpr bool BWD = WAY == SUM_BWD || WAY == APPLY_BWD;
+  static constexpr int CHUNK = BWD ? CHUNK_BWD : CHUNK_FWD, WAVES = sizeof(T) == 2 ? 8 : 16, ROWS = CHUNK / WAVES, NT = WAVES * 64;
+  static_assert(KEEP % ROWS == 0 && ROWS < 32, "");
 };
 
-template <typename T, int WAY>
-__global__ __launch_bounds__((Shape<WAY>::NT)) void recur_kernel(RecurP p) {
-  constexpr int ROWS = Shape<WAY>::ROWS, WAVES = Shape<WAY>::WAVES;
-  constexpr bool BWD = WAY == SUM_BWD || WAY == APPLY_BWD, STATE = WAY != SUM_BWD;       // STATE: h is computed
+// WHOLE: at least four channels.  The last vector of a row that would end beyond it begins earlier instead, and its first channels are computed twice, alike.
+template <typename T, int WAY, bool WHOLE>
+__global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p) {
+  constexpr int ROWS = Shape<T, WAY>::ROWS, WAVES = Shape<T, WAY>::WAVES, CHUNK = Shape<T, WAY>::CHUNK;
+  constexpr bool BWD = Shape<T, WAY>::BWD, STATE = WAY != SUM_BWD;   // STATE: h is computed
   __shared__ float s_a[STATE ? WAVES : 1][BLOCK], s_h[STATE ? WAVES : 1][BLOCK], s_b[BWD ? WAVES : 1][BLOCK], s_r[BWD ? WAVES : 1][BLOCK];
   const int blocks = (p.channels + BLOCK - 1) / BLOCK, job = blockIdx.x;
-  const int chunk = job / blocks, at = (threadIdx.x & 63) * V, c = (job - chunk * blocks) * BLOCK + at, cnt = p.channels - c;
+  const int chunk = job / blocks, at = (threadIdx.x & 63) * V, c0 = (job - chunk * blocks) * BLOCK + at;
+  const unsigned c = WHOLE && c0 > p.channels - V ? p.channels - V : c0;       // an offset of 32 bits from what is the same for the wave
+  const bool column = c0 < p.channels;
+  const int cnt = WHOLE ? V : p.channels - c0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long r0 = (long long)(p.chunk0 + chunk) * CHUNK + wave * ROWS;
-  const bool there = cnt > 0 && r0 < p.rows, gated = p.o != nullptr;
+  const bool there = column && r0 < p.rows, gated = p.o != nullptr;
 
   // all that is read of the rows, in flight at once; rows beyond the last: the last, for nothing
   Raw<T, V> x[STATE ? ROWS : 1], g[ROWS], o[WAY == SUM_FWD ? 1 : ROWS], dy[BWD ? ROWS : 1];
@@ -120,41 +129,39 @@ __global__ __launch_bounds__((Shape<WAY>::NT)) void recur_kernel(RecurP p) {
         for (int r = 0; r < ROWS; ++r) o[r] = raw<V>((const T*)p.o + (r0 + r < p.rows ? r0 + r : p.rows - 1) * p.ldx + c, cnt);
   }
   float state[V] = {}, behind[V] = {};                            // h that enters the chunk; r that enters it from behind
-  if (cnt > 0) {
-    const long long entry = (long long)(p.chunk0 + chunk) * p.channels + c;
-    if (WAY == APPLY_FWD && p.in) load4(p.in + entry, cnt, state);
-    if (WAY == APPLY_BWD && p.kept) load4(p.kept + entry, cnt, state);
-    if (WAY == APPLY_BWD && p.in) load4(p.in + entry + p.channels, cnt, behind);
+  if (column) {
+    const long long entry = (long long)(p.chunk0 + chunk) * p.channels;
+    if (WAY == APPLY_FWD && p.in) load4(p.in + entry + c, cnt, state);
+    if (WAY == APPLY_BWD && p.kept) load4(p.kept + entry + c, cnt, state);
+    if (WAY == APPLY_BWD && p.in) load4(p.in + entry + p.channels + c, cnt, behind);
   }
   const Marks m = marks<ROWS>(p, r0);
-  auto of_sequence = [&](const float* t, int r, float (&v)[V]) {  // the values of row r's sequence, zeros where there are none
+  auto of_sequence = [&](const float* t, int r, float (&v)[V]) __attribute__((always_inline)) {  // the values of row r's sequence, zeros where there are none
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.f;
-    if (t && cnt > 0) load4(t + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, v);
+    if (t && column) load4(t + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, v);
   };
 
   // ---- the wave's spans ----
-  // Backwards R = sum over rows of e times the product of a up to the row, which needs no order from behind.
-  float a[ROWS][V], rest[WAY == APPLY_BWD ? ROWS : 1][V], value[WAY == SUM_FWD ? 1 : ROWS][V], slope[WAY == APPLY_BWD ? ROWS : 1][V];      // value: act(o), backwards e = dy act(o); slope: dy act'(o)
-  if constexpr (WAY != SUM_FWD) {
+  float a[ROWS][V], err[BWD ? ROWS : 1][V];                       // err: e = dy act(o)
+  if constexpr (BWD) {
     if (gated && there) with_act(p.act, [&](auto act) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          float val, sl;
-          act_one<decltype(act)::value>(o[r].get(e), val, sl);
-          value[r][e] = BWD ? val * dy[BWD ? r : 0].get(e) : val;
-          if constexpr (WAY == APPLY_BWD) slope[r][e] = sl * dy[r].get(e);
+          float value, slope;
+          act_one<decltype(act)::value>(o[r].get(e), value, slope);
+          err[r][e] = value * dy[r].get(e);
         }
     });
     else
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int e = 0; e < V; ++e) value[r][e] = BWD && there ? dy[BWD ? r : 0].get(e) : 1.f;
+        for (int e = 0; e < V; ++e) err[r][e] = there ? dy[r].get(e) : 0.f;
   }
-  float A[V], H[V], B[V], R[V];                                   // B: A of the way backwards
+  float A[V], H[V], B[V], R[V];                                   // B: A of the way backwards.  R = sum over rows of e times the product of a up to the row, which needs no order from behind
 #pragma unroll
   for (int e = 0; e < V; ++e) { A[e] = B[e] = 1.f; H[e] = R[e] = 0.f; }
 #pragma unroll
@@ -166,14 +173,10 @@ __global__ __launch_bounds__((Shape<WAY>::NT)) void recur_kernel(RecurP p) {
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      float s, sr;
-      gate(there ? g[r].get(e) : 0.f, s, sr);
-      a[r][e] = s;
-      if constexpr (WAY == APPLY_BWD) rest[r][e] = sr;
+      a[r][e] = sigmoid(there ? g[r].get(e) : 0.f);
       if constexpr (STATE) {
-        const float xv = there ? x[r].get(e) : 0.f;
-        A[e] *= s;
-        H[e] = mix(s, H[e], xv);
+        A[e] *= a[r][e];
+        H[e] = mix(a[r][e], H[e], there ? x[r].get(e) : 0.f);
       }
     }
     if constexpr (BWD)
@@ -184,7 +187,7 @@ __global__ __launch_bounds__((Shape<WAY>::NT)) void recur_kernel(RecurP p) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           B[e] *= a[r][e];
-          R[e] = __builtin_fmaf(B[e], value[r][e] + d[e], R[e]);
+          R[e] = __builtin_fmaf(B[e], err[r][e] + d[e], R[e]);
           if (end) B[e] = -0.f;
         }
       }
@@ -193,12 +196,12 @@ __global__ __launch_bounds__((Shape<WAY>::NT)) void recur_kernel(RecurP p) {
   if constexpr (STATE) { put(s_a[wave], A); put(s_h[wave], H); }
   if constexpr (BWD) { put(s_b[wave], B); put(s_r[wave], R); }
   __syncthreads();
-  auto compose = [&](const float (&sa)[BLOCK], const float (&sh)[BLOCK], float (&v)[V]) {
+  auto compose = [&](const float (&sa)[BLOCK], const float (&sh)[BLOCK], float (&v)[V]) __attribute__((always_inline)) {
     const float4 k = *reinterpret_cast<const float4*>(&sa[at]), d = *reinterpret_cast<const float4*>(&sh[at]);
     v[0] = through(k.x, v[0], d.x); v[1] = through(k.y, v[1], d.y); v[2] = through(k.z, v[2], d.z); v[3] = through(k.w, v[3], d.w);
   };
   if constexpr (WAY == SUM_FWD || WAY == SUM_BWD) {
-    if (wave != 0 || cnt <= 0) return;
+    if (wave != 0 || !column) return;
     float k[V] = {1.f, 1.f, 1.f, 1.f}, d[V] = {};
     for (int i = 0; i < WAVES; ++i) {
       const int w = WAY == SUM_FWD ? i : WAVES - 1 - i;
@@ -218,65 +221,96 @@ __global__ __launch_bounds__((Shape<WAY>::NT)) void recur_kernel(RecurP p) {
       float* to = BWD ? p.dh0 : p.last;
       const float* from = BWD ? p.dlast : p.h0;
       if (to && (p.offsets || p.rows == 0))
-        for (int s0 = wave * 64; s0 < p.seqs; s0 += Shape<WAY>::NT) {
+        for (int s0 = wave * 64; s0 < p.seqs; s0 += Shape<T, WAY>::NT) {
           const int s = s0 + (threadIdx.x & 63);
           unsigned long long empty = __ballot(s < p.seqs && (!p.offsets || p.offsets[s] == p.offsets[s + 1]));
           for (; empty; empty &= empty - 1) {
             const long long entry = (long long)(s0 + __builtin_ctzll(empty)) * p.channels + c;
             float v[V] = {};
-            if (from && cnt > 0) load4(from + entry, cnt, v);
+            if (!column) continue;
+            if (from) load4(from + entry, cnt, v);
             store4(to + entry, cnt, v);
           }
         }
     }
     if (!there) return;
+    // what was computed of the inputs is computed again from here on: kept, it takes twice the registers of the inputs, and with them the second work-group of a compute unit
+    auto anew = [](auto& t) __attribute__((always_inline)) {
+#pragma unroll
+      for (auto& v : t)
+#pragma unroll
+        for (unsigned& w : v.q) asm volatile("" : "+v"(w));
+    };
+    anew(x);
+    if constexpr (BWD) { anew(g); anew(o); }
     for (int w = 0; w < wave; ++w) compose(s_a[w], s_h[w], state);
-    float h[BWD ? ROWS : 1][V], now[V];
+    auto entry_of = [&](int r) { return (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c; };
+    if constexpr (WAY == APPLY_FWD) {
+      if (p.kept && r0 % KEEP == 0) store4(p.kept + r0 / KEEP * p.channels + c, cnt, state);
+      auto finish = [&](auto act, auto with_gate) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) now[e] = state[e];
+        for (int r = 0; r < ROWS; ++r) {
+          if (m.first >> r & 1) of_sequence(p.h0, r, state);
+          float y[V];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      if (m.first >> r & 1) of_sequence(p.h0, r, now);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float xv = x[r].get(e);
-        now[e] = mix(a[r][e], now[e], xv);
-        if constexpr (BWD) h[r][e] = now[e];
-      }
-      if constexpr (WAY == APPLY_FWD) {
-        if (!(m.live >> r & 1)) continue;
-        float y[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = now[e] * value[r][e];
-        store4((T*)p.y + (r0 + r) * p.ldy + c, cnt, y);
-        if ((m.last >> r & 1) && p.last) store4(p.last + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, now);
-      }
-    }
-    if constexpr (WAY == APPLY_BWD) {
-      for (int w = WAVES - 1; w > wave; --w) compose(s_b[w], s_r[w], behind);
-#pragma unroll
-      for (int r = ROWS - 1; r >= 0; --r) {
-        if (!(m.live >> r & 1)) continue;
-        const bool first = m.first >> r & 1;
-        if (m.last >> r & 1) of_sequence(p.dlast, r, behind);
-        float before[V], dx[V], dg[V], dout[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) before[e] = r > 0 ? h[r > 0 ? r - 1 : 0][e] : state[e];
-        if (first) of_sequence(p.h0, r, before);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float dh = value[r][e] + behind[e];
-          dx[e] = rest[r][e] * dh;
-          behind[e] = a[r][e] * dh;
-          dg[e] = behind[e] * rest[r][e] * (before[e] - x[r].get(e));
-          dout[e] = slope[r][e] * h[r][e];
+          for (int e = 0; e < V; ++e) {
+            y[e] = state[e] = mix(a[r][e], state[e], x[r].get(e));
+            if constexpr (decltype(with_gate)::value) {
+              float value, slope;
+              act_one<decltype(act)::value>(o[r].get(e), value, slope);
+              y[e] *= value;
+            }
+          }
+          if (!(m.live >> r & 1)) continue;
+          store4((T*)p.y + (r0 + r) * p.ldy + c, cnt, y);
+          if ((m.last >> r & 1) && p.last) store4(p.last + entry_of(r), cnt, state);
         }
-        const long long to = (r0 + r) * p.ldx + c;
-        if (p.dx) store4((T*)p.dx + to, cnt, dx);
-        if (p.dg) store4((T*)p.dg + to, cnt, dg);
-        if (p.dout) store4((T*)p.dout + to, cnt, dout);
-        if (first && p.dh0) store4(p.dh0 + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, behind);
+      };
+      if (gated) with_act(p.act, [&](auto act) __attribute__((always_inline)) { finish(act, std::true_type{}); });
+      else finish(std::integral_constant<int, LMS_ACT_NONE>{}, std::false_type{});
+    } else {
+      float h[ROWS][V], now[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) now[e] = state[e];
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        if (m.first >> r & 1) of_sequence(p.h0, r, now);
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[r][e] = now[e] = mix(a[r][e], now[e], x[r].get(e));
       }
+      for (int w = WAVES - 1; w > wave; --w) compose(s_b[w], s_r[w], behind);
+      auto finish = [&](auto act, auto with_gate) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = ROWS - 1; r >= 0; --r) {
+          if (!(m.live >> r & 1)) continue;
+          const bool first = m.first >> r & 1;
+          if (m.last >> r & 1) of_sequence(p.dlast, r, behind);
+          float before[V], dx[V], dg[V], dout[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) before[e] = r > 0 ? h[r > 0 ? r - 1 : 0][e] : state[e];
+          if (first) of_sequence(p.h0, r, before);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float dh = err[r][e] + behind[e], rest = rest_of(g[r].get(e), a[r][e]);
+            dx[e] = rest * dh;
+            behind[e] = a[r][e] * dh;
+            dg[e] = behind[e] * rest * (before[e] - x[r].get(e));
+            if constexpr (decltype(with_gate)::value) {
+              float value, slope;
+              act_one<decltype(act)::value>(o[r].get(e), value, slope);
+              dout[e] = dy[r].get(e) * slope * h[r][e];
+            }
+          }
+          const long long to = (r0 + r) * p.ldx;
+          if (p.dx) store4((T*)p.dx + to + c, cnt, dx);
+          if (p.dg) store4((T*)p.dg + to + c, cnt, dg);
+          if constexpr (decltype(with_gate)::value)
+            if (p.dout) store4((T*)p.dout + to + c, cnt, dout);
+          if (first && p.dh0) store4(p.dh0 + entry_of(r), cnt, behind);
+        }
+      };
+      if (gated) with_act(p.act, [&](auto act) __attribute__((always_inline)) { finish(act, std::true_type{}); });
+      else finish(std::integral_constant<int, LMS_ACT_NONE>{}, std::false_type{});
     }
   }
 }
@@ -341,10 +375,7 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurP p, const int32_t
     float y[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      float a, rest;
-      gate(g.get(e), a, rest);
-      const float xv = x.get(e);
-      y[e] = h[e] = mix(a, h[e], xv);
+      y[e] = h[e] = mix(sigmoid(g.get(e)), h[e], x.get(e));
     }
     if (p.o) with_act(p.act, [&](auto act) {
 #pragma unroll
@@ -366,22 +397,22 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurP p, const int32_t
   if (cnt > 0) store4(to + (long long)slot * p.channels + c, cnt, h);
 }
 
-long long chunks_of(long long rows) { return rows <= CHUNK ? 1 : (rows + CHUNK - 1) / CHUNK; }
-// Chunks of a part of the line: the rows of its inputs take PART_BYTES at most.
-long long part_chunks(const lms_recur_desc* d) {
-  const long long bytes = (long long)CHUNK * d->channels * (d->dtype == LMS_F32 ? 4 : 2) * 3, fit = PART_BYTES / bytes, blocks = (d->channels + BLOCK - 1) / BLOCK;
-  const long long most = (1LL << 21) / blocks;                    // 2^21 work-groups of up to 1024 threads are a grid
+long long chunks_of(long long rows, int chunk) { return rows <= chunk ? 1 : (rows + chunk - 1) / chunk; }
+// Chunks of a part of the line, whose rows' inputs take PART_BYTES at most.
+long long part_chunks(const lms_recur_desc* d, int chunk) {
+  const long long bytes = (long long)chunk * d->channels * (d->dtype == LMS_F32 ? 4 : 2) * 3, fit = PART_BYTES / bytes, blocks = (d->channels + BLOCK - 1) / BLOCK;
+  const long long most = (1LL << 21) / blocks;                    // 2^21 work-groups of 512 threads are a grid
   return fit < 1 ? 1 : fit < most ? fit : most;
 }
-uint64_t sums_bytes(const lms_recur_desc* d) {
-  const long long part = part_chunks(d), all = chunks_of(d->rows);
+uint64_t sums_bytes(const lms_recur_desc* d, int chunk) {
+  const long long part = part_chunks(d, chunk), all = chunks_of(d->rows, chunk);
   return up256((uint64_t)(part < all ? part : all) * 2 * d->channels * 4);
 }
-uint64_t in_bytes(const lms_recur_desc* d) { return up256((uint64_t)(chunks_of(d->rows) + 1) * d->channels * 4); }
+uint64_t in_bytes(const lms_recur_desc* d, int chunk) { return up256((uint64_t)(chunks_of(d->rows, chunk) + 1) * d->channels * 4); }
 
 lms_status check(const char* what, const lms_recur_desc* d, bool step) {
   NEED(d->rows >= 0 && d->channels >= 1 && d->seqs >= 1, "%s: rows must be >= 0, channels and sequences >= 1", what);
-  NEED(d->rows <= 0x7fffffffLL - CHUNK, "%s: more than 2^31 - 65 rows", what);
+  NEED(d->rows <= 0x7fffffffLL - 64, "%s: more than 2^31 - 65 rows", what);
   NEED(d->channels <= 1 << 26 && d->seqs <= 1 << 30, "%s: more than 2^26 channels, or 2^30 sequences", what);
   NEED(d->act >= LMS_ACT_NONE && d->act <= LMS_ACT_GELU_TANH, "%s: unknown activation %d", what, d->act);
   NEED(d->dtype == LMS_BF16 || d->dtype == LMS_F32, "%s: dtype must be LMS_BF16 or LMS_F32", what);
@@ -407,22 +438,24 @@ bool overlap(const lms_recur_desc* d, const float* a, const float* b) {
   const uintptr_t n = (uintptr_t)d->seqs * d->channels * 4, x = (uintptr_t)a, y = (uintptr_t)b;
   return a && b && x < y + n && y < x + n;
 }
-RecurP params(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0) {
+RecurP params(const lms_recur_desc* d, int chunk, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0) {
   RecurP p{};
   p.x = x; p.g = g; p.o = o; p.offsets = offsets; p.h0 = h0;
   p.rows = d->rows; p.ldx = d->ldx ? d->ldx : d->channels; p.ldy = d->ldy ? d->ldy : d->channels;
   p.each = d->rows / d->seqs > 0 ? d->rows / d->seqs : 1;
   p.seqs = d->seqs; p.channels = d->channels; p.act = d->act;
-  p.all_chunks = (int)chunks_of(d->rows);
+  p.all_chunks = (int)chunks_of(d->rows, chunk);
   return p;
 }
 // No chunk needs what another leaves: one chunk, or whole sequences in each.
-bool alone(const lms_recur_desc* d, const int32_t* offsets) { return d->rows <= CHUNK || (!offsets && CHUNK % (d->rows / d->seqs) == 0); }
+bool alone(const lms_recur_desc* d, int chunk, const int32_t* offsets) { return d->rows <= chunk || (!offsets && chunk % (d->rows / d->seqs) == 0); }
 
 template <typename T, int WAY>
 hipError_t launch(const RecurP& p, hipStream_t s) {
   const int blocks = (p.channels + BLOCK - 1) / BLOCK;
-  hipLaunchKernelGGL((recur_kernel<T, WAY>), dim3((unsigned)(blocks * p.chunks)), dim3(Shape<WAY>::NT), 0, s, p);
+  const dim3 grid((unsigned)(blocks * p.chunks)), threads((Shape<T, WAY>::NT));
+  if (p.channels >= V) hipLaunchKernelGGL((recur_kernel<T, WAY, true>), grid, threads, 0, s, p);
+  else hipLaunchKernelGGL((recur_kernel<T, WAY, false>), grid, threads, 0, s, p);
   return hipGetLastError();
 }
 
@@ -454,14 +487,15 @@ hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
 
 lms_status recur_kept(const lms_recur_desc* d, uint64_t* bytes) {
   if (const lms_status st = check("lms_recur_kept_bytes", d, false)) return st;
-  *bytes = d->rows <= CHUNK ? 0 : in_bytes(d);
+  *bytes = d->rows <= CHUNK_BWD ? 0 : up256((uint64_t)chunks_of(d->rows, KEEP) * d->channels * 4);
   return LMS_OK;
 }
 
 lms_status recur_workspace(const lms_recur_desc* d, int which, uint64_t* bytes) {
   if (const lms_status st = check("lms_recur_workspace_bytes", d, false)) return st;
   NEED(which == LMS_RECUR_FWD || which == LMS_RECUR_BWD, "lms_recur_workspace_bytes: unknown call %d", which);
-  *bytes = d->rows <= CHUNK ? 0 : sums_bytes(d) + in_bytes(d);
+  const int chunk = which == LMS_RECUR_FWD ? CHUNK_FWD : CHUNK_BWD;
+  *bytes = d->rows <= chunk ? 0 : sums_bytes(d, chunk) + in_bytes(d, chunk);
   return LMS_OK;
 }
 
@@ -476,13 +510,15 @@ lms_status recur_fwd(const lms_recur_desc* d, const void* x, const void* g, cons
   recur_workspace(d, LMS_RECUR_FWD, &need);
   NEED(!need || ws, "%s: workspace of %llu bytes required", what, (unsigned long long)need);
   NEED((((uintptr_t)ws | (uintptr_t)kept) & 15) == 0, "%s: the workspace is not aligned", what);
-  RecurP p = params(d, x, g, o, offsets, h0);
+  RecurP p = params(d, CHUNK_FWD, x, g, o, offsets, h0);
   p.y = y; p.last = last;
+  p.kept = d->rows <= CHUNK_BWD ? nullptr : (float*)kept;
   p.sums = (float*)ws;
-  p.in = kept ? (float*)kept : (float*)((char*)ws + sums_bytes(d));
-  const bool whole = alone(d, offsets);
+  p.in = (float*)((char*)ws + sums_bytes(d, CHUNK_FWD));
+  const bool whole = alone(d, CHUNK_FWD, offsets);
+  const long long part = part_chunks(d, CHUNK_FWD);
   hipStream_t s = (hipStream_t)stream;
-  return done(what, d->dtype == LMS_F32 ? line<float, false>(p, whole, part_chunks(d), s) : line<uint16_t, false>(p, whole, part_chunks(d), s));
+  return done(what, d->dtype == LMS_F32 ? line<float, false>(p, whole, part, s) : line<uint16_t, false>(p, whole, part, s));
 }
 
 lms_status recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, const void* kept, const float* dlast,
@@ -493,20 +529,21 @@ lms_status recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, con
   if (const lms_status st = aligned(what, d, {dy, x, g, o, dx, dg, dout}, {offsets, h0, dlast, dh0})) return st;
   NEED(o || !dout, "%s: the gradient of o needs o", what);
   NEED(!overlap(d, dlast, dh0) && !overlap(d, h0, dh0), "%s: the gradient of the initial states must not overlap the states or the gradient of the last ones", what);
-  const bool whole = alone(d, offsets);
+  const bool whole = alone(d, CHUNK_BWD, offsets);
   NEED(whole || kept, "%s: what the forward pass kept is needed", what);
   uint64_t need = 0;
   recur_workspace(d, LMS_RECUR_BWD, &need);
   NEED(!need || ws, "%s: workspace of %llu bytes required", what, (unsigned long long)need);
   NEED((((uintptr_t)ws | (uintptr_t)kept) & 15) == 0, "%s: the workspace is not aligned", what);
-  RecurP p = params(d, x, g, o, offsets, h0);
+  RecurP p = params(d, CHUNK_BWD, x, g, o, offsets, h0);
   p.dy = dy; p.dlast = dlast;
   p.dx = dx; p.dg = dg; p.dout = dout; p.dh0 = dh0;
-  p.kept = whole ? nullptr : (const float*)kept;
+  p.kept = whole ? nullptr : (float*)const_cast<void*>(kept);
   p.sums = (float*)ws;
-  p.in = (float*)((char*)ws + sums_bytes(d));
+  p.in = (float*)((char*)ws + sums_bytes(d, CHUNK_BWD));
+  const long long part = part_chunks(d, CHUNK_BWD);
   hipStream_t s = (hipStream_t)stream;
-  return done(what, d->dtype == LMS_F32 ? line<float, true>(p, whole, part_chunks(d), s) : line<uint16_t, true>(p, whole, part_chunks(d), s));
+  return done(what, d->dtype == LMS_F32 ? line<float, true>(p, whole, part, s) : line<uint16_t, true>(p, whole, part, s));
 }
 
 lms_status recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream) {
@@ -515,7 +552,7 @@ lms_status recur_step(const lms_recur_desc* d, const void* x, const void* g, con
   if (const lms_status st = aligned(what, d, {x, g, o, y}, {slots, state, next})) return st;
   NEED(state == next || !overlap(d, state, next), "%s: the new states are the old ones or apart from them", what);
   if (d->rows == 0) return LMS_OK;
-  RecurP p = params(d, x, g, o, nullptr, nullptr);
+  RecurP p = params(d, CHUNK_FWD, x, g, o, nullptr, nullptr);
   p.y = y;
   const long long groups = d->rows * ((d->channels + 4 * BLOCK - 1) / (4 * BLOCK));
   NEED(groups < 1 << 24, "%s: rows times channels above 2^34", what);
