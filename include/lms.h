@@ -583,7 +583,7 @@ lms_status lms_linear_q8_product(const lms_linear_q8_desc* d, const void* xq, co
  * the first draft i that is not accepted (from p_i where that is 0 everywhere), from the row of p behind the last draft where all are: the first class whose running sum is above v times the
  * whole (the last class with a share, if rounding leaves none; -1 if no class has one).  What is NaN or below 0 has no share; drafted tokens that are no class are not accepted. */
 typedef struct {
-  int32_t requests;         /* 0 .. 2^20 */
+  int32_t requests;         /* 0 .. 2^20, and requests * classes at most 2^34 */
   int32_t drafts;           /* places for drafts of a request, 0 .. 1024 */
   int32_t classes;          /* >= 1 */
   int64_t ldp, ldq;         /* row pitches of p and q */

@@ -16,7 +16,6 @@ namespace {
 
 constexpr int NT = 512, WAVES = NT / 64;
 constexpr int U = 8;                   // rows of a thread in flight
-constexpr long long PART_BYTES = 96LL << 20;                      // inputs that are read again before they have left the last-level cache
 
 struct NormP {
   const void *x, *dy;
@@ -36,7 +35,10 @@ struct NormP {
 struct Place {
   long long sample, row0, rows;        // rows of the chunk
   int chunk, c, cnt, first, stride;
+  bool there;
 };
+// WHOLE: at least four channels.  The last vector of a row that would end beyond it begins earlier instead, and its first channels are computed twice, alike.
+template <bool WHOLE>
 __device__ __forceinline__ Place place(const NormP& p, int job) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rpw = 64 / p.lpr;
   const int cb = job % p.cblocks, at = job / p.cblocks;
@@ -47,7 +49,9 @@ __device__ __forceinline__ Place place(const NormP& p, int job) {
   t.rows = p.s - begin < p.chunk_rows ? p.s - begin : p.chunk_rows;
   t.row0 = t.sample * p.s + begin;
   t.c = (cb * p.lpr + lane % p.lpr) * V;
-  t.cnt = p.c - t.c;
+  t.there = t.c < p.c;
+  if (WHOLE && t.c > p.c - V) t.c = p.c - V;
+  t.cnt = WHOLE ? V : p.c - t.c;
   t.first = wave * rpw + lane / p.lpr;
   t.stride = WAVES * rpw;
   return t;
@@ -74,7 +78,7 @@ struct Coef {
 __device__ __forceinline__ void merge(float& n, float (&mean)[V], float (&m2)[V], float nb, const float (&mb)[V], const float (&qb)[V]) {
   const float all = n + nb;
   if (nb == 0.f) return;
-  const float share = nb / all;
+  const float share = nb * __builtin_amdgcn_rcpf(all);            // within an ulp: it weighs a distance
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     const float d = mb[e] - mean[e];
@@ -84,106 +88,149 @@ __device__ __forceinline__ void merge(float& n, float (&mean)[V], float (&m2)[V]
   n = all;
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(NT) void norm_stats_kernel(NormP p) {
   __shared__ float s_n[WAVES][64], s_mean[WAVES][64][V], s_m2[WAVES][64][V];
-  const Place t = place(p, blockIdx.x);
+  const Place t = place<WHOLE>(p, blockIdx.x);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float n = 0.f, mean[V] = {}, m2[V] = {};
   const T* x = (const T*)p.x + t.row0 * p.ldx + t.c;
-  if (t.cnt > 0)
+  if (t.there) {
+    Raw<T, V> v[U], next[U];
+    auto ask = [&](long long r) {                                 // rows beyond the last: the thread's first, for nothing
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = raw<V>(x + (r + u * t.stride < t.rows ? r + u * t.stride : t.first) * p.ldx, t.cnt);
+    };
+    if (t.first < t.rows) ask(t.first);
     for (long long r = t.first; r < t.rows; r += (long long)U * t.stride) {
-      Raw<T, V> v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = raw<V>(x + (r + u * t.stride < t.rows ? r + u * t.stride : r) * p.ldx, t.cnt);
+      for (int u = 0; u < U; ++u) v[u] = next[u];
+      if (r + U * t.stride < t.rows) ask(r + U * t.stride);       // while these are worked on
       float nb = 0.f, mb[V] = {}, qb[V] = {};
+      auto batch = [&](auto whole) {
+        auto have = [&](int u) { return decltype(whole)::value || r + u * t.stride < t.rows; };
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + u * t.stride < t.rows) {
-          nb += 1.f;
+        for (int u = 0; u < U; ++u)
+          if (have(u)) {
+            nb += 1.f;
 #pragma unroll
-          for (int e = 0; e < V; ++e) mb[e] += v[u].get(e);
-        }
-      const float inv = 1.f / nb;
-#pragma unroll
-      for (int e = 0; e < V; ++e) mb[e] *= inv;
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + u * t.stride < t.rows)
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float d = v[u].get(e) - mb[e];
-            qb[e] = __builtin_fmaf(d, d, qb[e]);
+            for (int e = 0; e < V; ++e) mb[e] += v[u].get(e);
           }
+        const float inv = decltype(whole)::value ? 1.f / U : 1.f / nb;
+#pragma unroll
+        for (int e = 0; e < V; ++e) mb[e] *= inv;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (have(u))
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const float d = v[u].get(e) - mb[e];
+              qb[e] = __builtin_fmaf(d, d, qb[e]);
+            }
+      };
+      if (r + (U - 1) * t.stride < t.rows) batch(std::true_type{});
+      else batch(std::false_type{});
       merge(n, mean, m2, nb, mb, qb);
     }
+  }
+  for (int d = p.lpr; d < 64; d *= 2) {                           // the wave's rows of this column; both sides compute the same
+    const bool upper = lane & d;
+    float mb[V], qb[V];
+    const float nb = __shfl_xor(n, d);
+#pragma unroll
+    for (int e = 0; e < V; ++e) { mb[e] = __shfl_xor(mean[e], d); qb[e] = __shfl_xor(m2[e], d); }
+    if (!upper) merge(n, mean, m2, nb, mb, qb);
+  }
   s_n[wave][lane] = n;
 #pragma unroll
   for (int e = 0; e < V; ++e) { s_mean[wave][lane][e] = mean[e]; s_m2[wave][lane][e] = m2[e]; }
   __syncthreads();
-  if (threadIdx.x >= p.lpr || t.cnt <= 0) return;
-  for (int i = 0; i < WAVES * (64 / p.lpr); ++i) {                // this column's other rows
-    const int w = i / (64 / p.lpr), l = i % (64 / p.lpr) * p.lpr + lane;
-    if (w == 0 && l == lane) continue;
+  if (threadIdx.x >= p.lpr || !t.there) return;
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) {
     float mb[V], qb[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) { mb[e] = s_mean[w][l][e]; qb[e] = s_m2[w][l][e]; }
-    if (n == 0.f && s_n[w][l] == 0.f) continue;
-    merge(n, mean, m2, s_n[w][l], mb, qb);
+    for (int e = 0; e < V; ++e) { mb[e] = s_mean[w][lane][e]; qb[e] = s_m2[w][lane][e]; }
+    merge(n, mean, m2, s_n[w][lane], mb, qb);
   }
   float* to = p.part + ((t.sample - p.sample0) * p.chunks + t.chunk) * 2 * p.c + t.c;
   store4(to, t.cnt, mean);
   store4(to + p.c, t.cnt, m2);
 }
 
-// Sum of v over a work-group of 256, in a fixed order.
-__device__ __forceinline__ float group_sum(float v, float* lds) {
+// Sums of v and w over a work-group of JT threads, in a fixed order.
+constexpr int JT = 1024;
+__device__ __forceinline__ void group_sum(float& v, float& w, float (&lds)[2][JT / 64]) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  for (int d = 32; d > 0; d >>= 1) {
+    v += __shfl_xor(v, d);
+    w += __shfl_xor(w, d);
+  }
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0) { lds[0][threadIdx.x >> 6] = v; lds[1][threadIdx.x >> 6] = w; }
   __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  v = w = 0.f;
+#pragma unroll
+  for (int i = 0; i < JT / 64; ++i) { v += lds[0][i]; w += lds[1][i]; }
+}
+// f(chunk, channel of the group, the chunk's two values of the channel) for a group's chunks and channels, four in flight.
+template <typename F>
+__device__ __forceinline__ void each_partial(const NormP& p, const float* part, F&& f) {
+  constexpr int IN_FLIGHT = 4;
+  const int items = p.chunks * p.cg, dchunk = JT / p.cg, dc = JT - dchunk * p.cg;
+  int chunk = (int)threadIdx.x / p.cg, c = (int)threadIdx.x - chunk * p.cg;
+  for (int i = threadIdx.x; i < items; i += IN_FLIGHT * JT) {
+    float a[IN_FLIGHT], b[IN_FLIGHT];
+    int ch[IN_FLIGHT], cc[IN_FLIGHT];
+#pragma unroll
+    for (int u = 0; u < IN_FLIGHT; ++u) {
+      ch[u] = chunk;
+      cc[u] = c;
+      const float* at = part + (i + u * JT < items ? (long long)chunk * 2 * p.c + c : 0);
+      a[u] = at[0];
+      b[u] = at[p.c];
+      chunk += dchunk;
+      c += dc;
+      if (c >= p.cg) { c -= p.cg; ++chunk; }
+    }
+#pragma unroll
+    for (int u = 0; u < IN_FLIGHT; ++u)
+      if (i + u * JT < items) f(ch[u], cc[u], a[u], b[u]);
+  }
 }
 
 // Mean and 1 / deviation of a group from its channels' chunks.
-__global__ __launch_bounds__(256) void norm_join_kernel(NormP p) {
-  __shared__ float lds[4];
+__global__ __launch_bounds__(JT) void norm_join_kernel(NormP p) {
+  __shared__ float lds[2][JT / 64];
   const int g = blockIdx.x % p.groups;
-  const long long local = blockIdx.x / p.groups, sample = p.sample0 + local, items = (long long)p.chunks * p.cg;
+  const long long local = blockIdx.x / p.groups, sample = p.sample0 + local;
   const float* part = p.part + local * p.chunks * 2 * p.c + g * p.cg;
   const float inv = 1.f / ((float)p.s * (float)p.cg);
-  auto each = [&](auto&& f) {                                     // f(rows, mean, squared deviations)
-    for (long long i = threadIdx.x; i < items; i += 256) {
-      const int chunk = (int)(i / p.cg), c = (int)(i - (long long)chunk * p.cg);
-      const long long left = p.s - chunk * p.chunk_rows;
-      const float* at = part + (long long)chunk * 2 * p.c + c;
-      f((float)(left < p.chunk_rows ? left : p.chunk_rows), at[0], at[p.c]);
-    }
-  };
-  float sum = 0.f, dev = 0.f;
-  each([&](float n, float mean, float) { sum = __builtin_fmaf(n, mean, sum); });
-  const float mean = group_sum(sum, lds) * inv;
+  const float full = (float)p.chunk_rows, last = (float)(p.s - (p.chunks - 1) * p.chunk_rows);      // rows of a chunk
+  float sum = 0.f, unused = 0.f;
+  each_partial(p, part, [&](int chunk, int, float mean, float) { sum = __builtin_fmaf(chunk + 1 < p.chunks ? full : last, mean, sum); });
+  group_sum(sum, unused, lds);
+  const float mean = sum * inv;
   // what the rounding of the mean leaves is taken out of it: the deviations' own sum
-  float rest = 0.f;
-  each([&](float n, float m, float m2) {
-    const float d = m - mean;
+  float rest = 0.f, dev = 0.f;
+  each_partial(p, part, [&](int chunk, int, float m, float m2) {
+    const float n = chunk + 1 < p.chunks ? full : last, d = m - mean;
     rest = __builtin_fmaf(n, d, rest);
     dev += __builtin_fmaf(n * d, d, m2);
   });
-  const float shift = group_sum(rest, lds) * inv;
-  const float var = group_sum(dev, lds) * inv - shift * shift;
+  group_sum(rest, dev, lds);
+  const float shift = rest * inv, var = dev * inv - shift * shift;
   if (threadIdx.x == 0) {
     p.mean_out[sample * p.groups + g] = mean + shift;
     p.rstd_out[sample * p.groups + g] = 1.f / sqrtf((var > 0.f || var != var ? var : 0.f) + p.eps);
   }
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(NT) void norm_apply_kernel(NormP p) {
   // backwards through the jobs: what the statistics read last is still in the cache
-  const Place t = place(p, gridDim.x - 1 - blockIdx.x);
-  if (t.cnt <= 0) return;
+  const Place t = place<WHOLE>(p, gridDim.x - 1 - blockIdx.x);
+  if (!t.there) return;
   const Coef k(p, t.sample, t.c);
   float scale[V];
 #pragma unroll
@@ -219,13 +266,13 @@ __device__ __forceinline__ void slope4(const Coef& k, const Raw<T, V>& x, const 
   }
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(NT) void norm_sums_kernel(NormP p) {
   __shared__ float s_a[WAVES][64][V], s_b[WAVES][64][V];
-  const Place t = place(p, blockIdx.x);
+  const Place t = place<WHOLE>(p, blockIdx.x);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float a[V] = {}, b[V] = {};
-  if (t.cnt > 0) {
+  if (t.there) {
     const Coef k(p, t.sample, t.c);
     const T *x = (const T*)p.x + t.row0 * p.ldx + t.c, *dy = (const T*)p.dy + t.row0 * p.ldy + t.c;
     with_act(p.act, [&](auto act) {
@@ -251,47 +298,45 @@ __global__ __launch_bounds__(NT) void norm_sums_kernel(NormP p) {
       }
     });
   }
+  for (int d = p.lpr; d < 64; d *= 2)
+#pragma unroll
+    for (int e = 0; e < V; ++e) { a[e] += __shfl_xor(a[e], d); b[e] += __shfl_xor(b[e], d); }
 #pragma unroll
   for (int e = 0; e < V; ++e) { s_a[wave][lane][e] = a[e]; s_b[wave][lane][e] = b[e]; }
   __syncthreads();
-  if (threadIdx.x >= p.lpr || t.cnt <= 0) return;
-  for (int i = 1; i < WAVES * (64 / p.lpr); ++i) {
-    const int w = i / (64 / p.lpr), l = i % (64 / p.lpr) * p.lpr + lane;
+  if (threadIdx.x >= p.lpr || !t.there) return;
 #pragma unroll
-    for (int e = 0; e < V; ++e) { a[e] += s_a[w][l][e]; b[e] += s_b[w][l][e]; }
-  }
+  for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+    for (int e = 0; e < V; ++e) { a[e] += s_a[w][lane][e]; b[e] += s_b[w][lane][e]; }
   float* to = p.part + (t.sample * p.chunks + t.chunk) * 2 * p.c + t.c;
   store4(to, t.cnt, a);
   store4(to + p.c, t.cnt, b);
 }
 
 // Means over a group of gamma dv and of gamma dv xhat.
-__global__ __launch_bounds__(256) void norm_join_bwd_kernel(NormP p) {
-  __shared__ float lds[4];
+__global__ __launch_bounds__(JT) void norm_join_bwd_kernel(NormP p) {
+  __shared__ float lds[2][JT / 64];
   const int g = blockIdx.x % p.groups;
-  const long long sample = p.sample0 + blockIdx.x / p.groups, items = (long long)p.chunks * p.cg;
-  const float* part = p.part + sample * p.chunks * 2 * p.c + g * p.cg;
+  const long long sample = p.sample0 + blockIdx.x / p.groups;
   float a = 0.f, b = 0.f;
-  for (long long i = threadIdx.x; i < items; i += 256) {
-    const int chunk = (int)(i / p.cg), c = (int)(i - (long long)chunk * p.cg);
+  each_partial(p, p.part + sample * p.chunks * 2 * p.c + g * p.cg, [&](int, int c, float va, float vb) {
     const float gamma = p.gamma ? p.gamma[g * p.cg + c] : 1.f;
-    const float* at = part + (long long)chunk * 2 * p.c + c;
-    a = __builtin_fmaf(gamma, at[0], a);
-    b = __builtin_fmaf(gamma, at[p.c], b);
-  }
+    a = __builtin_fmaf(gamma, va, a);
+    b = __builtin_fmaf(gamma, vb, b);
+  });
+  group_sum(a, b, lds);
   const float inv = 1.f / ((float)p.s * (float)p.cg);
-  a = group_sum(a, lds) * inv;
-  b = group_sum(b, lds) * inv;
   if (threadIdx.x == 0) {
-    p.coef[(sample * p.groups + g) * 2] = a;
-    p.coef[(sample * p.groups + g) * 2 + 1] = b;
+    p.coef[(sample * p.groups + g) * 2] = a * inv;
+    p.coef[(sample * p.groups + g) * 2 + 1] = b * inv;
   }
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(NT) void norm_dx_kernel(NormP p) {
-  const Place t = place(p, gridDim.x - 1 - blockIdx.x);
-  if (t.cnt <= 0) return;
+  const Place t = place<WHOLE>(p, gridDim.x - 1 - blockIdx.x);
+  if (!t.there) return;
   const Coef k(p, t.sample, t.c);
   float m1[V], m2[V];
 #pragma unroll
@@ -348,6 +393,21 @@ __device__ __forceinline__ void slope8(const float (&ga)[W], const float (&be)[W
     dv[e] = dy.get(e) * slope;
   }
 }
+// A vector, or zeros.
+template <typename T>
+__device__ __forceinline__ Raw<T, W> vector(const T* p, bool there) {
+  Raw<T, W> r = {};
+  if (there) __builtin_memcpy(&r, p, sizeof(r));
+  return r;
+}
+// Makes the compiler compute anew what it has computed of these: kept, it takes twice their registers.
+template <typename T, int N>
+__device__ __forceinline__ void anew(Raw<T, W> (&t)[N]) {
+#pragma unroll
+  for (auto& v : t)
+#pragma unroll
+    for (unsigned& w : v.q) asm volatile("" : "+v"(w));
+}
 __device__ __forceinline__ void weights8(const NormP& p, int c, bool there, float (&ga)[W], float (&be)[W]) {
 #pragma unroll
   for (int e = 0; e < W; ++e) { ga[e] = 1.f; be[e] = 0.f; }
@@ -373,10 +433,10 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
     const bool there = row < q.samples;
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      const int cnt = there && vec(j) < nv ? W : 0;
-      nx[j] = raw<W>((const T*)p.x + row * p.ldx + vec(j) * W, cnt);
+      const bool cnt = there && vec(j) < nv;
+      nx[j] = vector((const T*)p.x + row * p.ldx + vec(j) * W, cnt);
       if constexpr (BWD) {
-        ndy[j] = raw<W>((const T*)p.dy + row * p.ldy + vec(j) * W, cnt);
+        ndy[j] = vector((const T*)p.dy + row * p.ldy + vec(j) * W, cnt);
         nmean[j] = cnt ? p.mean[row * p.groups + vec(j) / q.gv] : 0.f;
         nrstd[j] = cnt ? p.rstd[row * p.groups + vec(j) / q.gv] : 0.f;
       }
@@ -517,7 +577,7 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
 
 // Images: a sample's positions of one block of whole groups, K positions of a vector of channels a thread.
 template <typename T, int NT, int K, bool BWD>
-__global__ __launch_bounds__(NT) void norm_image_kernel(ResidentP q) {
+__global__ __launch_bounds__(NT, sizeof(T) * K <= 8 ? 4 : 2) void norm_image_kernel(ResidentP q) {
   __shared__ float s_part[2][NT], s_sum[2][64];
   __shared__ float s_chan[BWD ? 2 : 1][BWD ? W : 1][BWD ? NT : 1];
   const NormP& p = q.n;
@@ -532,18 +592,21 @@ __global__ __launch_bounds__(NT) void norm_image_kernel(ResidentP q) {
   weights8(p, c, there, ga, be);
   Raw<T, W> x[K], dy[BWD ? K : 1];
   float mean = 0.f, rstd = 0.f;
+  const int left = there ? (int)(p.s - pos) : 0;                  // positions from this thread's first on
+  auto have = [&](int j) { return j * lanes < left; };
+  {
+    const T *px = (const T*)p.x + (row0 + pos) * p.ldx + c, *pd = (const T*)p.dy + (row0 + pos) * p.ldy + c;
 #pragma unroll
-  for (int j = 0; j < K; ++j) {
-    const long long at = pos + (long long)j * lanes;
-    const int cnt = there && at < p.s ? W : 0;
-    x[j] = raw<W>((const T*)p.x + (row0 + at) * p.ldx + c, cnt);
-    if constexpr (BWD) dy[j] = raw<W>((const T*)p.dy + (row0 + at) * p.ldy + c, cnt);
+    for (int j = 0; j < K; ++j) {
+      x[j] = vector(px + j * (lanes * p.ldx), have(j));
+      if constexpr (BWD) dy[j] = vector(pd + j * (lanes * p.ldy), have(j));
+    }
   }
+  T* const out = (T*)p.out + (row0 + pos) * p.ldo + c;
   if (BWD && there) {
     mean = p.mean[sample * p.groups + (v0 + col) / q.gv];
     rstd = p.rstd[sample * p.groups + (v0 + col) / q.gv];
   }
-  auto have = [&](int j) { return there && pos + (long long)j * lanes < p.s; };
   auto join = [&](float& a, float& b) {                           // over the positions and a group's vectors
     __syncthreads();
     s_part[0][tid] = a;
@@ -600,7 +663,7 @@ __global__ __launch_bounds__(NT) void norm_image_kernel(ResidentP q) {
           float y[W], slope;
 #pragma unroll
           for (int e = 0; e < W; ++e) act_one<decltype(act)::value>(__builtin_fmaf((x[j].get(e) - mean) * rstd, ga[e], be[e]), y[e], slope);
-          store8((T*)p.out + (row0 + pos + (long long)j * lanes) * p.ldo + c, W, y);
+          store8(out + j * (lanes * p.ldo), W, y);
         }
     });
   } else {
@@ -616,6 +679,7 @@ __global__ __launch_bounds__(NT) void norm_image_kernel(ResidentP q) {
             db[e] += dv[e];
             da[e] = __builtin_fmaf(dv[e], hat[e], da[e]);
           }
+        __builtin_amdgcn_sched_barrier(0);
       }
     });
 #pragma unroll
@@ -634,6 +698,8 @@ __global__ __launch_bounds__(NT) void norm_image_kernel(ResidentP q) {
         p.part[(sample * 2 + which) * p.c + (v0 + v) * W + e] = t;
       }
     if (!p.out) return;
+    anew(x);
+    anew(dy);
     with_act(p.act, [&](auto act) {
 #pragma unroll
       for (int j = 0; j < K; ++j)
@@ -642,7 +708,8 @@ __global__ __launch_bounds__(NT) void norm_image_kernel(ResidentP q) {
           slope8<decltype(act)::value, T>(ga, be, mean, rstd, x[j], dy[j], hat, dv);
 #pragma unroll
           for (int e = 0; e < W; ++e) dv[e] = rstd * (__builtin_fmaf(ga[e], dv[e], -a * inv) - hat[e] * (b * inv));
-          store8((T*)p.out + (row0 + pos + (long long)j * lanes) * p.ldo + c, W, dv);
+          store8(out + j * (lanes * p.ldo), W, dv);
+          __builtin_amdgcn_sched_barrier(0);                      // one vector after the other: registers
         }
     });
   }
@@ -683,18 +750,16 @@ Split split_of(const lms_group_norm_desc* d) {
   for (t.lpr = 1; t.lpr < 64 && t.lpr * V < d->c;) t.lpr *= 2;
   t.cblocks = (d->c + t.lpr * V - 1) / (t.lpr * V);
   const long long step = (long long)WAVES * (64 / t.lpr) * U, most = (d->s + step - 1) / step;
-  const long long jobs = d->n * t.cblocks, want = jobs >= 2048 ? 1 : (2048 + jobs - 1) / (jobs ? jobs : 1);
+  const long long jobs = d->n * t.cblocks, want = jobs >= 1024 ? 1 : (1024 + jobs - 1) / (jobs ? jobs : 1);     // four work-groups on each compute unit
   const long long chunks = want < most ? want : most;
   t.chunk_rows = ((d->s + chunks - 1) / chunks + step - 1) / step * step;
   t.chunks = (int)((d->s + t.chunk_rows - 1) / t.chunk_rows);
   return t;
 }
-// Samples that are taken together.
-long long part_samples(const lms_group_norm_desc* d, const Split& t, int tensors) {
-  const long long bytes = d->s * d->c * (d->dtype == LMS_F32 ? 4 : 2) * tensors, fit = PART_BYTES / bytes > 0 ? PART_BYTES / bytes : 1;
-  const long long jobs = (long long)t.chunks * t.cblocks, groups = d->groups, each = jobs > groups ? jobs : groups, most = (1LL << 22) / each > 0 ? (1LL << 22) / each : 1;
-  const long long n = fit < most ? fit : most;
-  return n < d->n ? n : d->n;
+// Samples of one launch: 2^22 work-groups of 512 threads are a grid.
+long long part_samples(const lms_group_norm_desc* d, const Split& t) {
+  const long long jobs = (long long)t.chunks * t.cblocks, each = jobs > 2 * d->groups ? jobs : 2 * d->groups, most = (1LL << 22) / each > 0 ? (1LL << 22) / each : 1;
+  return most < d->n ? most : d->n;
 }
 
 // How a work-group holds samples, if it does: from the sizes and the type alone.
@@ -726,10 +791,12 @@ Held held_of(const lms_group_norm_desc* d) {
   h.block = groups * gv;
   h.blocks = (nv + h.block - 1) / h.block;
   if (h.block > 512) return Held{};
-  for (const int nt : {256, 512}) {
+  // the fewest threads whose four positions each hold the sample, else those whose eight do (which leaves half the waves: 64 x 196 x 1024 in bf16 backward 26.4 us with eight of 256 threads)
+  for (const int i : {0, 1, 2, 3}) {
+    const int nt = i % 2 ? 512 : 256;
     if (h.block > nt) continue;
     const long long k = (d->s + nt / h.block - 1) / (nt / h.block);
-    if (k > 8) continue;
+    if (k > (i < 2 ? 4 : 8)) continue;
     if (d->n * h.blocks > (1LL << 31) / nt) return Held{};
     h.kind = IMAGES;
     h.nt = nt;
@@ -790,15 +857,15 @@ hipError_t resident(const lms_group_norm_desc* d, const Held& h, const NormP& p,
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 hipError_t forward(const lms_group_norm_desc* d, const Split& t, NormP& p, hipStream_t s) {
-  const long long part = part_samples(d, t, 1);
+  const long long part = part_samples(d, t);
   for (p.sample0 = 0; p.sample0 < d->n; p.sample0 += part) {
     const long long take = d->n - p.sample0 < part ? d->n - p.sample0 : part;
     const dim3 jobs((unsigned)(take * t.chunks * t.cblocks));
-    hipLaunchKernelGGL(norm_stats_kernel<T>, jobs, dim3(NT), 0, s, p);
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(take * d->groups)), dim3(256), 0, s, p);
-    hipLaunchKernelGGL(norm_apply_kernel<T>, jobs, dim3(NT), 0, s, p);
+    hipLaunchKernelGGL((norm_stats_kernel<T, WHOLE>), jobs, dim3(NT), 0, s, p);
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(take * d->groups)), dim3(JT), 0, s, p);
+    hipLaunchKernelGGL((norm_apply_kernel<T, WHOLE>), jobs, dim3(NT), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -810,16 +877,16 @@ hipError_t sum_weights(const float* part, long long rows, int c, float* dgamma, 
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 hipError_t backward(const lms_group_norm_desc* d, const Split& t, NormP& p, float* dgamma, float* dbeta, hipStream_t s) {
-  const long long part = part_samples(d, t, 2);
+  const long long part = part_samples(d, t);
   for (p.sample0 = 0; p.sample0 < d->n; p.sample0 += part) {
     const long long take = d->n - p.sample0 < part ? d->n - p.sample0 : part;
     const dim3 jobs((unsigned)(take * t.chunks * t.cblocks));
-    hipLaunchKernelGGL(norm_sums_kernel<T>, jobs, dim3(NT), 0, s, p);
+    hipLaunchKernelGGL((norm_sums_kernel<T, WHOLE>), jobs, dim3(NT), 0, s, p);
     if (p.out) {
-      hipLaunchKernelGGL(norm_join_bwd_kernel, dim3((unsigned)(take * d->groups)), dim3(256), 0, s, p);
-      hipLaunchKernelGGL(norm_dx_kernel<T>, jobs, dim3(NT), 0, s, p);
+      hipLaunchKernelGGL(norm_join_bwd_kernel, dim3((unsigned)(take * d->groups)), dim3(JT), 0, s, p);
+      hipLaunchKernelGGL((norm_dx_kernel<T, WHOLE>), jobs, dim3(NT), 0, s, p);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -839,7 +906,7 @@ lms_status group_norm_workspace(const lms_group_norm_desc* d, int which, uint64_
   const Held h = held_of(d);
   if (d->n == 0) *bytes = 0;
   else if (h.kind != NOT_HELD) *bytes = 2 * stat_bytes(d) + (which == LMS_GROUP_NORM_BWD ? up256((uint64_t)h.rows * 2 * d->c * 4) : 0);
-  else if (which == LMS_GROUP_NORM_FWD) *bytes = part_bytes(d, t, part_samples(d, t, 1)) + 2 * stat_bytes(d);
+  else if (which == LMS_GROUP_NORM_FWD) *bytes = part_bytes(d, t, part_samples(d, t)) + 2 * stat_bytes(d);
   else *bytes = part_bytes(d, t, d->n) + 2 * stat_bytes(d);
   return LMS_OK;
 }
@@ -862,7 +929,9 @@ lms_status group_norm_fwd(const lms_group_norm_desc* d, const void* x, const flo
   hipStream_t s = (hipStream_t)stream;
   const Held h = held_of(d);
   if (h.kind != NOT_HELD) return done(what, d->dtype == LMS_F32 ? resident<float, false>(d, h, p, s) : resident<uint16_t, false>(d, h, p, s));
-  return done(what, d->dtype == LMS_F32 ? forward<float>(d, t, p, s) : forward<uint16_t>(d, t, p, s));
+  const bool f32 = d->dtype == LMS_F32;
+  if (d->c >= V) return done(what, f32 ? forward<float, true>(d, t, p, s) : forward<uint16_t, true>(d, t, p, s));
+  return done(what, f32 ? forward<float, false>(d, t, p, s) : forward<uint16_t, false>(d, t, p, s));
 }
 
 lms_status group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const void* x, const float* gamma, const float* beta, const float* mean, const float* rstd, void* dx,
@@ -884,7 +953,9 @@ lms_status group_norm_bwd(const lms_group_norm_desc* d, const void* dy, const vo
     const hipError_t e = d->dtype == LMS_F32 ? resident<float, true>(d, h, p, s) : resident<uint16_t, true>(d, h, p, s);
     return done(what, e != hipSuccess || !p.part ? e : sum_weights(p.part, h.rows, d->c, dgamma, dbeta, s));
   }
-  return done(what, d->dtype == LMS_F32 ? backward<float>(d, t, p, dgamma, dbeta, s) : backward<uint16_t>(d, t, p, dgamma, dbeta, s));
+  const bool f32 = d->dtype == LMS_F32;
+  if (d->c >= V) return done(what, f32 ? backward<float, true>(d, t, p, dgamma, dbeta, s) : backward<uint16_t, true>(d, t, p, dgamma, dbeta, s));
+  return done(what, f32 ? backward<float, false>(d, t, p, dgamma, dbeta, s) : backward<uint16_t, false>(d, t, p, dgamma, dbeta, s));
 }
 
 }  // namespace lms

@@ -81,6 +81,162 @@ __global__ __launch_bounds__(NT) void q8_rows_kernel(const T* x, long long ldx, 
   });
 }
 
+// ---- few rows ----
+//
+// Bound by reading the weights once.  A wave takes CW columns, its lanes consecutive 16 bytes of the reduction, and has eight loads of weights in flight before anything else happens; the rows of x lie
+// in LDS, 4-byte dot products go to whole sums of each lane, and the lanes meet by shuffles: whole numbers, in any order the same.  FUSED: every work-group quantises the rows itself,
+// while its weights are on their way, instead of waiting for another launch.
+constexpr int FT = 512, FEW_LDS = 65536;
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float v) {
+  float value, slope;
+  act_one<ACT>(v, value, slope);
+  return value;
+}
+
+template <typename T, int R, int CW, bool FUSED>
+__global__ __launch_bounds__(FT) void q8_few_kernel(DenseP p, const T* x, long long ldx, int k, int kp) {
+  constexpr int S = 8 / CW;                                       // loads of a column in flight
+  extern __shared__ __attribute__((aligned(16))) signed char s_x[];           // R rows of kp steps
+  __shared__ unsigned s_most[R][FT / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rows = (int)p.M;
+  const int waves = (int)gridDim.x * (FT / 64);
+  const signed char* wq = (const signed char*)p.b[0];
+  v4u w[CW][S];
+  auto ask = [&](int col, int k0) {
+#pragma unroll
+    for (int j = 0; j < CW; ++j)
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const int at = k0 + s * 1024 + lane * 16;
+        w[j][s] = v4u{0u, 0u, 0u, 0u};
+        if (col + j < p.N && at < kp) w[j][s] = *reinterpret_cast<const v4u*>(wq + (long long)(col + j) * kp + at);
+      }
+  };
+  int col = ((int)blockIdx.x * (FT / 64) + wave) * CW;
+  ask(col, 0);
+  float sx[R];
+  if constexpr (FUSED) {
+    constexpr int HELD = 2;
+    Raw<T, 8> held[R][HELD];
+    unsigned most[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int v = 0; v < HELD; ++v) {
+        const int c = (tid + v * FT) * 8;
+        held[r][v] = raw<8>(x + (r < rows ? r : 0) * ldx + c, c < k ? k - c : 0);
+      }
+    auto vec = [&](int r, int v) -> Raw<T, 8> {                   // any vector of a row
+      const int c = (tid + v * FT) * 8;
+      return raw<8>(x + (r < rows ? r : 0) * ldx + c, c < k ? k - c : 0);
+    };
+    auto largest = [](unsigned m, const Raw<T, 8>& q) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const unsigned b = magnitude_bits(q.get(e));
+        m = m > b ? m : b;
+      }
+      return m;
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      most[r] = 0;
+#pragma unroll
+      for (int v = 0; v < HELD; ++v) most[r] = largest(most[r], held[r][v]);
+      for (int v = HELD; v * FT * 8 < kp; ++v) most[r] = largest(most[r], vec(r, v));
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) {
+        const unsigned m = __shfl_xor(most[r], d);
+        most[r] = most[r] > m ? most[r] : m;
+      }
+      if (lane == 0) s_most[r][wave] = most[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int i = 0; i < FT / 64; ++i) most[r] = most[r] > s_most[r][i] ? most[r] : s_most[r][i];
+      sx[r] = scale_of(most[r]);
+      const float top = __uint_as_float(most[r]);
+      const bool some = steps(most[r]);
+      auto put = [&](int v, const Raw<T, 8>& d) {
+        const int c = (tid + v * FT) * 8;
+        if (c >= kp) return;
+        unsigned q[2] = {0u, 0u};
+        if (some)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) q[e >> 2] |= (unsigned)(step_of<T>(d.get(e), top) & 255) << (8 * (e & 3));
+        __builtin_memcpy(s_x + r * kp + c, q, 8);
+      };
+#pragma unroll
+      for (int v = 0; v < HELD; ++v) put(v, held[r][v]);
+      for (int v = HELD; v * FT * 8 < kp; ++v) put(v, vec(r, v));
+    }
+  } else {
+    const signed char* xq = (const signed char*)p.a[0];
+    for (int i = tid * 16; i < R * kp; i += FT * 16) {
+      const int r = i / kp;
+      *reinterpret_cast<v4u*>(s_x + i) = *reinterpret_cast<const v4u*>(xq + (long long)(r < rows ? i : i - r * kp));      // rows that are not there: the first
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) sx[r] = p.sx[r < rows ? r : 0];
+  }
+  __syncthreads();
+  while (col < p.N) {                                             // uniform in a wave
+    int acc[CW][R] = {};
+    for (int k0 = 0;;) {
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const int at = k0 + s * 1024 + lane * 16;
+        if (at < kp)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const v4u d = *reinterpret_cast<const v4u*>(s_x + r * kp + at);
+#pragma unroll
+            for (int j = 0; j < CW; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[j][r] = __builtin_amdgcn_sdot4((int)d[i], (int)w[j][s][i], acc[j][r], false);
+          }
+      }
+      k0 += S * 1024;
+      if (k0 >= kp) break;
+      ask(col, k0);
+    }
+    const int done = col;
+    col += waves * CW;
+    if (col < p.N) ask(col, 0);
+    // output (r, j) is lane r CW + j's
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < CW; ++j)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        int v = acc[j][r];
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+        mine = lane == r * CW + j ? v : mine;
+      }
+    const int r = lane / CW, n = done + lane % CW;
+    if (lane < rows * CW && n < p.N) {
+      float s = sx[0];
+#pragma unroll
+      for (int i = 1; i < R; ++i) s = r == i ? sx[i] : s;
+      float v = (float)mine * (s * p.sw[n]);
+      if (p.bias) v += p.bias[n];
+      with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
+      if constexpr (sizeof(T) == 2) {
+        if (p.res) v += bf2f(((const T*)p.res)[r * p.ldr + n]);
+        ((T*)p.out[0])[r * p.ldo + n] = f2bf(v);
+      } else {
+        if (p.res) v += ((const T*)p.res)[r * p.ldr + n];
+        ((T*)p.out[0])[r * p.ldo + n] = v;
+      }
+    }
+  }
+}
+
 // 64 columns of the weights: their scales, and the steps turned into rows.
 template <typename T>
 __global__ __launch_bounds__(256) void q8_weight_kernel(const T* w, long long ldw, int n, int k, int kp, signed char* wq, float* sw) {
@@ -152,10 +308,43 @@ hipError_t quantise(const lms_linear_q8_desc* d, const T* x, signed char* xq, fl
   return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
 
+// Up to eight rows that fit the LDS; up to two are quantised there too.
+int few_rows(const lms_linear_q8_desc* d) {
+  const int r = d->m <= 2 ? (int)d->m : d->m <= 4 ? 4 : 8;
+  return d->m >= 1 && d->m <= 8 && (long long)r * pitch(d) <= FEW_LDS ? r : 0;
+}
+bool few_fused(const lms_linear_q8_desc* d) { return d->m <= 2 && few_rows(d); }
+
+template <typename T, int R, bool FUSED>
+hipError_t few(const lms_linear_q8_desc* d, DenseP& p, const T* x, hipStream_t s) {
+  const int kp = pitch(d), steps = (kp + 1023) / 1024;
+  auto go = [&](auto cw) {
+    constexpr int CW = decltype(cw)::value;
+    const long long need = ((long long)d->n + CW * (FT / 64) - 1) / (CW * (FT / 64));
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(q8_few_kernel<T, R, CW, FUSED>), hipFuncAttributeMaxDynamicSharedMemorySize, FEW_LDS);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL((q8_few_kernel<T, R, CW, FUSED>), dim3((unsigned)(need < 512 ? need : 512)), dim3(FT), R * kp, s, p, x, d->ldx ? d->ldx : (long long)d->k, d->k, kp);
+    return hipGetLastError();
+  };
+  if (steps >= 8) return go(std::integral_constant<int, 1>{});
+  if (steps >= 3) return go(std::integral_constant<int, 2>{});
+  return go(std::integral_constant<int, 4>{});
+}
+template <typename T>
+hipError_t few_product(const lms_linear_q8_desc* d, DenseP& p, const void* x, hipStream_t s) {
+  const T* t = (const T*)x;
+  switch (few_rows(d)) {
+    case 1: return x ? few<T, 1, true>(d, p, t, s) : few<T, 1, false>(d, p, t, s);
+    case 2: return x ? few<T, 2, true>(d, p, t, s) : few<T, 2, false>(d, p, t, s);
+    case 4: return few<T, 4, false>(d, p, t, s);
+    default: return few<T, 8, false>(d, p, t, s);
+  }
+}
+
 uint64_t rows_bytes(const lms_linear_q8_desc* d) { return up256((uint64_t)d->m * pitch(d)); }
 uint64_t scale_bytes(const lms_linear_q8_desc* d) { return up256((uint64_t)d->m * 4); }
 int mode_of(const lms_linear_q8_desc* d) { return d->dtype == LMS_F32 ? DENSE_Q8_F32 : DENSE_Q8; }
-uint64_t product_bytes(const lms_linear_q8_desc* d) { return up256(dense_bf16_ws(mode_of(d), d->m, d->n, pitch(d) / 2, 1, 1)); }
+uint64_t product_bytes(const lms_linear_q8_desc* d) { return few_rows(d) ? 0 : up256(dense_bf16_ws(mode_of(d), d->m, d->n, pitch(d) / 2, 1, 1)); }
 
 lms_status check(const char* what, const lms_linear_q8_desc* d) {
   NEED(d->m >= 0 && d->n >= 1 && d->k >= 1, "%s: rows must be >= 0, widths >= 1", what);
@@ -179,7 +368,8 @@ lms_status aligned(const char* what, const lms_linear_q8_desc* d, std::initializ
   return LMS_OK;
 }
 
-hipError_t product(const lms_linear_q8_desc* d, const void* xq, const float* sx, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* ws, hipStream_t s) {
+// x: the rows themselves where few_fused, then no xq
+hipError_t product(const lms_linear_q8_desc* d, const void* x, const void* xq, const float* sx, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* ws, hipStream_t s) {
   DenseP p{};
   p.a[0] = xq; p.b[0] = wq; p.out[0] = y;
   p.sx = sx; p.sw = sw; p.bias = bias; p.res = res;
@@ -189,6 +379,7 @@ hipError_t product(const lms_linear_q8_desc* d, const void* xq, const float* sx,
   p.ldr = d->ldr ? d->ldr : d->n;
   p.segs = 1; p.srcs = 1; p.act = d->act;
   p.part = (float*)ws;
+  if (few_rows(d)) return d->dtype == LMS_F32 ? few_product<float>(d, p, x, s) : few_product<uint16_t>(d, p, x, s);
   return dense_bf16(mode_of(d), p, s);
 }
 
@@ -233,7 +424,7 @@ lms_status linear_q8_product(const lms_linear_q8_desc* d, const void* xq, const 
   NEED(res != y || (d->ldr ? d->ldr : d->n) == (d->ldy ? d->ldy : d->n), "%s: res may be y only with the same pitch", what);
   if (d->m == 0) return LMS_OK;
   NEED(ws || product_bytes(d) == 0, "%s: workspace of %llu bytes required", what, (unsigned long long)product_bytes(d));
-  return done(what, product(d, xq, sx, wq, sw, bias, res, y, ws, (hipStream_t)stream));
+  return done(what, product(d, nullptr, xq, sx, wq, sw, bias, res, y, ws, (hipStream_t)stream));
 }
 
 lms_status linear_q8_fwd(const lms_linear_q8_desc* d, const void* x, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* ws, void* stream) {
@@ -246,8 +437,9 @@ lms_status linear_q8_fwd(const lms_linear_q8_desc* d, const void* x, const void*
   char* at = (char*)ws;
   float* sx = (float*)(at + rows_bytes(d));
   hipStream_t s = (hipStream_t)stream;
+  if (few_fused(d)) return done(what, product(d, x, nullptr, nullptr, wq, sw, bias, res, y, nullptr, s));
   hipError_t e = d->dtype == LMS_F32 ? quantise<float>(d, (const float*)x, (signed char*)at, sx, s) : quantise<uint16_t>(d, (const uint16_t*)x, (signed char*)at, sx, s);
-  if (e == hipSuccess) e = product(d, at, sx, wq, sw, bias, res, y, at + rows_bytes(d) + scale_bytes(d), s);
+  if (e == hipSuccess) e = product(d, nullptr, at, sx, wq, sw, bias, res, y, at + rows_bytes(d) + scale_bytes(d), s);
   return done(what, e);
 }
 

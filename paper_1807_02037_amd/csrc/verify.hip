@@ -1,6 +1,6 @@
 // Verification of drafted tokens (include/lms.h has the rule).
 //
-// Two launches.  The first sums, for each request, the chunks of the one distribution that its next token comes from; every work-group finds that out by itself, from a few reads of the drafts.
+// Two launches.  The first sums, for each request, the chunks of the one distribution that its next token comes from, a wave a chunk; every wave finds that distribution by itself, from a few reads of the drafts.
 // The second picks the chunk in which the running sum passes the drawn share of the whole, and the class in it.  Differences and sums are fp64: the token is that of exact sums but
 // where the drawn number lies within some 2^-50 of a border, and whole numbers have no tolerance.
 #include <hip/hip_runtime.h>
@@ -14,7 +14,8 @@ namespace lms {
 
 namespace {
 
-constexpr int NT = 256, MAX_CHUNKS = 64, STEP = NT * 4;            // classes of a work-group at a time
+constexpr int NT = 256, STEP = NT * 4;  // classes of a work-group at a time, and of a chunk at least
+constexpr int MAX_CHUNKS = 256;        // of a request: four a lane
 
 struct VerifyP {
   const float *p, *q;
@@ -45,11 +46,8 @@ __device__ __forceinline__ int accepted_drafts(const VerifyP& p, int b, int& cou
   return count;
 }
 
-// Four classes from c on: max(p - q, 0) where there is a q, and p where it is above 0; nothing beyond the last, nothing for NaN.
-__device__ __forceinline__ void masses(const VerifyP& p, const float* pr, const float* qr, int c, double (&r)[4], double (&w)[4]) {
-  float a[4], b[4] = {0.f, 0.f, 0.f, 0.f};
-  load4(pr + c, p.classes - c, a);
-  if (qr) load4(qr + c, p.classes - c, b);
+// Of four classes: max(p - q, 0), and p where it is above 0; nothing for NaN.
+__device__ __forceinline__ void masses(const float (&a)[4], const float (&b)[4], double (&r)[4], double (&w)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const double d = (double)a[e] - (double)b[e];
@@ -59,32 +57,42 @@ __device__ __forceinline__ void masses(const VerifyP& p, const float* pr, const 
 }
 
 __global__ __launch_bounds__(NT) void verify_sums_kernel(VerifyP p) {
-  __shared__ double lds[NT / 64][2];
-  const int b = blockIdx.x / p.chunks, chunk = blockIdx.x - b * p.chunks;
+  const int lane = threadIdx.x & 63;
+  const long long job = (long long)blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (job >= (long long)p.requests * p.chunks) return;
+  const int b = (int)(job / p.chunks), chunk = (int)(job - (long long)b * p.chunks);
   int count;
   const int at = accepted_drafts(p, b, count);
   const float* pr = p.p + ((long long)b * (p.drafts + 1) + at) * p.ldp;
   const float* qr = at < count ? p.q + ((long long)b * p.drafts + at) * p.ldq : nullptr;
   const int begin = chunk * p.chunk, end = begin + p.chunk < p.classes ? begin + p.chunk : p.classes;
   double sr = 0.0, sp = 0.0;
-  for (int c = begin + (int)threadIdx.x * 4; c < end; c += STEP) {
-    double r[4], w[4];
-    masses(p, pr, qr, c, r, w);
-    sr += (r[0] + r[1]) + (r[2] + r[3]);
-    sp += (w[0] + w[1]) + (w[2] + w[3]);
+  for (int c0 = begin; c0 < end; c0 += STEP) {
+    float a[4][4], q[4][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int c = c0 + u * 256 + lane * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[u][e] = q[u][e] = 0.f;
+      if (c < end) load4(pr + c, p.classes - c, a[u]);
+      if (c < end && qr) load4(qr + c, p.classes - c, q[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      double r[4], w[4];
+      masses(a[u], q[u], r, w);
+      sr += (r[0] + r[1]) + (r[2] + r[3]);
+      sp += (w[0] + w[1]) + (w[2] + w[3]);
+    }
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) {
     sr += __shfl_xor(sr, d);
     sp += __shfl_xor(sp, d);
   }
-  if ((threadIdx.x & 63) == 0) { lds[threadIdx.x >> 6][0] = sr; lds[threadIdx.x >> 6][1] = sp; }
-  __syncthreads();
-  if (threadIdx.x < 2) {
-    double t = lds[0][threadIdx.x];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) t += lds[w][threadIdx.x];
-    p.sums[(long long)blockIdx.x * 2 + threadIdx.x] = t;
+  if (lane == 0) {
+    p.sums[job * 2] = sr;
+    p.sums[job * 2 + 1] = sp;
   }
 }
 
@@ -107,52 +115,82 @@ __global__ __launch_bounds__(NT) void verify_pick_kernel(VerifyP p) {
   const int at = accepted_drafts(p, b, count);
   const float* pr = p.p + ((long long)b * (p.drafts + 1) + at) * p.ldp;
   const float* qr = at < count ? p.q + ((long long)b * p.drafts + at) * p.ldq : nullptr;
-  // the chunk
-  const double sr = lane < p.chunks ? p.sums[((long long)b * p.chunks + lane) * 2] : 0.0, sp = lane < p.chunks ? p.sums[((long long)b * p.chunks + lane) * 2 + 1] : 0.0;
-  const bool rest = __ballot(sr > 0.0) != 0;                      // else p, which has no more than q anywhere, itself
-  const double mine = rest ? sr : sp, upto = running(mine), whole = __shfl(upto, 63), target = (double)p.v[b] * whole;
-  const unsigned long long any = __ballot(mine > 0.0), beyond = __ballot(mine > 0.0 && upto > target);
+  // the chunk: lane l has four, from 4 l on
+  constexpr int NONE = 0x7fffffff;
+  double er[4], ep[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool there = lane * 4 + e < p.chunks;
+    const double* from = p.sums + ((long long)b * p.chunks + lane * 4 + e) * 2;
+    er[e] = there ? from[0] : 0.0;
+    ep[e] = there ? from[1] : 0.0;
+  }
+  const bool rest = __ballot(er[0] > 0.0 || er[1] > 0.0 || er[2] > 0.0 || er[3] > 0.0) != 0;      // else p, which has no more than q anywhere, itself
+#pragma unroll
+  for (int e = 0; e < 4; ++e) er[e] = rest ? er[e] : ep[e];
+  const double four = (er[0] + er[1]) + (er[2] + er[3]), upto = running(four), whole = __shfl(upto, 63), target = (double)p.v[b] * whole;
+  double before[4], sofar = upto - four;
+  int chunk = NONE, high = -1;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    before[e] = sofar;
+    sofar += er[e];
+    if (er[e] > 0.0) {
+      high = lane * 4 + e;
+      if (sofar > target && chunk == NONE) chunk = lane * 4 + e;
+    }
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const int f = __shfl_xor(chunk, d), h = __shfl_xor(high, d);
+    chunk = chunk < f ? chunk : f;
+    high = high > h ? high : h;
+  }
   int token = -1;
-  if (any) {                                                      // else there is no class to take
-    const int chunk = beyond ? __builtin_ctzll(beyond) : 63 - __builtin_clzll(any);
-    double base = __shfl(upto - mine, chunk);
+  if (high >= 0) {                                                // else there is no class to take
+    chunk = __builtin_amdgcn_readfirstlane(chunk != NONE ? chunk : high);
+    const double pick = chunk % 4 == 0 ? before[0] : chunk % 4 == 1 ? before[1] : chunk % 4 == 2 ? before[2] : before[3];
+    double base = __shfl(pick, chunk / 4);
     const int begin = chunk * p.chunk, end = begin + p.chunk < p.classes ? begin + p.chunk : p.classes;
     int last = -1;                                                // the last class with a share so far
     for (int c0 = begin; c0 < end && token < 0; c0 += STEP) {
       const int c = c0 + (int)threadIdx.x * 4;
-      double r[4] = {0.0, 0.0, 0.0, 0.0}, w[4] = {0.0, 0.0, 0.0, 0.0};
-      if (c < end) masses(p, pr, qr, c, r, w);
+      float a[4] = {0.f, 0.f, 0.f, 0.f}, q[4] = {0.f, 0.f, 0.f, 0.f};
+      if (c < end) load4(pr + c, p.classes - c, a);
+      if (c < end && qr) load4(qr + c, p.classes - c, q);
+      double r[4], w[4];
+      masses(a, q, r, w);
 #pragma unroll
       for (int e = 0; e < 4; ++e) r[e] = rest ? r[e] : w[e];
-      const double own = (r[0] + r[1]) + (r[2] + r[3]), before = running(own);
+      const double own = (r[0] + r[1]) + (r[2] + r[3]), wave_upto = running(own);
       __syncthreads();
-      if (lane == 63) lds[wave] = before;
+      if (lane == 63) lds[wave] = wave_upto;
       __syncthreads();
-      double sum = base + (before - own);
+      double sum = base + (wave_upto - own);
       for (int i = 0; i < wave; ++i) sum += lds[i];
-      int first = 0x7fffffff, high = -1;
+      int first = NONE, top = -1;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         sum += r[e];
         if (r[e] > 0.0) {
-          high = c + e;
-          if (sum > target && first == 0x7fffffff) first = c + e;
+          top = c + e;
+          if (sum > target && first == NONE) first = c + e;
         }
       }
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) {
-        const int f = __shfl_xor(first, d), h = __shfl_xor(high, d);
+        const int f = __shfl_xor(first, d), h = __shfl_xor(top, d);
         first = first < f ? first : f;
-        high = high > h ? high : h;
+        top = top > h ? top : h;
       }
-      if (lane == 0) { s_first[wave] = first; s_last[wave] = high; }
+      if (lane == 0) { s_first[wave] = first; s_last[wave] = top; }
       __syncthreads();
       for (int i = 0; i < NT / 64; ++i) {
         first = first < s_first[i] ? first : s_first[i];
         last = last > s_last[i] ? last : s_last[i];
         base += lds[i];
       }
-      if (first != 0x7fffffff) token = first;
+      if (first != NONE) token = first;
     }
     if (token < 0) token = last;
   }
@@ -162,8 +200,7 @@ __global__ __launch_bounds__(NT) void verify_pick_kernel(VerifyP p) {
 }
 
 void chunks_of(const lms_verify_desc* d, int& chunks, int& chunk) {
-  const int steps = (d->classes + STEP - 1) / STEP, want = d->requests >= 512 ? 1 : (512 + d->requests - 1) / (d->requests ? d->requests : 1);
-  const int most = want < MAX_CHUNKS ? want : MAX_CHUNKS, per = (steps + most - 1) / most;
+  const int steps = (d->classes + STEP - 1) / STEP, per = (steps + MAX_CHUNKS - 1) / MAX_CHUNKS;
   chunk = per * STEP;
   chunks = (steps + per - 1) / per;
 }
@@ -172,6 +209,7 @@ lms_status check(const char* what, const lms_verify_desc* d) {
   NEED(d->requests >= 0 && d->drafts >= 0 && d->classes >= 1, "%s: requests and drafts must be >= 0, classes >= 1", what);
   NEED(d->requests <= 1 << 20 && d->drafts <= 1 << 10, "%s: more than 2^20 requests, or 2^10 drafts", what);
   NEED(d->classes <= 1 << 30, "%s: more than 2^30 classes", what);
+  NEED((long long)d->requests * d->classes <= 1LL << 34, "%s: requests times classes above 2^34", what);
   const long long most = 1LL << 40;
   NEED((d->ldp == 0 || (d->ldp >= d->classes && d->ldp <= most)) && (d->ldq == 0 || (d->ldq >= d->classes && d->ldq <= most)),
        "%s: a row pitch is shorter than the row, or above 2^40", what);
@@ -205,7 +243,7 @@ lms_status verify(const lms_verify_desc* d, const float* pr, const float* q, con
   p.requests = d->requests; p.drafts = d->drafts; p.classes = d->classes;
   chunks_of(d, p.chunks, p.chunk);
   hipStream_t s = (hipStream_t)stream;
-  hipLaunchKernelGGL(verify_sums_kernel, dim3((unsigned)(d->requests * p.chunks)), dim3(NT), 0, s, p);
+  hipLaunchKernelGGL(verify_sums_kernel, dim3((unsigned)(((long long)d->requests * p.chunks + NT / 64 - 1) / (NT / 64))), dim3(NT), 0, s, p);
   hipLaunchKernelGGL(verify_pick_kernel, dim3((unsigned)d->requests), dim3(NT), 0, s, p);
   return done(what, hipGetLastError());
 }

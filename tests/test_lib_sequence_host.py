@@ -135,7 +135,7 @@ def verify(**kw):
 
 
 @pytest.mark.parametrize("kw,match", [(dict(requests=-1), "requests"), (dict(drafts=-1), "drafts"), (dict(classes=0), "classes"), (dict(requests=(1 << 20) + 1), "requests"),
-                                      (dict(drafts=1025), "drafts"), (dict(classes=(1 << 30) + 1), "classes"), (dict(ldp=49), "pitch"), (dict(ldq=49), "pitch"),
+                                      (dict(drafts=1025), "drafts"), (dict(classes=(1 << 30) + 1), "classes"), (dict(ldp=49), "pitch"), (dict(ldq=49), "pitch"), (dict(requests=1 << 20, classes=1 << 15), "requests times classes"),
                                       (dict(ldq=1 << 41), "pitch")])
 def test_verify_descriptors(kw, match):
     d = verify(**kw)
