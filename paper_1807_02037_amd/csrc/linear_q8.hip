@@ -237,52 +237,96 @@ __global__ __launch_bounds__(FT) void q8_few_kernel(DenseP p, const T* x, long l
   }
 }
 
-// 64 columns of the weights: their scales, and the steps turned into rows.
+// ---- weights, laid out once ----
+//
+// Columns' largest magnitudes meet in sw as bits, by a maximum whose order does not matter; then tiles are turned through LDS; then the bits become scales.
+__global__ __launch_bounds__(256) void q8_clear_kernel(unsigned* most, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) most[i] = 0;
+}
+__global__ __launch_bounds__(256) void q8_scales_kernel(float* sw, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) sw[i] = scale_of(__float_as_uint(sw[i]));
+}
+
+constexpr int WROWS = 256;             // of the reduction, a work-group
+constexpr int WBLOCKS = 1 << 14;       // blocks of columns of a launch
+
 template <typename T>
-__global__ __launch_bounds__(256) void q8_weight_kernel(const T* w, long long ldw, int n, int k, int kp, signed char* wq, float* sw) {
-  __shared__ unsigned s_most[4][64];
-  __shared__ int s_q[64][65];
-  const int col = threadIdx.x & 63, way = threadIdx.x >> 6, j = blockIdx.x * 64 + col;
-  unsigned most = 0;
-  if (j < n)
-    for (int r = way; r < k; r += 4) {
-      float v;
-      if constexpr (sizeof(T) == 2) v = bf2f(w[r * ldw + j]);
-      else v = w[r * ldw + j];
-      const unsigned m = magnitude_bits(v);
-      most = most > m ? most : m;
-    }
-  s_most[way][col] = most;
-  __syncthreads();
+__device__ __forceinline__ float element(const T* p) {
+  if constexpr (sizeof(T) == 2) return bf2f(*p);
+  else return *p;
+}
+// 256 columns, eight a thread
+template <typename T>
+__global__ __launch_bounds__(256) void q8_columns_kernel(const T* w, long long ldw, int n, int k, unsigned* sw, int block0) {
+  __shared__ unsigned s_most[8][256];
+  const int c = (threadIdx.x & 31) * 8, way = threadIdx.x >> 5, j = (block0 + (int)blockIdx.x) * 256 + c, r0 = blockIdx.y * WROWS, cnt = n - j;
+  unsigned most[8] = {};
+  if (cnt > 0)
+#pragma unroll 4
+    for (int r = r0 + way; r < r0 + WROWS; r += 8) {
+      const Raw<T, 8> v = raw<8>(w + (long long)(r < k ? r : r0) * ldw + j, cnt);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) most = most > s_most[i][col] ? most : s_most[i][col];
-  if (way == 0 && j < n) sw[j] = scale_of(most);
-  const float top = __uint_as_float(most);
-  const bool some = steps(most) && j < n;
-  for (int r0 = 0; r0 < kp; r0 += 64) {
-    __syncthreads();
-    for (int r = way; r < 64; r += 4) {
-      int q = 0;
-      if (some && r0 + r < k) {
-        float v;
-        if constexpr (sizeof(T) == 2) v = bf2f(w[(r0 + r) * ldw + j]);
-        else v = w[(r0 + r) * ldw + j];
-        q = step_of<T>(v, top);
+      for (int e = 0; e < 8; ++e) {
+        const unsigned m = magnitude_bits(v.get(e));
+        most[e] = most[e] > m ? most[e] : m;
       }
-      s_q[r][col] = q;
     }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s_most[way][c + e] = most[e];
+  __syncthreads();
+  const int col = (block0 + (int)blockIdx.x) * 256 + threadIdx.x;
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = m > s_most[i][threadIdx.x] ? m : s_most[i][threadIdx.x];
+  if (col < n) atomicMax(sw + col, m);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void q8_turn_kernel(const T* w, long long ldw, int n, int k, int kp, signed char* wq, const unsigned* sw, int block0) {
+  __shared__ int s_q[64][65];
+  const int c0 = (block0 + (int)blockIdx.x) * 64, col = threadIdx.x & 63, way = threadIdx.x >> 6, j = c0 + col;
+  const unsigned most = j < n ? sw[j] : 0u;
+  const float top = __uint_as_float(most);
+  const bool some = steps(most);
+  for (int r0 = blockIdx.y * WROWS; r0 < (int)(blockIdx.y + 1) * WROWS && r0 < kp; r0 += 64) {
+    __syncthreads();
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = r0 + way + 4 * i;
+      v[i] = some && r < k ? element(w + (long long)r * ldw + j) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s_q[way + 4 * i][col] = some ? step_of<T>(v[i], top) : 0;
     __syncthreads();
     const int row = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;          // 16 steps of one column
-    if (blockIdx.x * 64 + row < n && r0 + part < kp) {
+    if (c0 + row < n && r0 + part < kp) {
       unsigned q[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
       for (int e = 0; e < 16; ++e) q[e >> 2] |= (unsigned)(s_q[part + e][row] & 255) << (8 * (e & 3));
-      __builtin_memcpy(wq + (long long)(blockIdx.x * 64 + row) * kp + r0 + part, q, 16);
+      __builtin_memcpy(wq + (long long)(c0 + row) * kp + r0 + part, q, 16);
     }
   }
 }
 
 int pitch(const lms_linear_q8_desc* d) { return (d->k + 15) / 16 * 16; }
+
+template <typename T>
+hipError_t lay_out(const lms_linear_q8_desc* d, const T* w, signed char* wq, float* sw, hipStream_t s) {
+  const int kp = pitch(d), n = d->n, deep = (kp + WROWS - 1) / WROWS;
+  const long long ldw = d->ldw ? d->ldw : d->n;
+  const dim3 flat((unsigned)((n + 255) / 256));
+  auto blocks = [&](int width, auto&& launch) {
+    const int all = (n + width - 1) / width;
+    for (int b = 0; b < all; b += WBLOCKS) launch(dim3((unsigned)(all - b < WBLOCKS ? all - b : WBLOCKS), (unsigned)deep), b);
+  };
+  hipLaunchKernelGGL(q8_clear_kernel, flat, dim3(256), 0, s, (unsigned*)sw, n);
+  blocks(256, [&](dim3 grid, int b) { hipLaunchKernelGGL(q8_columns_kernel<T>, grid, dim3(256), 0, s, w, ldw, n, d->k, (unsigned*)sw, b); });
+  blocks(64, [&](dim3 grid, int b) { hipLaunchKernelGGL(q8_turn_kernel<T>, grid, dim3(256), 0, s, w, ldw, n, d->k, kp, wq, (const unsigned*)sw, b); });
+  hipLaunchKernelGGL(q8_scales_kernel, flat, dim3(256), 0, s, sw, n);
+  return hipGetLastError();
+}
 
 template <typename T>
 hipError_t quantise(const lms_linear_q8_desc* d, const T* x, signed char* xq, float* sx, hipStream_t s) {
@@ -400,12 +444,8 @@ lms_status linear_q8_weight(const lms_linear_q8_desc* d, const void* w, void* wq
   const char* what = "lms_linear_q8_weight";
   if (const lms_status st = check(what, d)) return st;
   if (const lms_status st = aligned(what, d, {w}, {sw}, {wq})) return st;
-  const dim3 grid((unsigned)((d->n + 63) / 64));
-  const long long ldw = d->ldw ? d->ldw : d->n;
   hipStream_t s = (hipStream_t)stream;
-  if (d->dtype == LMS_F32) hipLaunchKernelGGL(q8_weight_kernel<float>, grid, dim3(256), 0, s, (const float*)w, ldw, d->n, d->k, pitch(d), (signed char*)wq, sw);
-  else hipLaunchKernelGGL(q8_weight_kernel<uint16_t>, grid, dim3(256), 0, s, (const uint16_t*)w, ldw, d->n, d->k, pitch(d), (signed char*)wq, sw);
-  return done(what, hipGetLastError());
+  return done(what, d->dtype == LMS_F32 ? lay_out<float>(d, (const float*)w, (signed char*)wq, sw, s) : lay_out<uint16_t>(d, (const uint16_t*)w, (signed char*)wq, sw, s));
 }
 
 lms_status linear_q8_rows(const lms_linear_q8_desc* d, const void* x, void* xq, float* sx, void* stream) {
