@@ -1,0 +1,255 @@
+"""A student that reads sequences, is distilled from a teacher, and drafts tokens that the teacher verifies: the sequence operators of the library used together.
+
+    python -m paper_1807_02037_amd.sequence_student [--steps 60] [--width 256] [--classes 1000] [--drafts 4] [--tokens 24]
+
+A position's embedding e passes a gated recurrence over its sequence, a group normalisation, a projection with a residual sum and a head over the vocabulary.  Everything but
+the embedding lookup, the softmax over the logits and the update of the weights runs in liblms.so:
+
+    x, g, o = columns of e wp + bp      lms_linear_fwd
+    h = recurrence of x, g, o           lms_recur_fwd; for single tokens lms_recur_step
+    n = group norm of h                 lms_group_norm_fwd
+    r = n wd + bd + e,  z = r wh        lms_linear_fwd; while answering lms_linear_q8_fwd
+    loss, dz and back                   lms_distill_loss_grad, lms_linear_bwd, lms_group_norm_bwd, lms_recur_bwd
+    drafts against the teacher          lms_verify
+
+While answering, each request has a slot with its state; a run of drafted tokens goes through in one call, and only the accepted ones are taken into the states."""
+import argparse
+
+import torch
+
+from . import _lib as A
+from . import api as L
+from .student import _bf16, _expect
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+class SequenceStudent:
+    """Weights, the buffers of a training batch of `rows` positions in at most `seqs` sequences, and the states of `slots` requests."""
+
+    GROUPS = 4
+
+    def __init__(self, rows, seqs, width, classes, top, slots=1, temperature=2.0, seed=0):
+        if width % self.GROUPS:
+            raise ValueError(f"width: a multiple of {self.GROUPS} is needed, not {width}")
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.rows, self.seqs, self.width, self.classes, self.top, self.slots = rows, seqs, width, classes, top, slots
+        self.embed = _bf16(classes, width, scale=1.0, gen=gen)
+        self.weights = {"wp": _bf16(width, 3 * width, scale=width ** -0.5, gen=gen), "wd": _bf16(width, width, scale=width ** -0.5, gen=gen),
+                        "wh": _bf16(width, classes, scale=width ** -0.5, gen=gen)}
+        self.params = {"bp": torch.zeros(3 * width, device="cuda"), "bd": torch.zeros(width, device="cuda"), "gamma": torch.ones(width, device="cuda"),
+                       "beta": torch.zeros(width, device="cuda")}
+        self.params["bp"][width:2 * width] = 1.0                    # states are remembered at first
+        self.grads = {k: torch.empty(v.shape, device="cuda") for k, v in {**self.weights, **self.params}.items()}
+        self.proj, self.down, self.head = self._linears(rows)
+        self.recur, self.norm = self._blocks(rows, seqs)
+        self.loss_desc = L.distill_desc(rows, classes, top, temperature=temperature, scale=1.0 / rows)
+
+        def act(cols):
+            return torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+        self.a = {"xgo": act(3 * width), "h": act(width), "n": act(width), "r": act(width), "z": act(classes)}
+        self.d = {"xgo": act(3 * width), "h": act(width), "n": act(width), "r": act(width)}
+        self.mean, self.rstd = (torch.empty(rows, self.GROUPS, device="cuda") for _ in range(2))
+        self.kept = torch.empty(L.recur_kept_bytes(self.recur) + 16, dtype=torch.uint8, device="cuda")
+        self.loss = torch.empty(1, device="cuda")
+        need = [L.linear_workspace_bytes(d, w) for d in (self.proj, self.down, self.head) for w in (A.LINEAR_FWD, A.LINEAR_BWD)]
+        need += [L.recur_workspace_bytes(self.recur, w) for w in (A.RECUR_FWD, A.RECUR_BWD)]
+        need += [L.group_norm_workspace_bytes(self.norm, w) for w in (A.GROUP_NORM_FWD, A.GROUP_NORM_BWD)]
+        need.append(L.distill_workspace_bytes(self.loss_desc, A.DISTILL_LOSS_GRAD))
+        self.ws = torch.empty(max(need) + 16, dtype=torch.uint8, device="cuda")
+        self.state = torch.zeros(slots, width, device="cuda")
+        self.q8 = None
+
+    def _linears(self, rows):
+        return [L.linear_desc(rows, n, k) for n, k in ((3 * self.width, self.width), (self.width, self.width), (self.classes, self.width))]
+
+    def _blocks(self, rows, seqs):
+        w = self.width
+        return L.recur_desc(rows, w, seqs, act=A.ACT_SILU, ldx=3 * w, ldy=w), L.group_norm_desc(rows, 1, w, self.GROUPS)
+
+    # ---- training ----
+    def logits(self, tokens, offsets):
+        """Logits of a batch (the student's own buffer): tokens: rows class numbers, offsets: seqs + 1 borders of the sequences, which cover all rows."""
+        _expect("tokens", tokens, (self.rows,), torch.int64)
+        _expect("offsets", offsets, (self.seqs + 1,), torch.int32)
+        s, w, p, a, ws, width = _stream(), self.weights, self.params, self.a, _ptr(self.ws), self.width
+        self.e = self.embed[tokens]
+        L.linear_fwd(self.proj, _ptr(self.e), _ptr(w["wp"]), _ptr(p["bp"]), None, _ptr(a["xgo"]), None, ws, s)
+        x, g, o = (_ptr(a["xgo"][:, i * width:]) for i in range(3))
+        L.recur_fwd(self.recur, x, g, o, _ptr(offsets), None, _ptr(a["h"]), None, _ptr(self.kept), ws, s)
+        L.group_norm_fwd(self.norm, _ptr(a["h"]), _ptr(p["gamma"]), _ptr(p["beta"]), _ptr(a["n"]), _ptr(self.mean), _ptr(self.rstd), ws, s)
+        L.linear_fwd(self.down, _ptr(a["n"]), _ptr(w["wd"]), _ptr(p["bd"]), _ptr(self.e), _ptr(a["r"]), None, ws, s)
+        L.linear_fwd(self.head, _ptr(a["r"]), _ptr(w["wh"]), None, None, _ptr(a["z"]), None, ws, s)
+        return a["z"]
+
+    def step(self, tokens, offsets, t, ids):
+        """Forward, loss and gradients of a batch; t, ids: the teacher's top logits and their classes.  Returns the loss (a tensor, not waited for)."""
+        _expect("t", t, (self.rows, self.top), torch.float32)
+        _expect("ids", ids, (self.rows, self.top), torch.int32)
+        self.logits(tokens, offsets)
+        s, w, p, a, d, g, ws, width = _stream(), self.weights, self.params, self.a, self.d, self.grads, _ptr(self.ws), self.width
+        L.distill_loss_grad(self.loss_desc, _ptr(a["z"]), _ptr(t), _ptr(ids), None, _ptr(self.loss), _ptr(a["z"]), ws, s)
+        L.linear_bwd(self.head, _ptr(a["z"]), _ptr(a["r"]), _ptr(w["wh"]), None, _ptr(d["r"]), _ptr(g["wh"]), None, ws, s)
+        L.linear_bwd(self.down, _ptr(d["r"]), _ptr(a["n"]), _ptr(w["wd"]), None, _ptr(d["n"]), _ptr(g["wd"]), _ptr(g["bd"]), ws, s)
+        L.group_norm_bwd(self.norm, _ptr(d["n"]), _ptr(a["h"]), _ptr(p["gamma"]), _ptr(p["beta"]), _ptr(self.mean), _ptr(self.rstd), _ptr(d["h"]), _ptr(g["gamma"]),
+                         _ptr(g["beta"]), ws, s)
+        x, gate, o = (_ptr(a["xgo"][:, i * width:]) for i in range(3))
+        dx, dg, do = (_ptr(d["xgo"][:, i * width:]) for i in range(3))
+        L.recur_bwd(self.recur, _ptr(d["h"]), x, gate, o, _ptr(offsets), None, _ptr(self.kept), None, dx, dg, do, None, ws, s)
+        L.linear_bwd(self.proj, _ptr(d["xgo"]), _ptr(self.e), None, None, None, _ptr(g["wp"]), _ptr(g["bp"]), ws, s)
+        return self.loss
+
+    def update(self, lr):
+        for k, v in self.weights.items():
+            v.copy_(v.float() - lr * self.grads[k])
+        for k, v in self.params.items():
+            v -= lr * self.grads[k]
+        self.q8 = None
+
+    # ---- answering ----
+    def quantise(self):
+        """Lays the weights out in 8-bit integers; answers take them from then on, until the next update."""
+        self.q8, s = {}, _stream()
+        for k, (n, width) in {"wp": (3 * self.width, self.width), "wd": (self.width, self.width), "wh": (self.classes, self.width)}.items():
+            d = L.linear_q8_desc(1, n, width)
+            wq, sw = torch.empty(L.linear_q8_weight_bytes(d), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+            L.linear_q8_weight(d, _ptr(self.weights[k]), _ptr(wq), _ptr(sw), s)
+            self.q8[k] = (wq, sw)
+
+    def _linear(self, key, x, n, bias, res):
+        rows, y = x.shape[0], torch.empty(x.shape[0], n, dtype=torch.bfloat16, device="cuda")
+        if self.q8 is None:
+            d = L.linear_desc(rows, n, self.width)
+            ws = torch.empty(L.linear_workspace_bytes(d, A.LINEAR_FWD) + 16, dtype=torch.uint8, device="cuda")
+            L.linear_fwd(d, _ptr(x), _ptr(self.weights[key]), _ptr(bias), _ptr(res), _ptr(y), None, _ptr(ws), _stream())
+        else:
+            d = L.linear_q8_desc(rows, n, self.width)
+            ws = torch.empty(L.linear_q8_workspace_bytes(d) + 16, dtype=torch.uint8, device="cuda")
+            wq, sw = self.q8[key]
+            L.linear_q8_fwd(d, _ptr(x), _ptr(wq), _ptr(sw), _ptr(bias), _ptr(res), _ptr(y), _ptr(ws), _stream())
+        return y
+
+    def read(self, tokens, slots, into=None):
+        """Logits behind each of some tokens (class numbers), whose requests' states lie in `slots`; tokens of one slot are consecutive, -1: none.  The new states go to `into` (slots x width fp32),
+        or over the old ones."""
+        n = tokens.shape[0]
+        _expect("tokens", tokens, (n,), torch.int64)
+        _expect("slots", slots, (n,), torch.int32)
+        into = self.state if into is None else into
+        _expect("into", into, (self.slots, self.width), torch.float32)
+        p, s, w = self.params, _stream(), self.width
+        e = self.embed[tokens]
+        xgo = self._linear("wp", e, 3 * w, p["bp"], None)
+        recur, norm = L.recur_desc(n, w, self.slots, act=A.ACT_SILU, ldx=3 * w, ldy=w), L.group_norm_desc(n, 1, w, self.GROUPS)
+        h, y = torch.zeros(n, w, dtype=torch.bfloat16, device="cuda"), torch.empty(n, w, dtype=torch.bfloat16, device="cuda")
+        L.recur_step(recur, *(_ptr(xgo[:, i * w:]) for i in range(3)), _ptr(slots), _ptr(self.state), _ptr(into), _ptr(h), s)
+        ws = torch.empty(L.group_norm_workspace_bytes(norm, A.GROUP_NORM_FWD) + 16, dtype=torch.uint8, device="cuda")
+        L.group_norm_fwd(norm, _ptr(h), _ptr(p["gamma"]), _ptr(p["beta"]), _ptr(y), None, None, _ptr(ws), s)
+        return self._linear("wh", self._linear("wd", y, w, p["bd"], e), self.classes, None, None)
+
+    def draft(self, tokens, count, u):
+        """For every slot: `count` tokens behind `tokens`, drawn with the random numbers u (slots x count), and the probabilities that they were drawn from.  The states stay as they are."""
+        slots = torch.arange(self.slots, dtype=torch.int32, device="cuda")
+        old, drafted, probs = self.state, [], []
+        self.state = old.clone()
+        for i in range(count):
+            q = torch.softmax(self.read(tokens, slots).float(), dim=1)
+            run = q.double().cumsum(1)
+            tokens = (run > u[:, i:i + 1] * run[:, -1:]).long().argmax(1)
+            drafted.append(tokens)
+            probs.append(q)
+        self.state = old
+        return torch.stack(drafted, 1), torch.stack(probs, 1).contiguous()
+
+
+def verify(p, q, drafted, u, v):
+    """The accepted counts and the tokens of lms_verify; p: (requests, drafts + 1, classes), q: (requests, drafts, classes)."""
+    b, d, c = q.shape
+    _expect("p", p, (b, d + 1, c), torch.float32)
+    _expect("q", q, (b, d, c), torch.float32)
+    _expect("drafted", drafted, (b, d), torch.int32)
+    _expect("u", u, (b, d), torch.float32)
+    _expect("v", v, (b,), torch.float32)
+    desc = L.verify_desc(b, d, c)
+    ws = torch.empty(L.verify_workspace_bytes(desc) + 16, dtype=torch.uint8, device="cuda")
+    accepted, tokens = torch.empty(b, dtype=torch.int32, device="cuda"), torch.empty(b, d + 1, dtype=torch.int32, device="cuda")
+    L.verify(desc, _ptr(p), _ptr(q), _ptr(drafted), None, _ptr(u), _ptr(v), _ptr(accepted), _ptr(tokens), _ptr(ws), _stream())
+    return accepted, tokens
+
+
+def answer(student, teacher, tokens, length, drafts, gen):
+    """Tokens of every slot behind `tokens`, at least `length` of each, distributed as the teacher's: the student drafts, the teacher reads each run of drafts in one call.  Returns a list of lists and
+    the mean of accepted drafts."""
+    b = teacher.slots
+    answers, counts = [[] for _ in range(b)], []
+    at = torch.arange(drafts + 1, device="cuda")
+    slots = torch.arange(b, dtype=torch.int32, device="cuda")[:, None].expand(b, drafts + 1)
+    while min(len(a) for a in answers) < length:
+        u, v = torch.rand(b, drafts, generator=gen, device="cuda"), torch.rand(b, generator=gen, device="cuda")
+        drafted, q = student.draft(tokens, drafts, torch.rand(b, drafts, generator=gen, device="cuda", dtype=torch.float64))
+        run = torch.cat([tokens[:, None], drafted], 1)
+        trial = teacher.state.clone()                              # a run that may be taken back
+        z = teacher.read(run.reshape(-1).contiguous(), slots.reshape(-1).contiguous(), into=trial)
+        p = torch.softmax(z.float(), dim=1).reshape(b, drafts + 1, -1)
+        accepted, got = verify(p, q, drafted.int().contiguous(), u, v)
+        # the token before the drafts and the accepted ones go into the states; the next token will with the next run
+        keep = torch.where(at[None, :] <= accepted[:, None], slots, torch.full_like(slots, -1)).reshape(-1).contiguous()
+        for m in (student, teacher):
+            m.read(run.reshape(-1).contiguous(), keep)
+        tokens = got.gather(1, accepted.long()[:, None])[:, 0].long()
+        counts.append(accepted.float().mean().item())
+        for i, (n, t) in enumerate(zip(accepted.tolist(), got.tolist())):
+            answers[i] += t[:n + 1]
+    return answers, sum(counts) / len(counts)
+
+
+def batches(teacher, rows, seqs, classes, top, gen, sharp=3.0):
+    """Endless batches: packed sequences of random tokens, and the teacher's top logits."""
+    while True:
+        tokens = torch.randint(classes, (rows,), generator=gen, device="cuda")
+        cuts = torch.randint(rows + 1, (seqs - 1,), generator=gen, device="cuda").sort().values
+        offsets = torch.cat([cuts.new_zeros(1), cuts, cuts.new_full((1,), rows)]).int().contiguous()
+        t, ids = torch.topk(teacher.logits(tokens, offsets).float() * sharp, top, dim=1)
+        yield tokens, offsets, t.contiguous(), ids.int().contiguous()
+
+
+def train(steps=60, rows=1024, seqs=8, width=256, classes=1000, top=32, slots=4, lr=4.0, seed=0):
+    """Trains a student on a synthetic teacher with the same embeddings; returns both and the losses."""
+    teacher = SequenceStudent(rows, seqs, width, classes, top, slots, seed=seed + 1)
+    student = SequenceStudent(rows, seqs, width, classes, top, slots, seed=seed)
+    student.embed = teacher.embed
+    gen = torch.Generator(device="cuda").manual_seed(seed + 2)
+    losses = []
+    for _, batch in zip(range(steps), batches(teacher, rows, seqs, classes, top, gen)):
+        losses.append(student.step(*batch).clone())
+        student.update(lr)
+    return student, teacher, [v.item() for v in losses]
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--steps", type=int, default=60)
+    ap.add_argument("--rows", type=int, default=1024)
+    ap.add_argument("--width", type=int, default=256)
+    ap.add_argument("--classes", type=int, default=1000)
+    ap.add_argument("--lr", type=float, default=4.0)
+    ap.add_argument("--drafts", type=int, default=4)
+    ap.add_argument("--tokens", type=int, default=24)
+    a = ap.parse_args()
+    student, teacher, losses = train(a.steps, a.rows, width=a.width, classes=a.classes, lr=a.lr)
+    for i in range(0, len(losses), max(1, len(losses) // 10)):
+        print(f"step {i:4d}  loss {losses[i]:.4f}")
+    student.quantise()
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    answers, accepted = answer(student, teacher, torch.randint(a.classes, (teacher.slots,), generator=gen, device="cuda"), a.tokens, a.drafts, gen)
+    print(f"{sum(map(len, answers))} tokens of {len(answers)} requests, {accepted:.2f} of {a.drafts} drafts accepted at a time")
+
+
+if __name__ == "__main__":
+    main()
