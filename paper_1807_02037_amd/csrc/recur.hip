@@ -357,6 +357,189 @@ __global__ __launch_bounds__(64 * JOIN_SPANS) void recur_join_kernel(RecurP p) {
   walk(a, in, true);
 }
 
+// ---- sequences of one length, each by work-groups that walk along it ----
+//
+// Where there are enough of them for the chip, every tensor is read once: a work-group takes two channels a lane of one sequence and goes through it 64 rows at a time, eight waves of eight rows, the next rows' loads out
+// before these are worked on.  The waves' spans meet in LDS, every wave composes all of them, and so each knows the state that the next 64 rows begin with: one barrier a step.  Rows
+// beyond a sequence's end pass r on as it is (a = 1, e = 0), so that the gradient of the last state enters there.
+constexpr int WV = 2, WBLOCK = 64 * WV, WROWS = 8, WSTEP = 8 * WROWS;
+
+template <typename T, bool BWD>
+__global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
+  __shared__ float2 s_a[2][8][64], s_h[2][8][64], s_r[2][BWD ? 8 : 1][BWD ? 64 : 1];
+  const int blocks = (p.channels + WBLOCK - 1) / WBLOCK, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int seq = blockIdx.x / blocks, c0 = (int)(blockIdx.x - seq * blocks) * WBLOCK + lane * WV;
+  const unsigned c = c0 > p.channels - WV ? p.channels - WV : c0;  // the last pair of an odd row begins earlier, and its first channel is computed twice, alike
+  const bool column = c0 < p.channels, gated = p.o != nullptr;
+  const long long row0 = seq * p.each;
+  const int each = (int)p.each, steps = (each + WSTEP - 1) / WSTEP, keeps = (each + KEEP - 1) / KEEP;
+  typedef Raw<T, WV> Pair;
+  Pair x[WROWS], g[WROWS], o[WROWS], dy[BWD ? WROWS : 1], nx[WROWS], ng[WROWS], no[WROWS], ndy[BWD ? WROWS : 1];
+  float2 entry = {}, next_entry = {};                             // backward: the state that these rows begin with
+  auto pair = [](const T* q) { Pair r; __builtin_memcpy(&r, q, sizeof(r)); return r; };
+  auto ask = [&](int step) __attribute__((always_inline)) {
+    if (!column) return;
+#pragma unroll
+    for (int r = 0; r < WROWS; ++r) {
+      const int at = step * WSTEP + wave * WROWS + r;
+      const long long row = row0 + (at < each ? at : each - 1);
+      nx[r] = pair((const T*)p.x + row * p.ldx + c);
+      ng[r] = pair((const T*)p.g + row * p.ldx + c);
+      if constexpr (BWD) ndy[r] = pair((const T*)p.dy + row * p.ldy + c);
+    }
+    if (gated)
+#pragma unroll
+      for (int r = 0; r < WROWS; ++r) {
+        const int at = step * WSTEP + wave * WROWS + r;
+        no[r] = pair((const T*)p.o + (row0 + (at < each ? at : each - 1)) * p.ldx + c);
+      }
+    if constexpr (BWD) __builtin_memcpy(&next_entry, p.kept + ((long long)seq * keeps + step * (WSTEP / KEEP)) * p.channels + c, 8);
+  };
+  const float* from = BWD ? p.dlast : p.h0;
+  float2 carry = {};
+  if (from && column) __builtin_memcpy(&carry, from + (long long)seq * p.channels + c, 8);
+  auto get = [](const float2& v, int e) { return e ? v.y : v.x; };
+  auto pass = [](const float2& a, const float2& v, const float2& h) { return make_float2(__builtin_fmaf(a.x, v.x, h.x), __builtin_fmaf(a.y, v.y, h.y)); };
+  auto put = [&](T* base, long long row, const float (&v)[WV]) {
+    if constexpr (sizeof(T) == 2) {
+      const unsigned q = pack_bf16x2(v[0], v[1]);
+      __builtin_memcpy(base + row + c, &q, 4);
+    } else __builtin_memcpy(base + row + c, v, 8);
+  };
+  ask(BWD ? steps - 1 : 0);
+  for (int i = 0; i < steps; ++i) {
+    const int step = BWD ? steps - 1 - i : i, half = i & 1, at0 = step * WSTEP + wave * WROWS;
+#pragma unroll
+    for (int r = 0; r < WROWS; ++r) {
+      x[r] = nx[r]; g[r] = ng[r]; o[r] = no[r];
+      if constexpr (BWD) dy[r] = ndy[r];
+    }
+    entry = next_entry;
+    if (i + 1 < steps) ask(BWD ? step - 1 : step + 1);
+    float a[WROWS][WV], err[BWD ? WROWS : 1][WV];
+    if constexpr (BWD) {
+      if (gated) with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < WROWS; ++r)
+#pragma unroll
+          for (int e = 0; e < WV; ++e) {
+            float value, slope;
+            act_one<decltype(act)::value>(o[r].get(e), value, slope);
+            err[r][e] = value * dy[r].get(e);
+          }
+      });
+      else
+#pragma unroll
+        for (int r = 0; r < WROWS; ++r)
+#pragma unroll
+          for (int e = 0; e < WV; ++e) err[r][e] = dy[r].get(e);
+    }
+    float2 A = {1.f, 1.f}, H = {0.f, 0.f}, R = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < WROWS; ++r) {
+      const bool live = at0 + r < each;
+#pragma unroll
+      for (int e = 0; e < WV; ++e) {
+        a[r][e] = sigmoid(g[r].get(e));
+        if constexpr (BWD) {
+          a[r][e] = live ? a[r][e] : 1.f;
+          err[r][e] = live ? err[r][e] : 0.f;
+        }
+      }
+      A = make_float2(A.x * a[r][0], A.y * a[r][1]);
+      H = make_float2(mix(a[r][0], H.x, x[r].get(0)), mix(a[r][1], H.y, x[r].get(1)));
+      if constexpr (BWD) R = make_float2(__builtin_fmaf(A.x, err[r][0], R.x), __builtin_fmaf(A.y, err[r][1], R.y));
+    }
+    s_a[half][wave][lane] = A;
+    s_h[half][wave][lane] = H;
+    if constexpr (BWD) s_r[half][wave][lane] = R;
+    __syncthreads();                                              // the other half is read by none: its readers have written this one since
+    float2 state = BWD ? entry : carry, behind = {};
+    if constexpr (!BWD) {
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        if (w == wave) state = carry;
+        carry = pass(s_a[half][w][lane], carry, s_h[half][w][lane]);
+      }
+    } else {
+      for (int w = 0; w < wave; ++w) state = pass(s_a[half][w][lane], state, s_h[half][w][lane]);
+#pragma unroll
+      for (int w = 7; w >= 0; --w) {
+        if (w == wave) behind = carry;
+        carry = pass(s_a[half][w][lane], carry, s_r[half][w][lane]);
+      }
+    }
+    // computed anew from here on: see recur_kernel
+    auto anew = [](auto& t) __attribute__((always_inline)) {
+#pragma unroll
+      for (auto& v : t)
+#pragma unroll
+        for (unsigned& w : v.q) asm volatile("" : "+v"(w));
+    };
+    anew(x);
+    if (!column) continue;
+    if constexpr (!BWD) {
+      if (p.kept && at0 % KEEP == 0 && at0 < each) __builtin_memcpy(p.kept + ((long long)seq * keeps + at0 / KEEP) * p.channels + c, &state, 8);
+      auto finish = [&](auto act, auto with_gate) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < WROWS; ++r) {
+          float y[WV];
+          state = make_float2(mix(a[r][0], state.x, x[r].get(0)), mix(a[r][1], state.y, x[r].get(1)));
+#pragma unroll
+          for (int e = 0; e < WV; ++e) {
+            y[e] = get(state, e);
+            if constexpr (decltype(with_gate)::value) {
+              float value, slope;
+              act_one<decltype(act)::value>(o[r].get(e), value, slope);
+              y[e] *= value;
+            }
+          }
+          if (at0 + r >= each) continue;
+          put((T*)p.y, (row0 + at0 + r) * p.ldy, y);
+          if (at0 + r == each - 1 && p.last) __builtin_memcpy(p.last + (long long)seq * p.channels + c, &state, 8);
+        }
+      };
+      if (gated) with_act(p.act, [&](auto act) __attribute__((always_inline)) { finish(act, std::true_type{}); });
+      else finish(std::integral_constant<int, LMS_ACT_NONE>{}, std::false_type{});
+    } else {
+      float2 h[WROWS], now = state;
+#pragma unroll
+      for (int r = 0; r < WROWS; ++r) h[r] = now = make_float2(mix(a[r][0], now.x, x[r].get(0)), mix(a[r][1], now.y, x[r].get(1)));
+      anew(g);
+      anew(o);
+      auto finish = [&](auto act, auto with_gate) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = WROWS - 1; r >= 0; --r) {
+          if (at0 + r >= each) continue;
+          const float2 before = r > 0 ? h[r > 0 ? r - 1 : 0] : state;
+          float dx[WV], dg[WV], dout[WV], back[WV];
+#pragma unroll
+          for (int e = 0; e < WV; ++e) {
+            const float dh = err[r][e] + get(behind, e), rest = rest_of(g[r].get(e), a[r][e]);
+            dx[e] = rest * dh;
+            back[e] = a[r][e] * dh;
+            dg[e] = back[e] * rest * (get(before, e) - x[r].get(e));
+            if constexpr (decltype(with_gate)::value) {
+              float value, slope;
+              act_one<decltype(act)::value>(o[r].get(e), value, slope);
+              dout[e] = dy[r].get(e) * slope * get(h[r], e);
+            }
+          }
+          behind = make_float2(back[0], back[1]);
+          const long long to = (row0 + at0 + r) * p.ldx;
+          if (p.dx) put((T*)p.dx, to, dx);
+          if (p.dg) put((T*)p.dg, to, dg);
+          if constexpr (decltype(with_gate)::value)
+            if (p.dout) put((T*)p.dout, to, dout);
+          if (at0 + r == 0 && p.dh0) __builtin_memcpy(p.dh0 + (long long)seq * p.channels + c, &behind, 8);
+        }
+      };
+      if (gated) with_act(p.act, [&](auto act) __attribute__((always_inline)) { finish(act, std::true_type{}); });
+      else finish(std::integral_constant<int, LMS_ACT_NONE>{}, std::false_type{});
+    }
+  }
+}
+
 // One position of each request, its state in a slot.  Rows of the same slot are consecutive positions of one request: the first of them takes them all, in order.
 template <typename T>
 __global__ __launch_bounds__(256) void recur_step_kernel(RecurP p, const int32_t* slots, const float* from, float* to, int n) {
@@ -449,6 +632,26 @@ RecurP params(const lms_recur_desc* d, int chunk, const void* x, const void* g, 
 // No chunk needs what another leaves: one chunk, or whole sequences in each.
 bool alone(const lms_recur_desc* d, int chunk, const int32_t* offsets) { return d->rows <= chunk || (!offsets && chunk % (d->rows / d->seqs) == 0); }
 
+// Whether work-groups walk along sequences of one length, for both directions together, since they share what is kept: by what both are estimated to take.  A step of 64 rows takes
+// 8.5 us there and back, on each compute unit one at a time, or as long as the eleven tensors take; the line reads five of them twice and has two more launches each way.
+// us, bf16 with a gate, forward + backward, walk / line:
+//   sequences x rows x channels   8 x 4096 x 4096  222 + 412 / 325 + 528     4 x 4096 x 4096  176 + 352 / 184 + 287     8 x 2048 x 2048  93 + 184 / 94 + 158
+//   32 x 512 x 512  23 + 42 / 30 + 54     16 x 128 x 1024  9 + 15 / 17 + 20     4 x 1024 x 2048  41 + 79 / 28 + 44     1 x 8192 x 4096  331 + 636 / 95 + 156
+bool walks(const lms_recur_desc* d, const int32_t* offsets) {
+  const long long each = d->rows / d->seqs, groups = (long long)d->seqs * ((d->channels + WBLOCK - 1) / WBLOCK);
+  if (offsets || each <= CHUNK_FWD || d->channels < WV || groups >= 1 << 22) return false;
+  const double bytes = (double)d->rows * d->channels * (d->dtype == LMS_F32 ? 4 : 2), rounds = (double)((groups + 255) / 256);
+  const double steps = (double)((each + WSTEP - 1) / WSTEP) * rounds * 8.5, walk = steps > bytes * 11 / 4.7e6 ? steps : bytes * 11 / 4.7e6;
+  return walk < 25.0 + bytes * 16 / 4.9e6;
+}
+template <bool BWD>
+hipError_t walk(const lms_recur_desc* d, const RecurP& p, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)d->seqs * ((d->channels + WBLOCK - 1) / WBLOCK)));
+  if (d->dtype == LMS_F32) hipLaunchKernelGGL((recur_walk_kernel<float, BWD>), grid, dim3(512), 0, s, p);
+  else hipLaunchKernelGGL((recur_walk_kernel<uint16_t, BWD>), grid, dim3(512), 0, s, p);
+  return hipGetLastError();
+}
+
 template <typename T, int WAY>
 hipError_t launch(const RecurP& p, hipStream_t s) {
   const int blocks = (p.channels + BLOCK - 1) / BLOCK;
@@ -486,7 +689,9 @@ hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
 
 lms_status recur_kept(const lms_recur_desc* d, uint64_t* bytes) {
   if (const lms_status st = check("lms_recur_kept_bytes", d, false)) return st;
-  *bytes = d->rows <= CHUNK_BWD ? 0 : up256((uint64_t)chunks_of(d->rows, KEEP) * d->channels * 4);
+  // one for each KEEP rows of the line, or of each sequence
+  const uint64_t line = chunks_of(d->rows, KEEP), seqs = d->rows % d->seqs ? 0 : (uint64_t)d->seqs * ((d->rows / d->seqs + KEEP - 1) / KEEP);
+  *bytes = d->rows <= CHUNK_BWD ? 0 : up256((line > seqs ? line : seqs) * d->channels * 4);
   return LMS_OK;
 }
 
@@ -517,6 +722,7 @@ lms_status recur_fwd(const lms_recur_desc* d, const void* x, const void* g, cons
   const bool whole = alone(d, CHUNK_FWD, offsets);
   const long long part = part_chunks(d);
   hipStream_t s = (hipStream_t)stream;
+  if (walks(d, offsets)) return done(what, walk<false>(d, p, s));
   return done(what, d->dtype == LMS_F32 ? line<float, false>(p, whole, part, s) : line<uint16_t, false>(p, whole, part, s));
 }
 
@@ -542,6 +748,7 @@ lms_status recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, con
   p.in = (float*)((char*)ws + sums_bytes(d, CHUNK_BWD));
   const long long part = part_chunks(d);
   hipStream_t s = (hipStream_t)stream;
+  if (walks(d, offsets)) return done(what, walk<true>(d, p, s));
   return done(what, d->dtype == LMS_F32 ? line<float, true>(p, whole, part, s) : line<uint16_t, true>(p, whole, part, s));
 }
 

@@ -12,7 +12,10 @@ ODD = [0, 1, 0, 7, 63, 64, 65, 0, 0, 130, 2, 1, 200, 0]           # lengths, wit
 # channels, lengths (or rows, sequences of one length), act, dtype, pad
 CASES = [(1, [1], None, "fp32", 0), (4, [0, 0], "silu", "bf16", 0), (5, [3, 0, 1], "none", "bf16", 3), (256, ODD, "silu", "bf16", 0), (257, ODD, "gelu", "fp32", 1),
          (40, ODD, "gelu_tanh", "bf16", 8), (513, [1] * 70, "relu", "bf16", 5), (64, (64, 64), "silu", "bf16", 0), (64, (256, 8), "silu", "fp32", 0), (130, (300, 3), "silu", "bf16", 2),
-         (300, (1500, 1), "silu", "bf16", 0), (16, [700, 0, 3, 900], None, "bf16", 0), (260, (192, 3), None, "fp32", 0)]
+         (300, (1500, 1), "silu", "bf16", 0), (16, [700, 0, 3, 900], None, "bf16", 0), (260, (192, 3), None, "fp32", 0),
+         # work-groups that walk along sequences: steps of 64 rows that end in them, begin and end with them, pairs of channels that overlap
+         (8190, (3 * 100, 3), "silu", "bf16", 2), (24577, (129, 1), "gelu", "fp32", 0), (2050, (12 * 65, 12), "relu", "bf16", 0), (130, (100 * 192, 100), None, "bf16", 1),
+         (256, (96 * 224, 96), "gelu_tanh", "fp32", 0)]
 
 
 def make(torch, seed, c, lengths, act, dtype, pad):
@@ -165,19 +168,37 @@ def test_a_sequence_keeps_its_nan_to_itself():
 
 
 @pytest.mark.parametrize("packed", [True, False])
-def test_a_line_in_several_parts(packed):
-    """More rows than are taken at a time; the oracle on a few channels."""
+def test_long_sequences(packed):
+    """The oracle on a few channels."""
     import torch
     import paper_1807_02037_amd as L
     c, rows = 1024, 40000
     d = make(torch, 8, c, [17000, 1, 22999] if packed else (rows, 2), "silu", "bf16", 0)
-    assert d["rows"] * c * 6 > 2 * (96 << 20)
     out = call(torch, L, d, c, "silu", 0)
     torch.cuda.synchronize()
     few = [0, 255, 256, 700, 1023]
     part = {k: v[:, few] if torch.is_tensor(v) and v.dim() == 2 else v for k, v in d.items()}
     got = {k: v[:, few] for k, v in out.items()}
     check(torch, part, got, oracle(part, "silu"), len(few))
+
+
+def test_a_line_in_several_launches():
+    """More rows than a grid has work-groups for (2^21 of 64 rows, of 32 backward): the sequences on either side of the launches' borders against the same ones alone."""
+    import torch
+    import paper_1807_02037_amd as L
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    rows, border = (1 << 27) + 5000, [0, (1 << 26) - 700, (1 << 26) + 900, (1 << 27) - 333, (1 << 27) + 444, (1 << 27) + 5000]
+    offsets = torch.tensor(border, dtype=torch.int32, device="cuda")
+    d = dict(rows=rows, seqs=5, kind=torch.bfloat16, offsets=offsets)
+    for n in ("x", "g", "o", "dy"):
+        d[n] = torch.randn(rows, 1, generator=gen, device="cuda", dtype=torch.bfloat16)
+    d["h0"], d["dlast"] = (torch.randn(5, 1, generator=gen, device="cuda") for _ in range(2))
+    out = call(torch, L, d, 1, "silu", 0)
+    for s in (1, 3, 4):
+        b, e = border[s], border[s + 1]
+        one = dict(d, rows=e - b, seqs=1, offsets=None, h0=d["h0"][s:s + 1], dlast=d["dlast"][s:s + 1], **{n: d[n][b:e].contiguous() for n in ("x", "g", "o", "dy")})
+        got = {n: out[n][b:e] if n in ("y", "dx", "dg", "do") else out[n][s:s + 1] for n in out}
+        check(torch, one, got, oracle(one, "silu"), 1)
 
 
 @pytest.mark.parametrize("dtype,c,n,slots", [("bf16", 256, 5, 9), ("fp32", 1033, 3, 3), ("bf16", 4100, 70, 200), ("bf16", 3, 1, 1)])
