@@ -91,15 +91,19 @@ __device__ __forceinline__ void merge(float& n, float (&mean)[V], float (&m2)[V]
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(NT) void norm_stats_kernel(NormP p) {
   __shared__ float s_n[WAVES][64], s_mean[WAVES][64][V], s_m2[WAVES][64][V];
+  constexpr int U = 4;                                            // and the next four on their way: registers for four work-groups on a compute unit
   const Place t = place<WHOLE>(p, blockIdx.x);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float n = 0.f, mean[V] = {}, m2[V] = {};
   const T* x = (const T*)p.x + t.row0 * p.ldx + t.c;
   if (t.there) {
     Raw<T, V> v[U], next[U];
+    const T *const begin = x + t.first * p.ldx, *from = begin;
+    const long long step = t.stride * p.ldx;
     auto ask = [&](long long r) {                                 // rows beyond the last: the thread's first, for nothing
 #pragma unroll
-      for (int u = 0; u < U; ++u) next[u] = raw<V>(x + (r + u * t.stride < t.rows ? r + u * t.stride : t.first) * p.ldx, t.cnt);
+      for (int u = 0; u < U; ++u) next[u] = raw<V>(r + u * t.stride < t.rows ? from + u * step : begin, t.cnt);
+      from += U * step;
     };
     if (t.first < t.rows) ask(t.first);
     for (long long r = t.first; r < t.rows; r += (long long)U * t.stride) {
@@ -235,21 +239,24 @@ __global__ __launch_bounds__(NT) void norm_apply_kernel(NormP p) {
   float scale[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) scale[e] = k.rstd[e] * k.gamma[e];
-  const T* x = (const T*)p.x + t.row0 * p.ldx + t.c;
-  T* y = (T*)p.out + t.row0 * p.ldo + t.c;
+  const long long xstep = t.stride * p.ldx, ystep = t.stride * p.ldo;
+  const T* x = (const T*)p.x + (t.row0 + t.first) * p.ldx + t.c;
+  T* y = (T*)p.out + (t.row0 + t.first) * p.ldo + t.c;
   with_act(p.act, [&](auto act) {
     for (long long r = t.first; r < t.rows; r += (long long)U * t.stride) {
       Raw<T, V> v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = raw<V>(x + (r + u * t.stride < t.rows ? r + u * t.stride : r) * p.ldx, t.cnt);
+      for (int u = 0; u < U; ++u) v[u] = raw<V>(x + (r + u * t.stride < t.rows ? u * xstep : 0), t.cnt);
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (r + u * t.stride < t.rows) {
           float o[V], slope;
 #pragma unroll
           for (int e = 0; e < V; ++e) act_one<decltype(act)::value>(__builtin_fmaf(v[u].get(e) - k.mean[e], scale[e], k.beta[e]), o[e], slope);
-          store4(y + (r + u * t.stride) * p.ldo, t.cnt, o);
+          store4(y + u * ystep, t.cnt, o);
         }
+      x += U * xstep;
+      y += U * ystep;
     }
   });
 }
@@ -274,16 +281,19 @@ __global__ __launch_bounds__(NT) void norm_sums_kernel(NormP p) {
   float a[V] = {}, b[V] = {};
   if (t.there) {
     const Coef k(p, t.sample, t.c);
-    const T *x = (const T*)p.x + t.row0 * p.ldx + t.c, *dy = (const T*)p.dy + t.row0 * p.ldy + t.c;
+    const long long xstep = t.stride * p.ldx, dstep = t.stride * p.ldy;
+    const T *x = (const T*)p.x + (t.row0 + t.first) * p.ldx + t.c, *dy = (const T*)p.dy + (t.row0 + t.first) * p.ldy + t.c;
     with_act(p.act, [&](auto act) {
       for (long long r = t.first; r < t.rows; r += (long long)U * t.stride) {
         Raw<T, V> v[U], d[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const long long row = r + u * t.stride < t.rows ? r + u * t.stride : r;
-          v[u] = raw<V>(x + row * p.ldx, t.cnt);
-          d[u] = raw<V>(dy + row * p.ldy, t.cnt);
+          const bool have = r + u * t.stride < t.rows;
+          v[u] = raw<V>(x + (have ? u * xstep : 0), t.cnt);
+          d[u] = raw<V>(dy + (have ? u * dstep : 0), t.cnt);
         }
+        x += U * xstep;
+        dy += U * dstep;
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (r + u * t.stride < t.rows) {
@@ -344,17 +354,20 @@ __global__ __launch_bounds__(NT) void norm_dx_kernel(NormP p) {
     m1[e] = p.coef[(t.sample * p.groups + k.group[e]) * 2];
     m2[e] = p.coef[(t.sample * p.groups + k.group[e]) * 2 + 1];
   }
-  const T *x = (const T*)p.x + t.row0 * p.ldx + t.c, *dy = (const T*)p.dy + t.row0 * p.ldy + t.c;
-  T* dx = (T*)p.out + t.row0 * p.ldo + t.c;
+  const long long xstep = t.stride * p.ldx, dstep = t.stride * p.ldy, ostep = t.stride * p.ldo;
+  const T *x = (const T*)p.x + (t.row0 + t.first) * p.ldx + t.c, *dy = (const T*)p.dy + (t.row0 + t.first) * p.ldy + t.c;
+  T* dx = (T*)p.out + (t.row0 + t.first) * p.ldo + t.c;
   with_act(p.act, [&](auto act) {
     for (long long r = t.first; r < t.rows; r += (long long)U * t.stride) {
       Raw<T, V> v[U], d[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const long long row = r + u * t.stride < t.rows ? r + u * t.stride : r;
-        v[u] = raw<V>(x + row * p.ldx, t.cnt);
-        d[u] = raw<V>(dy + row * p.ldy, t.cnt);
+        const bool have = r + u * t.stride < t.rows;
+        v[u] = raw<V>(x + (have ? u * xstep : 0), t.cnt);
+        d[u] = raw<V>(dy + (have ? u * dstep : 0), t.cnt);
       }
+      x += U * xstep;
+      dy += U * dstep;
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (r + u * t.stride < t.rows) {
@@ -362,8 +375,9 @@ __global__ __launch_bounds__(NT) void norm_dx_kernel(NormP p) {
           slope4<decltype(act)::value, T>(k, v[u], d[u], hat, dv);
 #pragma unroll
           for (int e = 0; e < V; ++e) dv[e] = k.rstd[e] * (__builtin_fmaf(k.gamma[e], dv[e], -m1[e]) - hat[e] * m2[e]);
-          store4(dx + (r + u * t.stride) * p.ldo, t.cnt, dv);
+          store4(dx + u * ostep, t.cnt, dv);
         }
+      dx += U * ostep;
     }
   });
 }

@@ -86,13 +86,31 @@ __global__ __launch_bounds__(NT) void q8_rows_kernel(const T* x, long long ldx, 
 // Bound by reading the weights once.  A wave takes CW columns, its lanes consecutive 16 bytes of the reduction, and has eight loads of weights in flight before anything else happens; the rows of x lie
 // in LDS, 4-byte dot products go to whole sums of each lane, and the lanes meet by shuffles: whole numbers, in any order the same.  FUSED: every work-group quantises the rows itself,
 // while its weights are on their way, instead of waiting for another launch.
-constexpr int FT = 512, FEW_LDS = 65536;
+constexpr int FT = 512, FEW_LDS = 65536 - 256;      // with what the kernel has besides, no more than any launch may have
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float v) {
   float value, slope;
   act_one<ACT>(v, value, slope);
   return value;
+}
+
+// Sums over the wave of N values of each lane: the i-th in the lanes from 64 / N i on.  Each exchange halves the values that a lane holds: N - 1 of them and the rest of six, where sums one by one take 6 N.
+template <int N>
+__device__ __forceinline__ int lanes_sum(int (&v)[N]) {
+  const int lane = threadIdx.x & 63;
+  int d = 32;
+#pragma unroll
+  for (int half = N / 2; half >= 1; half /= 2, d /= 2) {
+    const bool upper = lane & d;
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const int keep = upper ? v[i + half] : v[i], give = upper ? v[i] : v[i + half];
+      v[i] = keep + __shfl_xor(give, d);
+    }
+  }
+  for (; d >= 1; d /= 2) v[0] += __shfl_xor(v[0], d);
+  return v[0];
 }
 
 template <typename T, int R, int CW, bool FUSED>
@@ -207,19 +225,14 @@ __global__ __launch_bounds__(FT) void q8_few_kernel(DenseP p, const T* x, long l
     const int done = col;
     col += waves * CW;
     if (col < p.N) ask(col, 0);
-    // output (r, j) is lane r CW + j's
-    int mine = 0;
+    constexpr int N = CW * R, SHARE = 64 / N;                     // outputs of the wave; lanes of one: output r CW + j is that of the lanes from (r CW + j) SHARE on
+    int all[N];
 #pragma unroll
     for (int j = 0; j < CW; ++j)
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        int v = acc[j][r];
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-        mine = lane == r * CW + j ? v : mine;
-      }
-    const int r = lane / CW, n = done + lane % CW;
-    if (lane < rows * CW && n < p.N) {
+      for (int r = 0; r < R; ++r) all[r * CW + j] = acc[j][r];
+    const int mine = lanes_sum<N>(all), r = lane / SHARE / CW, n = done + lane / SHARE % CW;
+    if (lane % SHARE == 0 && r < rows && n < p.N) {
       float s = sx[0];
 #pragma unroll
       for (int i = 1; i < R; ++i) s = r == i ? sx[i] : s;
@@ -352,12 +365,9 @@ hipError_t quantise(const lms_linear_q8_desc* d, const T* x, signed char* xq, fl
   return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
 
-// Up to eight rows that fit the LDS; up to two are quantised there too.
-int few_rows(const lms_linear_q8_desc* d) {
-  const int r = d->m <= 2 ? (int)d->m : d->m <= 4 ? 4 : 8;
-  return d->m >= 1 && d->m <= 8 && (long long)r * pitch(d) <= FEW_LDS ? r : 0;
-}
-bool few_fused(const lms_linear_q8_desc* d) { return d->m <= 2 && few_rows(d); }
+// One or two rows that fit the LDS.  From three on the tiles, whose two launches then cost less than the dot products (us, few rows / tiles: 4096 -> 4096 one row 5.8 / 11.0, two 7.2 / 11.1, four 9.4 / 11.5,
+// eight 14.2 / 12.1; 2048 -> 8192 four rows 10.7 / 10.3; 8192 -> 16384 four rows 31.6 / 31.8).
+bool few_rows(const lms_linear_q8_desc* d) { return d->m >= 1 && d->m <= 2 && d->m * pitch(d) <= FEW_LDS; }
 
 template <typename T, int R, bool FUSED>
 hipError_t few(const lms_linear_q8_desc* d, DenseP& p, const T* x, hipStream_t s) {
@@ -365,8 +375,6 @@ hipError_t few(const lms_linear_q8_desc* d, DenseP& p, const T* x, hipStream_t s
   auto go = [&](auto cw) {
     constexpr int CW = decltype(cw)::value;
     const long long need = ((long long)d->n + CW * (FT / 64) - 1) / (CW * (FT / 64));
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(q8_few_kernel<T, R, CW, FUSED>), hipFuncAttributeMaxDynamicSharedMemorySize, FEW_LDS);
-    if (attr != hipSuccess) return attr;
     hipLaunchKernelGGL((q8_few_kernel<T, R, CW, FUSED>), dim3((unsigned)(need < 512 ? need : 512)), dim3(FT), R * kp, s, p, x, d->ldx ? d->ldx : (long long)d->k, d->k, kp);
     return hipGetLastError();
   };
@@ -377,12 +385,8 @@ hipError_t few(const lms_linear_q8_desc* d, DenseP& p, const T* x, hipStream_t s
 template <typename T>
 hipError_t few_product(const lms_linear_q8_desc* d, DenseP& p, const void* x, hipStream_t s) {
   const T* t = (const T*)x;
-  switch (few_rows(d)) {
-    case 1: return x ? few<T, 1, true>(d, p, t, s) : few<T, 1, false>(d, p, t, s);
-    case 2: return x ? few<T, 2, true>(d, p, t, s) : few<T, 2, false>(d, p, t, s);
-    case 4: return few<T, 4, false>(d, p, t, s);
-    default: return few<T, 8, false>(d, p, t, s);
-  }
+  if (d->m == 1) return x ? few<T, 1, true>(d, p, t, s) : few<T, 1, false>(d, p, t, s);
+  return x ? few<T, 2, true>(d, p, t, s) : few<T, 2, false>(d, p, t, s);
 }
 
 uint64_t rows_bytes(const lms_linear_q8_desc* d) { return up256((uint64_t)d->m * pitch(d)); }
@@ -412,7 +416,7 @@ lms_status aligned(const char* what, const lms_linear_q8_desc* d, std::initializ
   return LMS_OK;
 }
 
-// x: the rows themselves where few_fused, then no xq
+// x: the rows themselves where there are few, then no xq
 hipError_t product(const lms_linear_q8_desc* d, const void* x, const void* xq, const float* sx, const void* wq, const float* sw, const float* bias, const void* res, void* y, void* ws, hipStream_t s) {
   DenseP p{};
   p.a[0] = xq; p.b[0] = wq; p.out[0] = y;
@@ -477,7 +481,7 @@ lms_status linear_q8_fwd(const lms_linear_q8_desc* d, const void* x, const void*
   char* at = (char*)ws;
   float* sx = (float*)(at + rows_bytes(d));
   hipStream_t s = (hipStream_t)stream;
-  if (few_fused(d)) return done(what, product(d, x, nullptr, nullptr, wq, sw, bias, res, y, nullptr, s));
+  if (few_rows(d)) return done(what, product(d, x, nullptr, nullptr, wq, sw, bias, res, y, nullptr, s));
   hipError_t e = d->dtype == LMS_F32 ? quantise<float>(d, (const float*)x, (signed char*)at, sx, s) : quantise<uint16_t>(d, (const uint16_t*)x, (signed char*)at, sx, s);
   if (e == hipSuccess) e = product(d, nullptr, at, sx, wq, sw, bias, res, y, at + rows_bytes(d) + scale_bytes(d), s);
   return done(what, e);
