@@ -392,6 +392,7 @@ struct ResidentP {
   NormP n;
   long long samples;
   int lanes;                           // tokens: lanes of a row, a power of two
+  int span;                            // tokens: lanes among which a group meets by shuffles, or 0
   int block, blocks;                   // images: vectors of a work-group's channels, and how many such blocks there are
   int gv;                              // vectors of a group
 };
@@ -430,13 +431,12 @@ __device__ __forceinline__ void weights8(const NormP& p, int c, bool there, floa
 }
 
 // Tokens (s = 1).  A row takes `lanes` lanes of K vectors each; rows of a work-group run in parallel, and it goes on to others, the next row's loads out before this one is worked on.  Groups whose
-// vectors are a power of two of lanes of one wave meet by shuffles, others in LDS.  Backwards the sums for gamma and beta stay in registers until the work-group's last row.
+// vectors are a power of two of lanes of one wave, or all of them, meet by shuffles, others in LDS.  Backwards the sums for gamma and beta stay in registers until the work-group's last row.
 template <typename T, int NT, int K, bool BWD>
 __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
   __shared__ float s_part[2][NT * K], s_sum[2][NT * K];
   const NormP& p = q.n;
   const int tid = threadIdx.x, l = tid & (q.lanes - 1), sub = tid / q.lanes, rows = NT / q.lanes, nv = p.c / W;
-  const bool by_shuffles = (q.gv & (q.gv - 1)) == 0 && q.gv <= 64 && q.gv <= q.lanes;
   auto vec = [&](int j) { return l + j * q.lanes; };
   float ga[K][W], be[K][W], da[BWD ? K : 1][W] = {}, db[BWD ? K : 1][W] = {};
 #pragma unroll
@@ -458,8 +458,8 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
   };
   // a[j] and b[j] of each vector into the sums over its group
   auto join = [&](float (&a)[K], float (&b)[K], bool two) {
-    if (by_shuffles) {
-      for (int d = 1; d < q.gv; d *= 2)
+    if (q.span) {
+      for (int d = 1; d < q.span; d *= 2)
 #pragma unroll
         for (int j = 0; j < K; ++j) {
           a[j] += __shfl_xor(a[j], d);
@@ -475,7 +475,7 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
     }
     __syncthreads();
     int team = 1;
-    while (team < 64 && team < q.gv) team *= 2;
+    while (team < 64 && team < q.gv && 2 * team * rows * p.groups <= NT) team *= 2;
     for (int i = tid / team; i < rows * p.groups; i += NT / team) {
       const int at = i / p.groups * q.lanes * K + i % p.groups * q.gv;
       float ta = 0.f, tb = 0.f;
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
         d2[j] = b[j] = 0.f;
 #pragma unroll
         for (int e = 0; e < W; ++e) {
-          const float d = x[j].get(e) - m[j];
+          const float d = vec(j) < nv ? x[j].get(e) - m[j] : 0.f;
           b[j] += d;                                              // what the rounding of the mean left
           d2[j] = __builtin_fmaf(d, d, d2[j]);
         }
@@ -589,10 +589,162 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
         }
 }
 
+// Tokens whose groups, or rows, are not of whole vectors: the channels' values go through LDS, where a team of lanes sums each group's.
+template <typename T, int NT, int K, bool BWD>
+__global__ __launch_bounds__(NT) void norm_tokens_any_kernel(ResidentP q) {
+  extern __shared__ float s_any[];
+  const NormP& p = q.n;
+  const int tid = threadIdx.x, l = tid & (q.lanes - 1), sub = tid / q.lanes, rows = NT / q.lanes, width = q.lanes * K * W;
+  float *const s_a = s_any, *const s_b = s_a + rows * width, *const s_sum = s_b + rows * width;         // [row][channel], twice; [row][group][2]
+  int team = 1;                                                   // as many lanes for a group as there are for all of them at once
+  while (team < 64 && team < p.cg && 2 * team * rows * p.groups <= NT) team *= 2;
+  auto at = [&](int j) { return (l + j * q.lanes) * W; };
+  auto count = [&](int j) { return p.c - at(j) < W ? p.c - at(j) : W; };
+  float ga[K][W], be[K][W], da[BWD ? K : 1][W] = {}, db[BWD ? K : 1][W] = {};
+  int group[K][W];
+#pragma unroll
+  for (int j = 0; j < K; ++j)
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const bool there = at(j) + e < p.c;
+      group[j][e] = there ? (at(j) + e) / p.cg : 0;
+      ga[j][e] = there && p.gamma ? p.gamma[at(j) + e] : 1.f;
+      be[j][e] = there && p.beta ? p.beta[at(j) + e] : 0.f;
+    }
+  // the channels' values into the sums over their groups
+  auto join = [&](float (&a)[K][W], float (&b)[K][W]) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      store8(s_a + sub * width + at(j), W, a[j]);
+      store8(s_b + sub * width + at(j), W, b[j]);
+    }
+    __syncthreads();
+    for (int i = tid / team; i < rows * p.groups; i += NT / team) {
+      const int from = i / p.groups * width + i % p.groups * p.cg;
+      float ta = 0.f, tb = 0.f;
+      for (int k = tid & (team - 1); k < p.cg; k += team) {
+        ta += s_a[from + k];
+        tb += s_b[from + k];
+      }
+      for (int d = 1; d < team; d *= 2) {
+        ta += __shfl_xor(ta, d);
+        tb += __shfl_xor(tb, d);
+      }
+      if ((tid & (team - 1)) == 0) { s_sum[2 * i] = ta; s_sum[2 * i + 1] = tb; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+      for (int e = 0; e < W; ++e) {
+        const float2 t = reinterpret_cast<const float2*>(s_sum)[sub * p.groups + group[j][e]];
+        a[j][e] = t.x;
+        b[j][e] = t.y;
+      }
+  };
+  const float inv = 1.f / (float)p.cg;
+  const long long stride = (long long)gridDim.x * rows;
+  for (long long r0 = (long long)blockIdx.x * rows; r0 < q.samples; r0 += stride) {       // the same for the whole work-group
+    const long long row = r0 + sub;
+    const bool there = row < q.samples;
+    Raw<T, W> x[K], dy[BWD ? K : 1];
+    float a[K][W], b[K][W], mean[K][W], rstd[K][W];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      x[j] = raw<W>((const T*)p.x + row * p.ldx + at(j), there ? count(j) : 0);
+      if constexpr (BWD) {
+        dy[j] = raw<W>((const T*)p.dy + row * p.ldy + at(j), there ? count(j) : 0);
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          mean[j][e] = there ? p.mean[row * p.groups + group[j][e]] : 0.f;
+          rstd[j][e] = there ? p.rstd[row * p.groups + group[j][e]] : 0.f;
+        }
+      }
+    }
+    if constexpr (!BWD) {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int e = 0; e < W; ++e) { a[j][e] = x[j].get(e); b[j][e] = 0.f; }
+      join(a, b);
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          mean[j][e] = a[j][e] * inv;
+          b[j][e] = x[j].get(e) - mean[j][e];                     // their sum: what the rounding of the mean left
+          a[j][e] = b[j][e] * b[j][e];
+        }
+      join(a, b);
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (!there || count(j) <= 0) continue;
+        float y[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          const float shift = b[j][e] * inv, var = a[j][e] * inv - shift * shift, rs = 1.f / sqrtf((var > 0.f || var != var ? var : 0.f) + p.eps), m = mean[j][e] + shift;
+          if (e < count(j) && (at(j) + e) % p.cg == 0) {
+            p.mean_out[row * p.groups + group[j][e]] = m;
+            p.rstd_out[row * p.groups + group[j][e]] = rs;
+          }
+          y[e] = __builtin_fmaf((x[j].get(e) - m) * rs, ga[j][e], be[j][e]);
+        }
+        act8(p.act, y);
+        store8((T*)p.out + row * p.ldo + at(j), count(j), y);
+      }
+    } else {
+      float hat[K][W], dv[K][W];
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int e = 0; e < W; ++e) hat[j][e] = (x[j].get(e) - mean[j][e]) * rstd[j][e];
+      with_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            float value, slope;
+            act_one<decltype(act)::value>(__builtin_fmaf(ga[j][e], hat[j][e], be[j][e]), value, slope);
+            dv[j][e] = dy[j].get(e) * slope;
+          }
+      });
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          db[j][e] += dv[j][e];
+          da[j][e] = __builtin_fmaf(dv[j][e], hat[j][e], da[j][e]);
+          a[j][e] = dv[j][e] *= ga[j][e];
+          b[j][e] = dv[j][e] * hat[j][e];
+        }
+      if (!p.out) continue;
+      join(a, b);
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (!there || count(j) <= 0) continue;
+        float d[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) d[e] = rstd[j][e] * ((dv[j][e] - a[j][e] * inv) - hat[j][e] * (b[j][e] * inv));
+        store8((T*)p.out + row * p.ldo + at(j), count(j), d);
+      }
+    }
+  }
+  if constexpr (BWD)
+    if (p.part)
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (count(j) > 0) {
+          float* to = p.part + ((long long)blockIdx.x * rows + sub) * 2 * p.c + at(j);
+          store8(to, count(j), db[j]);
+          store8(to + p.c, count(j), da[j]);
+        }
+}
+
 // Images: a sample's positions of one block of whole groups, K positions of a vector of channels a thread.
 template <typename T, int NT, int K, bool BWD>
 __global__ __launch_bounds__(NT, sizeof(T) * K <= 8 ? 4 : 2) void norm_image_kernel(ResidentP q) {
-  __shared__ float s_part[2][NT], s_sum[2][64];
+  __shared__ float s_part[2][NT], s_sum[2][256];
   __shared__ float s_chan[BWD ? 2 : 1][BWD ? W : 1][BWD ? NT : 1];
   const NormP& p = q.n;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nv = p.c / W;
@@ -777,31 +929,36 @@ long long part_samples(const lms_group_norm_desc* d, const Split& t) {
 }
 
 // How a work-group holds samples, if it does: from the sizes and the type alone.
-enum { NOT_HELD, TOKENS, IMAGES };
+enum { NOT_HELD, TOKENS, TOKENS_ANY, IMAGES };
 struct Held {
-  int kind, nt, k, lanes, block, blocks;
+  int kind, nt, k, lanes, span, block, blocks;
   long long grid, rows;                // rows of sums for gamma and beta
+  unsigned lds;
 };
 constexpr int TOKEN_GROUPS = 512;      // work-groups that go through the tokens
 Held held_of(const lms_group_norm_desc* d) {
   Held h{};
-  const int cg = d->c / d->groups, nv = d->c / W, gv = cg / W;
-  if (cg % W) return h;
+  const int cg = d->c / d->groups, nv = (d->c + W - 1) / W, gv = cg / W;
   if (d->s == 1) {
     int lanes = 1;
     while (lanes < nv) lanes *= 2;
-    if (lanes <= 256) h = Held{TOKENS, 256, 1, lanes, 0, 0, 0, 0};
-    else if (nv <= 512) h = Held{TOKENS, 512, 1, 512, 0, 0, 0, 0};
-    else if (nv <= 1024) h = Held{TOKENS, 512, 2, 512, 0, 0, 0, 0};
-    else if (nv <= 2048) h = Held{TOKENS, 1024, 2, 1024, 0, 0, 0, 0};
+    if (lanes <= 256) { h.nt = 256; h.k = 1; h.lanes = lanes; }
+    else if (nv <= 512) { h.nt = 512; h.k = 1; h.lanes = 512; }
+    else if (nv <= 1024) { h.nt = 512; h.k = 2; h.lanes = 512; }
+    else if (nv <= 2048 && cg % W == 0) { h.nt = 1024; h.k = 2; h.lanes = 1024; }
     else return h;
     const long long rows = h.nt / h.lanes, need = (d->n + rows - 1) / rows;
+    h.kind = cg % W ? TOKENS_ANY : TOKENS;
+    h.span = cg % W ? 0 : (gv & (gv - 1)) == 0 && gv <= 64 ? gv : d->groups == 1 && h.lanes <= 64 ? h.lanes : 0;
+    h.lds = h.kind == TOKENS_ANY ? (unsigned)(h.nt * h.k * W * 8 + rows * d->groups * 8) : 0;
     h.grid = need < TOKEN_GROUPS ? need : TOKEN_GROUPS;
     h.rows = h.grid * rows;
     return h;
   }
-  // at least 64 channels of whole groups, whose rows are a cache line
-  const int each = gv >= 8 ? 1 : (8 + gv - 1) / gv, groups = each < d->groups ? each : d->groups;
+  if (cg % W) return h;
+  // at least 64 channels of whole groups, whose rows are a cache line, and of few positions as many as give all threads one
+  const long long fill = 256 / (d->s * gv), line = gv >= 8 ? 1 : (8 + gv - 1) / gv, each = fill > line ? fill : line;
+  const int groups = (int)(each < d->groups ? each : d->groups);
   h.block = groups * gv;
   h.blocks = (nv + h.block - 1) / h.block;
   if (h.block > 512) return Held{};
@@ -852,10 +1009,21 @@ NormP params(const lms_group_norm_desc* d, const Split& t) {
 
 template <typename T, bool BWD>
 hipError_t resident(const lms_group_norm_desc* d, const Held& h, const NormP& p, hipStream_t s) {
-  ResidentP q{p, d->n, h.lanes, h.block, h.blocks, p.cg / W};
+  ResidentP q{p, d->n, h.lanes, h.span, h.block, h.blocks, p.cg / W};
   const dim3 grid((unsigned)h.grid);
 #define TOKEN(NT, K) if (h.kind == TOKENS && h.nt == NT && h.k == K) hipLaunchKernelGGL((norm_tokens_kernel<T, NT, K, BWD>), grid, dim3(NT), 0, s, q)
 #define IMAGE(NT, K) if (h.kind == IMAGES && h.nt == NT && h.k == K) hipLaunchKernelGGL((norm_image_kernel<T, NT, K, BWD>), grid, dim3(NT), 0, s, q)
+#define ANY(NT, K)                                                                                                                                                 \
+  if (h.kind == TOKENS_ANY && h.nt == NT && h.k == K) {                                                                                                            \
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(norm_tokens_any_kernel<T, NT, K, BWD>), hipFuncAttributeMaxDynamicSharedMemorySize, \
+                                                       NT * K * W * 16);                                                                                          \
+    if (attr != hipSuccess) return attr;                                                                                                                           \
+    hipLaunchKernelGGL((norm_tokens_any_kernel<T, NT, K, BWD>), grid, dim3(NT), h.lds, s, q);                                                                      \
+  }
+  ANY(256, 1)
+  ANY(512, 1)
+  ANY(512, 2)
+#undef ANY
   TOKEN(256, 1);
   TOKEN(512, 1);
   TOKEN(512, 2);

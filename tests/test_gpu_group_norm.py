@@ -13,7 +13,11 @@ CASES = [(1, 1, 1, 1, "none", True, "fp32", 0), (3, 1, 8, 8, "silu", True, "bf16
          (65, 1, 1000, 8, "silu", False, "bf16", 8), (17, 1, 4096, 32, "none", True, "bf16", 0), (5, 1, 8192, 1, "gelu_tanh", True, "bf16", 0), (9, 1, 2044, 7, "relu", True, "fp32", 0),
          (33, 1, 2050, 2, "silu", True, "bf16", 1), (2, 1, 40000, 5, "none", True, "bf16", 0), (4, 49, 64, 8, "relu", True, "bf16", 0), (2, 63, 30, 10, "silu", True, "fp32", 2),
          (3, 196, 256, 32, "silu", True, "bf16", 0), (1, 4097, 24, 3, "gelu", True, "bf16", 8), (2, 3000, 6, 2, "none", False, "fp32", 0), (1, 70000, 16, 4, "relu", True, "bf16", 0),
-         (5, 2, 300, 1, "gelu_tanh", True, "bf16", 0), (1, 100, 1028, 257, "silu", True, "bf16", 4), (40, 5, 128, 2, "none", True, "fp32", 0), (1, 9000, 1, 1, "none", True, "fp32", 0)]
+         (5, 2, 300, 1, "gelu_tanh", True, "bf16", 0), (1, 100, 1028, 257, "silu", True, "bf16", 4), (40, 5, 128, 2, "none", True, "fp32", 0), (1, 9000, 1, 1, "none", True, "fp32", 0),
+         # tokens whose rows are all of a group, of no power of two of vectors; groups and rows that are not of whole vectors; images of few positions
+         (700, 1, 192, 1, "gelu", True, "bf16", 0), (33, 1, 440, 1, "silu", True, "fp32", 1), (1500, 1, 576, 16, "gelu", True, "bf16", 0), (90, 1, 1001, 7, "silu", True, "fp32", 3),
+         (21, 1, 4100, 41, "relu", False, "bf16", 0), (19, 1, 8190, 2, "gelu_tanh", True, "bf16", 2), (5, 1, 7000, 7000, "none", True, "bf16", 0), (3000, 1, 12, 4, "silu", True, "fp32", 0),
+         (50, 2, 1024, 32, "silu", True, "bf16", 0), (33, 3, 64, 8, "relu", True, "fp32", 0), (9, 7, 8, 1, "none", True, "bf16", 0), (6, 30, 2048, 2, "gelu", True, "bf16", 8)]
 
 
 def ptr(t):
