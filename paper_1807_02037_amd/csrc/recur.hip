@@ -35,28 +35,61 @@ struct RecurP {
   long long rows, ldx, ldy, each;      // each: rows of a sequence where there are no offsets
   int seqs, channels, act;
   int chunk0, chunks, all_chunks;      // chunks of this launch
+  int lpr, subs;               // lanes of a row, a power of two; runs of rows of a wave, 64 / lpr
 };
 
-// Rows of a wave: which begin a sequence, which end one, which belong to one; lane r holds the sequence of row r.
+// Rows of a run: which begin a sequence, which end one, which belong to one.  Of a whole wave: the same for all lanes, and lane r holds the sequence of row r.
+template <int ROWS, bool NARROW>
 struct Marks {
   unsigned first, last, live;
-  int seq;
+  int seq[NARROW ? ROWS : 1];
+  __device__ __forceinline__ int of(int r) const {
+    if constexpr (NARROW) return seq[r];
+    else return __builtin_amdgcn_readlane(seq[0], r);
+  }
 };
+// The last sequence that begins at or before the row; of several at the same place all but the last are empty.  -1: none.
+__device__ __forceinline__ int sequence_of(const RecurP& p, long long row) {
+  int lo = -1, hi = p.seqs + 1;                                   // offsets[lo] <= row < offsets[hi]
+  while (hi - lo > 1) {
+    const int mid = lo + (hi - lo) / 2;
+    if (p.offsets[mid] <= row) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+// Of each lane's own run.
 template <int ROWS>
-__device__ __forceinline__ Marks marks(const RecurP& p, long long r0) {
+__device__ __forceinline__ Marks<ROWS, true> own_marks(const RecurP& p, long long r0) {
+  Marks<ROWS, true> m = {0u, 0u, 0u, {}};
+  if (r0 >= p.rows) return m;
+  int s = p.offsets ? sequence_of(p, r0) : (int)(r0 / p.each);
+  long long begin = p.offsets ? (s >= 0 ? p.offsets[s] : 0) : s * p.each, next = p.offsets ? (s < p.seqs ? p.offsets[s + 1] : 0) : begin + p.each;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const long long row = r0 + r;
+    while (s < p.seqs && next <= row) {                           // on to the sequence of this row
+      ++s;
+      begin = next;
+      next = p.offsets ? (s < p.seqs ? p.offsets[s + 1] : 0) : begin + p.each;
+    }
+    const bool live = row < p.rows && s >= 0 && s < p.seqs;
+    m.live |= (unsigned)live << r;
+    m.first |= (unsigned)(live && begin == row) << r;
+    m.last |= (unsigned)(live && next == row + 1) << r;
+    m.seq[r] = live ? s : 0;
+  }
+  return m;
+}
+template <int ROWS>
+__device__ __forceinline__ Marks<ROWS, false> marks(const RecurP& p, long long r0) {
   const int lane = threadIdx.x & 63;
   const long long row = r0 + lane;
   bool first = false, last = false, live = lane < ROWS && row < p.rows;
   int s = 0;
   if (live) {
-    if (p.offsets) {                                              // the last sequence that begins at or before the row; of several at the same place all but the last are empty
-      int lo = -1, hi = p.seqs + 1;                               // offsets[lo] <= row < offsets[hi]
-      while (hi - lo > 1) {
-        const int mid = lo + (hi - lo) / 2;
-        if (p.offsets[mid] <= row) lo = mid;
-        else hi = mid;
-      }
-      s = lo;
+    if (p.offsets) {
+      s = sequence_of(p, row);
       live = s >= 0 && s < p.seqs;
       if (live) {
         first = p.offsets[s] == row;
@@ -69,13 +102,13 @@ __device__ __forceinline__ Marks marks(const RecurP& p, long long r0) {
       last = at == p.each - 1;
     }
   }
-  return Marks{(unsigned)__ballot(first), (unsigned)__ballot(last), (unsigned)__ballot(live), s};
+  return Marks<ROWS, false>{(unsigned)__ballot(first), (unsigned)__ballot(last), (unsigned)__ballot(live), {s}};
 }
 
 // 1 - a for a = sigmoid(g), without its cancellation: the exponential that a has below its line, times a.  Beyond 2^100 it is cut: a is then nothing against any state, and the rest 1.
 __device__ __forceinline__ float rest_of(float g, float a) {
   const float e = __builtin_amdgcn_exp2f(g * -1.44269504f);
-  return e < 0x1p100f ? e * a : 1.f;
+  return e >= 0x1p100f ? 1.f : e * a;
 }
 
 // a h + (1 - a) x: a difference that is exact from a = 1/2 on, so that a state no gate touches stays what it is.
@@ -87,7 +120,7 @@ __device__ __forceinline__ float product(float a, float second) { return __built
 
 enum { SUM_FWD, APPLY_FWD, SUM_BWD, APPLY_BWD };
 
-constexpr int CHUNK_FWD = 64, CHUNK_BWD = 32;                      // rows of a work-group
+constexpr int CHUNK_FWD = 64, CHUNK_BWD = 32;                      // rows of a work-group, times the runs of a wave
 static_assert(CHUNK_BWD == KEEP, "a chunk of the backward pass begins where a state is kept");
 
 // Rows of a wave: forward eight, whose raw inputs and gates leave registers for sixteen waves on a compute unit; backward, with twice the tensors, four; in fp32 half of that.
@@ -99,47 +132,54 @@ struct Shape {
 };
 
 // WHOLE: at least four channels.  The last vector of a row that would end beyond it begins earlier instead, and its first channels are computed twice, alike.
-template <typename T, int WAY, bool WHOLE>
+// NARROW: up to 128 channels.  They leave lanes free, and a wave takes several runs of rows one after the other, which meet by shuffles before the waves do.
+template <typename T, int WAY, bool WHOLE, bool NARROW>
 __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p) {
   constexpr int ROWS = Shape<T, WAY>::ROWS, WAVES = Shape<T, WAY>::WAVES, CHUNK = Shape<T, WAY>::CHUNK;
   constexpr bool BWD = Shape<T, WAY>::BWD, STATE = WAY != SUM_BWD;   // STATE: h is computed
   __shared__ float s_a[STATE ? WAVES : 1][BLOCK], s_h[STATE ? WAVES : 1][BLOCK], s_b[BWD ? WAVES : 1][BLOCK], s_r[BWD ? WAVES : 1][BLOCK];
-  const int blocks = (p.channels + BLOCK - 1) / BLOCK, job = blockIdx.x;
-  const int chunk = job / blocks, at = (threadIdx.x & 63) * V, c0 = (job - chunk * blocks) * BLOCK + at;
+  const int blocks = NARROW ? 1 : (p.channels + BLOCK - 1) / BLOCK, job = blockIdx.x, lane = threadIdx.x & 63;
+  const int run = NARROW ? lane / p.lpr : 0, runs = NARROW ? p.subs : 1, col = NARROW ? lane & (p.lpr - 1) : lane;
+  const int chunk = job / blocks, at = col * V, c0 = (job - chunk * blocks) * BLOCK + at;
   const unsigned c = WHOLE && c0 > p.channels - V ? p.channels - V : c0;       // an offset of 32 bits from what is the same for the wave
   const bool column = c0 < p.channels;
   const int cnt = WHOLE ? V : p.channels - c0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long r0 = (long long)(p.chunk0 + chunk) * CHUNK + wave * ROWS;
+  const long long row0 = (long long)(p.chunk0 + chunk) * (CHUNK * runs), r0 = row0 + (wave * runs + run) * ROWS;
+  const long long x0 = r0 * p.ldx, y0 = r0 * p.ldy;               // of the first row
   const bool there = column && r0 < p.rows, gated = p.o != nullptr;
 
-  // all that is read of the rows, in flight at once; rows beyond the last: the last, for nothing
+  // all that is read of the rows, in flight at once; rows beyond the last: the first, for nothing
   Raw<T, V> x[STATE ? ROWS : 1], g[ROWS], o[WAY == SUM_FWD ? 1 : ROWS], dy[BWD ? ROWS : 1];
   if (there) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const long long row = r0 + r < p.rows ? r0 + r : p.rows - 1;
-      g[r] = raw<V>((const T*)p.g + row * p.ldx + c, cnt);
-      if constexpr (STATE) x[r] = raw<V>((const T*)p.x + row * p.ldx + c, cnt);
-      if constexpr (BWD) dy[r] = raw<V>((const T*)p.dy + row * p.ldy + c, cnt);
+      const bool have = r0 + r < p.rows;
+      const long long xr = x0 + (have ? r * p.ldx : 0), yr = y0 + (have ? r * p.ldy : 0);
+      g[r] = raw<V>((const T*)p.g + xr + c, cnt);
+      if constexpr (STATE) x[r] = raw<V>((const T*)p.x + xr + c, cnt);
+      if constexpr (BWD) dy[r] = raw<V>((const T*)p.dy + yr + c, cnt);
     }
     if constexpr (WAY != SUM_FWD)
       if (gated)
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) o[r] = raw<V>((const T*)p.o + (r0 + r < p.rows ? r0 + r : p.rows - 1) * p.ldx + c, cnt);
+        for (int r = 0; r < ROWS; ++r) o[r] = raw<V>((const T*)p.o + x0 + (r0 + r < p.rows ? r * p.ldx : 0) + c, cnt);
   }
   float state[V] = {}, behind[V] = {};                            // h that enters the chunk; r that enters it from behind
   if (column) {
     const long long entry = (long long)(p.chunk0 + chunk) * p.channels;
     if (WAY == APPLY_FWD && p.in) load4(p.in + entry + c, cnt, state);
-    if (WAY == APPLY_BWD && p.kept) load4(p.kept + entry + c, cnt, state);
+    if (WAY == APPLY_BWD && p.kept) load4(p.kept + row0 / KEEP * p.channels + c, cnt, state);
     if (WAY == APPLY_BWD && p.in) load4(p.in + entry + p.channels + c, cnt, behind);
   }
-  const Marks m = marks<ROWS>(p, r0);
+  const auto m = [&]() __attribute__((always_inline)) {
+    if constexpr (NARROW) return own_marks<ROWS>(p, r0);
+    else return marks<ROWS>(p, r0);
+  }();
   auto of_sequence = [&](const float* t, int r, float (&v)[V]) __attribute__((always_inline)) {  // the values of row r's sequence, zeros where there are none
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.f;
-    if (t && column) load4(t + (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c, cnt, v);
+    if (t && column) load4(t + (long long)m.of(r) * p.channels + c, cnt, v);
   };
 
   // ---- the wave's spans ----
@@ -192,16 +232,46 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
         }
       }
   }
+  // runs of a wave: A, H become those of the runs up to this one, eA, eH of those before it; B, R of the runs from this one on, eB, eR of those behind it
+  float eA[V], eH[V], eB[V], eR[V];
+  if constexpr (NARROW) {
+    auto meet = [&](float (&a)[V], float (&h)[V], float (&ea)[V], float (&eh)[V], bool back) __attribute__((always_inline)) {
+      for (int d = 1; d < runs; d *= 2) {
+        const int from = back ? lane + d * p.lpr : lane - d * p.lpr;
+        const bool take = back ? run + d < runs : run >= d;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float oa = __shfl(a[e], from), oh = __shfl(h[e], from);
+          if (take) {
+            h[e] = through(a[e], oh, h[e]);
+            a[e] = product(oa, a[e]);
+          }
+        }
+      }
+      const int from = back ? lane + p.lpr : lane - p.lpr;
+      const bool edge = back ? run == runs - 1 : run == 0;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float oa = __shfl(a[e], from), oh = __shfl(h[e], from);
+        ea[e] = edge ? 1.f : oa;
+        eh[e] = edge ? 0.f : oh;
+      }
+    };
+    if constexpr (STATE) meet(A, H, eA, eH, false);
+    if constexpr (BWD) meet(B, R, eB, eR, true);
+  }
   auto put = [&](float (&t)[BLOCK], const float (&v)[V]) { *reinterpret_cast<float4*>(&t[at]) = make_float4(v[0], v[1], v[2], v[3]); };
-  if constexpr (STATE) { put(s_a[wave], A); put(s_h[wave], H); }
-  if constexpr (BWD) { put(s_b[wave], B); put(s_r[wave], R); }
+  if constexpr (STATE)
+    if (!NARROW || run == runs - 1) { put(s_a[wave], A); put(s_h[wave], H); }
+  if constexpr (BWD)
+    if (!NARROW || run == 0) { put(s_b[wave], B); put(s_r[wave], R); }
   __syncthreads();
   auto compose = [&](const float (&sa)[BLOCK], const float (&sh)[BLOCK], float (&v)[V]) __attribute__((always_inline)) {
     const float4 k = *reinterpret_cast<const float4*>(&sa[at]), d = *reinterpret_cast<const float4*>(&sh[at]);
     v[0] = through(k.x, v[0], d.x); v[1] = through(k.y, v[1], d.y); v[2] = through(k.z, v[2], d.z); v[3] = through(k.w, v[3], d.w);
   };
   if constexpr (WAY == SUM_FWD || WAY == SUM_BWD) {
-    if (wave != 0 || !column) return;
+    if (wave != 0 || run != 0 || !column) return;
     float k[V] = {1.f, 1.f, 1.f, 1.f}, d[V] = {};
     for (int i = 0; i < WAVES; ++i) {
       const int w = WAY == SUM_FWD ? i : WAVES - 1 - i;
@@ -244,7 +314,10 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
     anew(x);
     if constexpr (BWD) { anew(g); anew(o); }
     for (int w = 0; w < wave; ++w) compose(s_a[w], s_h[w], state);
-    auto entry_of = [&](int r) { return (long long)__builtin_amdgcn_readlane(m.seq, r) * p.channels + c; };
+    if constexpr (NARROW)
+#pragma unroll
+      for (int e = 0; e < V; ++e) state[e] = through(eA[e], state[e], eH[e]);
+    auto entry_of = [&](int r) { return (long long)m.of(r) * p.channels + c; };
     if constexpr (WAY == APPLY_FWD) {
       if (p.kept && r0 % KEEP == 0) store4(p.kept + r0 / KEEP * p.channels + c, cnt, state);
       auto finish = [&](auto act, auto with_gate) __attribute__((always_inline)) {
@@ -262,7 +335,7 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
             }
           }
           if (!(m.live >> r & 1)) continue;
-          store4((T*)p.y + (r0 + r) * p.ldy + c, cnt, y);
+          store4((T*)p.y + y0 + r * p.ldy + c, cnt, y);
           if ((m.last >> r & 1) && p.last) store4(p.last + entry_of(r), cnt, state);
         }
       };
@@ -279,6 +352,9 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
         for (int e = 0; e < V; ++e) h[r][e] = now[e] = mix(a[r][e], now[e], x[r].get(e));
       }
       for (int w = WAVES - 1; w > wave; --w) compose(s_b[w], s_r[w], behind);
+      if constexpr (NARROW)
+#pragma unroll
+        for (int e = 0; e < V; ++e) behind[e] = through(eB[e], behind[e], eR[e]);
       auto finish = [&](auto act, auto with_gate) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = ROWS - 1; r >= 0; --r) {
@@ -301,7 +377,7 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
               dout[e] = dy[r].get(e) * slope * h[r][e];
             }
           }
-          const long long to = (r0 + r) * p.ldx;
+          const long long to = x0 + r * p.ldx;
           if (p.dx) store4((T*)p.dx + to + c, cnt, dx);
           if (p.dg) store4((T*)p.dg + to + c, cnt, dg);
           if constexpr (decltype(with_gate)::value)
@@ -580,6 +656,13 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurP p, const int32_t
   if (cnt > 0) store4(to + (long long)slot * p.channels + c, cnt, h);
 }
 
+// Lanes of a row, and rows of a chunk: narrow rows leave a wave several runs.
+int lanes_of(int channels) {
+  int lanes = 1;
+  while (lanes < 64 && lanes * V < channels) lanes *= 2;
+  return lanes;
+}
+int chunk_of(const lms_recur_desc* d, bool bwd) { return (bwd ? CHUNK_BWD : CHUNK_FWD) * (64 / lanes_of(d->channels)); }
 long long chunks_of(long long rows, int chunk) { return rows <= chunk ? 1 : (rows + chunk - 1) / chunk; }
 // Chunks of one launch: 2^21 work-groups of up to 1024 threads are a grid.
 long long part_chunks(const lms_recur_desc* d) {
@@ -627,6 +710,8 @@ RecurP params(const lms_recur_desc* d, int chunk, const void* x, const void* g, 
   p.each = d->rows / d->seqs > 0 ? d->rows / d->seqs : 1;
   p.seqs = d->seqs; p.channels = d->channels; p.act = d->act;
   p.all_chunks = (int)chunks_of(d->rows, chunk);
+  p.lpr = lanes_of(d->channels);
+  p.subs = 64 / p.lpr;
   return p;
 }
 // No chunk needs what another leaves: one chunk, or whole sequences in each.
@@ -656,8 +741,9 @@ template <typename T, int WAY>
 hipError_t launch(const RecurP& p, hipStream_t s) {
   const int blocks = (p.channels + BLOCK - 1) / BLOCK;
   const dim3 grid((unsigned)(blocks * p.chunks)), threads((Shape<T, WAY>::NT));
-  if (p.channels >= V) hipLaunchKernelGGL((recur_kernel<T, WAY, true>), grid, threads, 0, s, p);
-  else hipLaunchKernelGGL((recur_kernel<T, WAY, false>), grid, threads, 0, s, p);
+  if (p.subs == 1) hipLaunchKernelGGL((recur_kernel<T, WAY, true, false>), grid, threads, 0, s, p);
+  else if (p.channels >= V) hipLaunchKernelGGL((recur_kernel<T, WAY, true, true>), grid, threads, 0, s, p);
+  else hipLaunchKernelGGL((recur_kernel<T, WAY, false, true>), grid, threads, 0, s, p);
   return hipGetLastError();
 }
 
@@ -698,7 +784,7 @@ lms_status recur_kept(const lms_recur_desc* d, uint64_t* bytes) {
 lms_status recur_workspace(const lms_recur_desc* d, int which, uint64_t* bytes) {
   if (const lms_status st = check("lms_recur_workspace_bytes", d, false)) return st;
   NEED(which == LMS_RECUR_FWD || which == LMS_RECUR_BWD, "lms_recur_workspace_bytes: unknown call %d", which);
-  const int chunk = which == LMS_RECUR_FWD ? CHUNK_FWD : CHUNK_BWD;
+  const int chunk = chunk_of(d, which == LMS_RECUR_BWD);
   *bytes = d->rows <= chunk ? 0 : sums_bytes(d, chunk) + in_bytes(d, chunk);
   return LMS_OK;
 }
@@ -714,12 +800,13 @@ lms_status recur_fwd(const lms_recur_desc* d, const void* x, const void* g, cons
   recur_workspace(d, LMS_RECUR_FWD, &need);
   NEED(!need || ws, "%s: workspace of %llu bytes required", what, (unsigned long long)need);
   NEED((((uintptr_t)ws | (uintptr_t)kept) & 15) == 0, "%s: the workspace is not aligned", what);
-  RecurP p = params(d, CHUNK_FWD, x, g, o, offsets, h0);
+  const int chunk = chunk_of(d, false);
+  RecurP p = params(d, chunk, x, g, o, offsets, h0);
   p.y = y; p.last = last;
   p.kept = d->rows <= CHUNK_BWD ? nullptr : (float*)kept;
   p.sums = (float*)ws;
-  p.in = (float*)((char*)ws + sums_bytes(d, CHUNK_FWD));
-  const bool whole = alone(d, CHUNK_FWD, offsets);
+  p.in = (float*)((char*)ws + sums_bytes(d, chunk));
+  const bool whole = alone(d, chunk, offsets);
   const long long part = part_chunks(d);
   hipStream_t s = (hipStream_t)stream;
   if (walks(d, offsets)) return done(what, walk<false>(d, p, s));
@@ -734,21 +821,22 @@ lms_status recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, con
   if (const lms_status st = aligned(what, d, {dy, x, g, o, dx, dg, dout}, {offsets, h0, dlast, dh0})) return st;
   NEED(o || !dout, "%s: the gradient of o needs o", what);
   NEED(!overlap(d, dlast, dh0) && !overlap(d, h0, dh0), "%s: the gradient of the initial states must not overlap the states or the gradient of the last ones", what);
-  const bool whole = alone(d, CHUNK_BWD, offsets);
+  const int chunk = chunk_of(d, true);
+  const bool walking = walks(d, offsets), whole = !walking && alone(d, chunk, offsets);
   NEED(whole || kept, "%s: what the forward pass kept is needed", what);
   uint64_t need = 0;
   recur_workspace(d, LMS_RECUR_BWD, &need);
   NEED(!need || ws, "%s: workspace of %llu bytes required", what, (unsigned long long)need);
   NEED((((uintptr_t)ws | (uintptr_t)kept) & 15) == 0, "%s: the workspace is not aligned", what);
-  RecurP p = params(d, CHUNK_BWD, x, g, o, offsets, h0);
+  RecurP p = params(d, chunk, x, g, o, offsets, h0);
   p.dy = dy; p.dlast = dlast;
   p.dx = dx; p.dg = dg; p.dout = dout; p.dh0 = dh0;
   p.kept = whole ? nullptr : (float*)const_cast<void*>(kept);
   p.sums = (float*)ws;
-  p.in = (float*)((char*)ws + sums_bytes(d, CHUNK_BWD));
+  p.in = (float*)((char*)ws + sums_bytes(d, chunk));
   const long long part = part_chunks(d);
   hipStream_t s = (hipStream_t)stream;
-  if (walks(d, offsets)) return done(what, walk<true>(d, p, s));
+  if (walking) return done(what, walk<true>(d, p, s));
   return done(what, d->dtype == LMS_F32 ? line<float, true>(p, whole, part, s) : line<uint16_t, true>(p, whole, part, s));
 }
 

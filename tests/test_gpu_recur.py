@@ -15,7 +15,11 @@ CASES = [(1, [1], None, "fp32", 0), (4, [0, 0], "silu", "bf16", 0), (5, [3, 0, 1
          (300, (1500, 1), "silu", "bf16", 0), (16, [700, 0, 3, 900], None, "bf16", 0), (260, (192, 3), None, "fp32", 0),
          # work-groups that walk along sequences: steps of 64 rows that end in them, begin and end with them, pairs of channels that overlap
          (8190, (3 * 100, 3), "silu", "bf16", 2), (24577, (129, 1), "gelu", "fp32", 0), (2050, (12 * 65, 12), "relu", "bf16", 0), (130, (100 * 192, 100), None, "bf16", 1),
-         (256, (96 * 224, 96), "gelu_tanh", "fp32", 0)]
+         (256, (96 * 224, 96), "gelu_tanh", "fp32", 0),
+         # few channels: several runs of rows in a wave, in one and in several chunks
+         (1, [3000, 0, 5000, 1, 777], "silu", "bf16", 0), (2, [9001], None, "fp32", 0), (3, (4200, 6), "gelu", "bf16", 1), (16, (3 * 1300, 3), "relu", "fp32", 0), (33, (5000, 2), "silu", "bf16", 3),
+         (100, ODD, "gelu_tanh", "fp32", 0), (128, ODD * 3, "silu", "bf16", 0), (64, [1] * 300 + [0] * 9 + [4] * 50, "none", "bf16", 0), (20, (50, 1), "silu", "bf16", 0), (7, [40], "silu", "fp32", 0),
+         (600, [50], "silu", "bf16", 0), (16, (64 * 128, 64), "silu", "bf16", 0)]
 
 
 def make(torch, seed, c, lengths, act, dtype, pad):

@@ -14,11 +14,11 @@ def refused(call, *args, match):
 
 
 def recur(**kw):
-    return L.recur_desc(**{**dict(rows=200, channels=12, seqs=4), **kw})
+    return L.recur_desc(**{**dict(rows=200, channels=300, seqs=4), **kw})
 
 
 BAD_RECUR = [(dict(rows=-1), "rows must be"), (dict(channels=0), "channels"), (dict(seqs=0), "sequences"), (dict(rows=(1 << 31) - 1), "rows"), (dict(channels=(1 << 26) + 1), "channels"),
-             (dict(seqs=(1 << 30) + 1), "sequences"), (dict(act=5), "activation"), (dict(dtype=A.I32), "dtype"), (dict(ldx=11), "pitch"), (dict(ldy=11), "pitch"),
+             (dict(seqs=(1 << 30) + 1), "sequences"), (dict(act=5), "activation"), (dict(dtype=A.I32), "dtype"), (dict(ldx=299), "pitch"), (dict(ldy=299), "pitch"),
              (dict(ldy=(1 << 40) + 1), "pitch")]
 
 
@@ -34,7 +34,7 @@ def test_recur_descriptors(kw, match):
 
 def test_recur_calls():
     d = recur()
-    n = 4 * 12 * 4
+    n = 4 * 300 * 4
     refused(L.recur_workspace_bytes, d, 2, match="unknown call")
     refused(L.recur_fwd, d, None, PTR, None, PTR, None, PTR, None, PTR, PTR, None, match="null argument")
     refused(L.recur_fwd, d, PTR, PTR, None, PTR, None, PTR, None, PTR, None, None, match="workspace of")
@@ -59,7 +59,7 @@ def test_recur_calls():
 
 def test_recur_sizes():
     assert L.recur_kept_bytes(recur(rows=32)) == 0 and L.recur_workspace_bytes(recur(rows=32), A.RECUR_FWD) == 0
-    assert L.recur_kept_bytes(recur(rows=65)) >= 3 * 12 * 4
+    assert L.recur_kept_bytes(recur(rows=65)) >= 3 * 300 * 4
     small, large = (L.recur_workspace_bytes(recur(rows=r, channels=1000), A.RECUR_BWD) for r in (1000, 1000000))
     assert small < large < 1000000 * 1000 * 2 // 4
     # sizes of 64 bits
