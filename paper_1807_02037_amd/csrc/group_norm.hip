@@ -833,17 +833,17 @@ __global__ __launch_bounds__(NT, sizeof(T) * K <= 8 ? 4 : 2) void norm_image_ker
         }
     });
   } else {
-    float da[W] = {}, db[W] = {};
-    with_act(p.act, [&](auto act) {
+    float da[W] = {}, db[W] = {}, dv[K][W];                       // dv stays, in the place of dy; xhat is computed anew from x
+    with_act(p.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < K; ++j) {
-        float hat[W], dv[W];
-        slope8<decltype(act)::value, T>(ga, be, mean, rstd, x[j], dy[j], hat, dv);
+        float hat[W];
+        slope8<decltype(act)::value, T>(ga, be, mean, rstd, x[j], dy[j], hat, dv[j]);
         if (have(j))
 #pragma unroll
           for (int e = 0; e < W; ++e) {
-            db[e] += dv[e];
-            da[e] = __builtin_fmaf(dv[e], hat[e], da[e]);
+            db[e] += dv[j][e];
+            da[e] = __builtin_fmaf(dv[j][e], hat[e], da[e]);
           }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -865,19 +865,18 @@ __global__ __launch_bounds__(NT, sizeof(T) * K <= 8 ? 4 : 2) void norm_image_ker
       }
     if (!p.out) return;
     anew(x);
-    anew(dy);
-    with_act(p.act, [&](auto act) {
 #pragma unroll
-      for (int j = 0; j < K; ++j)
-        if (have(j)) {
-          float hat[W], dv[W];
-          slope8<decltype(act)::value, T>(ga, be, mean, rstd, x[j], dy[j], hat, dv);
+    for (int j = 0; j < K; ++j)
+      if (have(j)) {
+        float d[W];
 #pragma unroll
-          for (int e = 0; e < W; ++e) dv[e] = rstd * (__builtin_fmaf(ga[e], dv[e], -a * inv) - hat[e] * (b * inv));
-          store8(out + j * (lanes * p.ldo), W, dv);
-          __builtin_amdgcn_sched_barrier(0);                      // one vector after the other: registers
+        for (int e = 0; e < W; ++e) {
+          const float hat = (x[j].get(e) - mean) * rstd;
+          d[e] = rstd * (__builtin_fmaf(ga[e], dv[j][e], -a * inv) - hat * (b * inv));
         }
-    });
+        store8(out + j * (lanes * p.ldo), W, d);
+        __builtin_amdgcn_sched_barrier(0);                        // one vector after the other: registers
+      }
   }
 }
 
