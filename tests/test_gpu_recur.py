@@ -287,3 +287,25 @@ def test_streams_and_graphs():
                 assert torch.equal(a[k], b[k]), k
                 a[k].fill_(777.0)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("c,lengths", [(300, ODD), (40, ODD), (130, (100 * 192, 100))])
+def test_gradients_that_are_not_asked_for(c, lengths):
+    import torch
+    import paper_1807_02037_amd as L
+    A = L.abi
+    d = make(torch, 6, c, lengths, "silu", "bf16", 0)
+    full = call(torch, L, d, c, "silu", 0)
+    s = torch.cuda.current_stream().cuda_stream
+    desc = L.recur_desc(d["rows"], c, d["seqs"], act=A.ACT_SILU)
+    kept = torch.empty(L.recur_kept_bytes(desc) + 16, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(max(L.recur_workspace_bytes(desc, w) for w in (0, 1)) + 16, dtype=torch.uint8, device="cuda")
+    y = torch.full_like(full["y"], 777.0)
+    L.recur_fwd(desc, ptr(d["x"]), ptr(d["g"]), ptr(d["o"]), ptr(d["offsets"]), ptr(d["h0"]), ptr(y), None, None, ptr(ws), s)
+    assert torch.equal(y, full["y"])                               # without the last states, nothing kept
+    L.recur_fwd(desc, ptr(d["x"]), ptr(d["g"]), ptr(d["o"]), ptr(d["offsets"]), ptr(d["h0"]), ptr(y), None, ptr(kept), ptr(ws), s)
+    for name in ("dx", "dg", "do", "dh0"):
+        got = {name: torch.full_like(full[name], 777.0)}
+        L.recur_bwd(desc, ptr(d["dy"]), ptr(d["x"]), ptr(d["g"]), ptr(d["o"]), ptr(d["offsets"]), ptr(d["h0"]), ptr(kept), ptr(d["dlast"]),
+                    *(ptr(got.get(n)) for n in ("dx", "dg", "do", "dh0")), ptr(ws), s)
+        assert torch.equal(got[name], full[name]), name
