@@ -35,43 +35,42 @@ struct RecurP {
   long long rows, ldx, ldy, each;      // each: rows of a sequence where there are no offsets
   int seqs, channels, act;
   int chunk0, chunks, all_chunks;      // chunks of this launch
+  int direct;                  // few chunks: each composes those that come before it out of sums itself, and there is no `in`
   int lpr, subs;               // lanes of a row, a power of two; runs of rows of a wave, 64 / lpr
 };
 
-// Rows of a run: which begin a sequence, which end one, which belong to one.  Of a whole wave: the same for all lanes, and lane r holds the sequence of row r.
-template <int ROWS, bool NARROW>
+// Rows of a run, of a whole wave the same for all lanes: which begin a sequence, which end one, which belong to one, and which one.
+template <int ROWS>
 struct Marks {
   unsigned first, last, live;
-  int seq[NARROW ? ROWS : 1];
-  __device__ __forceinline__ int of(int r) const {
-    if constexpr (NARROW) return seq[r];
-    else return __builtin_amdgcn_readlane(seq[0], r);
-  }
+  int seq[ROWS];
 };
+// The borders are read as constants: for a whole wave by scalar loads, which do not wait for the rows that are on their way.
+typedef const __attribute__((address_space(4))) int32_t* Borders;
 // The last sequence that begins at or before the row; of several at the same place all but the last are empty.  -1: none.
 __device__ __forceinline__ int sequence_of(const RecurP& p, long long row) {
   int lo = -1, hi = p.seqs + 1;                                   // offsets[lo] <= row < offsets[hi]
   while (hi - lo > 1) {
     const int mid = lo + (hi - lo) / 2;
-    if (p.offsets[mid] <= row) lo = mid;
+    if (((Borders)(uintptr_t)p.offsets)[mid] <= row) lo = mid;
     else hi = mid;
   }
   return lo;
 }
-// Of each lane's own run.
 template <int ROWS>
-__device__ __forceinline__ Marks<ROWS, true> own_marks(const RecurP& p, long long r0) {
-  Marks<ROWS, true> m = {0u, 0u, 0u, {}};
+__device__ __forceinline__ Marks<ROWS> marks(const RecurP& p, long long r0) {
+  Marks<ROWS> m = {0u, 0u, 0u, {}};
   if (r0 >= p.rows) return m;
+  const Borders off = (Borders)(uintptr_t)p.offsets;
   int s = p.offsets ? sequence_of(p, r0) : (int)(r0 / p.each);
-  long long begin = p.offsets ? (s >= 0 ? p.offsets[s] : 0) : s * p.each, next = p.offsets ? (s < p.seqs ? p.offsets[s + 1] : 0) : begin + p.each;
+  long long begin = p.offsets ? (s >= 0 ? off[s] : 0) : s * p.each, next = p.offsets ? (s < p.seqs ? off[s + 1] : 0) : begin + p.each;
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     const long long row = r0 + r;
     while (s < p.seqs && next <= row) {                           // on to the sequence of this row
       ++s;
       begin = next;
-      next = p.offsets ? (s < p.seqs ? p.offsets[s + 1] : 0) : begin + p.each;
+      next = p.offsets ? (s < p.seqs ? off[s + 1] : 0) : begin + p.each;
     }
     const bool live = row < p.rows && s >= 0 && s < p.seqs;
     m.live |= (unsigned)live << r;
@@ -80,29 +79,6 @@ __device__ __forceinline__ Marks<ROWS, true> own_marks(const RecurP& p, long lon
     m.seq[r] = live ? s : 0;
   }
   return m;
-}
-template <int ROWS>
-__device__ __forceinline__ Marks<ROWS, false> marks(const RecurP& p, long long r0) {
-  const int lane = threadIdx.x & 63;
-  const long long row = r0 + lane;
-  bool first = false, last = false, live = lane < ROWS && row < p.rows;
-  int s = 0;
-  if (live) {
-    if (p.offsets) {
-      s = sequence_of(p, row);
-      live = s >= 0 && s < p.seqs;
-      if (live) {
-        first = p.offsets[s] == row;
-        last = p.offsets[s + 1] == row + 1;
-      }
-    } else {
-      s = (int)(row / p.each);
-      const long long at = row - s * p.each;
-      first = at == 0;
-      last = at == p.each - 1;
-    }
-  }
-  return Marks<ROWS, false>{(unsigned)__ballot(first), (unsigned)__ballot(last), (unsigned)__ballot(live), {s}};
 }
 
 // 1 - a for a = sigmoid(g), without its cancellation: the exponential that a has below its line, times a.  Beyond 2^100 it is cut: a is then nothing against any state, and the rest 1.
@@ -172,14 +148,32 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
     if (WAY == APPLY_BWD && p.kept) load4(p.kept + row0 / KEEP * p.channels + c, cnt, state);
     if (WAY == APPLY_BWD && p.in) load4(p.in + entry + p.channels + c, cnt, behind);
   }
-  const auto m = [&]() __attribute__((always_inline)) {
-    if constexpr (NARROW) return own_marks<ROWS>(p, r0);
-    else return marks<ROWS>(p, r0);
-  }();
+  if constexpr (WAY == APPLY_FWD || WAY == APPLY_BWD)
+    if (p.direct && column) {
+      constexpr int IN_FLIGHT = 4;
+      float (&v)[V] = BWD ? behind : state;
+      const int before = BWD ? p.chunks - 1 - chunk : chunk;
+      for (int i0 = 0; i0 < before; i0 += IN_FLIGHT) {
+        float ka[IN_FLIGHT][V], kh[IN_FLIGHT][V];
+#pragma unroll
+        for (int u = 0; u < IN_FLIGHT; ++u) {
+          const int i = i0 + u < before ? i0 + u : i0;
+          const float* from = p.sums + (long long)(BWD ? p.chunks - 1 - i : i) * 2 * p.channels + c;
+          load4(from, cnt, ka[u]);
+          load4(from + p.channels, cnt, kh[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < IN_FLIGHT; ++u)
+          if (i0 + u < before)
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = through(ka[u][e], v[e], kh[u][e]);
+      }
+    }
+  const Marks<ROWS> m = marks<ROWS>(p, r0);
   auto of_sequence = [&](const float* t, int r, float (&v)[V]) __attribute__((always_inline)) {  // the values of row r's sequence, zeros where there are none
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.f;
-    if (t && column) load4(t + (long long)m.of(r) * p.channels + c, cnt, v);
+    if (t && column) load4(t + (long long)m.seq[r] * p.channels + c, cnt, v);
   };
 
   // ---- the wave's spans ----
@@ -317,7 +311,7 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
     if constexpr (NARROW)
 #pragma unroll
       for (int e = 0; e < V; ++e) state[e] = through(eA[e], state[e], eH[e]);
-    auto entry_of = [&](int r) { return (long long)m.of(r) * p.channels + c; };
+    auto entry_of = [&](int r) { return (long long)m.seq[r] * p.channels + c; };
     if constexpr (WAY == APPLY_FWD) {
       if (p.kept && r0 % KEEP == 0) store4(p.kept + r0 / KEEP * p.channels + c, cnt, state);
       auto finish = [&](auto act, auto with_gate) __attribute__((always_inline)) {
@@ -747,6 +741,10 @@ hipError_t launch(const RecurP& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Chunks up to which a launch for the states between them is not worth it (us, forward + backward, with it / without: 256 x 1024 in bf16 16.4 + 17.2 / 14.6 + 15.6, 512 x 960 16.9 + 18.4 / 15.1 + 17.2;
+// of 32 chunks, 1024 x 1024 backward 19.4 / 21.3).
+constexpr int DIRECT = 16;
+
 // in: entries of the states between chunks, sums: of a part.
 template <typename T, bool BWD>
 hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
@@ -760,7 +758,9 @@ hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
     if (!alone) {
       e = launch<T, BWD ? SUM_BWD : SUM_FWD>(p, s);
       if (e != hipSuccess) return e;
-      hipLaunchKernelGGL(recur_join_kernel<BWD>, dim3((unsigned)((p.channels + 63) / 64)), dim3(64 * JOIN_SPANS), 0, s, p);
+      p.direct = p.all_chunks <= DIRECT;
+      if (p.direct) p.in = nullptr;
+      else hipLaunchKernelGGL(recur_join_kernel<BWD>, dim3((unsigned)((p.channels + 63) / 64)), dim3(64 * JOIN_SPANS), 0, s, p);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
