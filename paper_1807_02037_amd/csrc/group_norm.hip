@@ -397,7 +397,7 @@ struct ResidentP {
   NormP n;
   long long samples;
   int lanes;                           // tokens: lanes of a row, a power of two
-  int span;                            // tokens: lanes among which a group meets by shuffles, or 0
+  int span, parts;                     // tokens: lanes that meet by shuffles, a power of two, and how many such make a group
   int block, blocks;                   // images: vectors of a work-group's channels, and how many such blocks there are
   int gv;                              // vectors of a group
 };
@@ -435,13 +435,16 @@ __device__ __forceinline__ void weights8(const NormP& p, int c, bool there, floa
   if (there && p.beta) load8(p.beta + c, W, be);
 }
 
-// Tokens (s = 1).  A row takes `lanes` lanes of K vectors each; rows of a work-group run in parallel, and it goes on to others, the next row's loads out before this one is worked on.  Groups whose
-// vectors are a power of two of lanes of one wave, or all of them, meet by shuffles, others in LDS.  Backwards the sums for gamma and beta stay in registers until the work-group's last row.
+// Tokens (s = 1).  A row takes `lanes` lanes of K vectors each; rows of a work-group run in parallel, and it goes on to others, the next row's loads out before this one is worked on.  A group's
+// vectors meet by shuffles, as far as its lanes go in powers of two within a wave, the rest in LDS, in two buffers by turns: one barrier for up to DIRECT parts, which every thread adds up for itself
+// (8192 x 4096 in one group, forward 54 us with a barrier for each of three steps, 42 so).  Backwards the sums for gamma and beta stay in registers until the work-group's last row.
 template <typename T, int NT, int K, bool BWD>
 __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
-  __shared__ float s_part[2][NT * K], s_sum[2][NT * K];
+  constexpr int DIRECT = 16;
+  __shared__ float s_part[2][2][NT * K], s_sum[2][2][NT * K / DIRECT];
   const NormP& p = q.n;
-  const int tid = threadIdx.x, l = tid & (q.lanes - 1), sub = tid / q.lanes, rows = NT / q.lanes, nv = p.c / W;
+  const int tid = threadIdx.x, l = tid & (q.lanes - 1), sub = tid / q.lanes, rows = NT / q.lanes, nv = p.c / W, each = q.lanes * K / q.span;     // each: parts of a row
+  int buffer = 0;
   auto vec = [&](int j) { return l + j * q.lanes; };
   float ga[K][W], be[K][W], da[BWD ? K : 1][W] = {}, db[BWD ? K : 1][W] = {};
 #pragma unroll
@@ -462,44 +465,71 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
     }
   };
   // a[j] and b[j] of each vector into the sums over its group
+  const bool fold = K > 1 && p.groups == 1;                       // a thread's vectors are of one group
   auto join = [&](float (&a)[K], float (&b)[K], bool two) {
-    if (q.span) {
-      for (int d = 1; d < q.span; d *= 2)
+    if (fold) {
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-          a[j] += __shfl_xor(a[j], d);
-          if (two) b[j] += __shfl_xor(b[j], d);
+      for (int j = 1; j < K; ++j) {
+        a[0] += a[j];
+        b[0] += b[j];
+        a[j] = b[j] = 0.f;
+      }
+    }
+    for (int d = 1; d < q.span; d *= 2)
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        a[j] += __shfl_xor(a[j], d);
+        if (two) b[j] += __shfl_xor(b[j], d);
+      }
+    if (q.parts == 1) return;
+    float (&part)[2][NT * K] = s_part[buffer], (&sum)[2][NT * K / DIRECT] = s_sum[buffer];
+    buffer ^= 1;
+    if (l % q.span == 0)
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        part[0][sub * each + vec(j) / q.span] = a[j];
+        part[1][sub * each + vec(j) / q.span] = b[j];
+      }
+    __syncthreads();                                              // this buffer's last readers have come through the other's barrier since
+    if (q.parts <= DIRECT) {
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (fold && j > 0) {
+          a[j] = a[0];
+          b[j] = b[0];
+          continue;
         }
+        a[j] = b[j] = 0.f;
+        if (vec(j) >= nv) continue;
+        const int at = sub * each + vec(j) / q.gv * q.parts;
+        for (int k = 0; k < (fold ? q.lanes / q.span : q.parts); ++k) {
+          a[j] += part[0][at + k];
+          b[j] += part[1][at + k];
+        }
+      }
       return;
     }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < K; ++j) {
-      s_part[0][sub * q.lanes * K + vec(j)] = a[j];
-      s_part[1][sub * q.lanes * K + vec(j)] = b[j];
-    }
-    __syncthreads();
     int team = 1;
-    while (team < 64 && team < q.gv && 2 * team * rows * p.groups <= NT) team *= 2;
+    while (team < 64 && team < q.parts && 2 * team * rows * p.groups <= NT) team *= 2;
     for (int i = tid / team; i < rows * p.groups; i += NT / team) {
-      const int at = i / p.groups * q.lanes * K + i % p.groups * q.gv;
+      const int at = i / p.groups * each + i % p.groups * q.parts;
       float ta = 0.f, tb = 0.f;
-      for (int k = tid & (team - 1); k < q.gv; k += team) {
-        ta += s_part[0][at + k];
-        tb += s_part[1][at + k];
+      for (int k = tid & (team - 1); k < q.parts; k += team) {
+        ta += part[0][at + k];
+        tb += part[1][at + k];
       }
       for (int d = 1; d < team; d *= 2) {
         ta += __shfl_xor(ta, d);
         tb += __shfl_xor(tb, d);
       }
-      if ((tid & (team - 1)) == 0) { s_sum[0][i] = ta; s_sum[1][i] = tb; }
+      if ((tid & (team - 1)) == 0) { sum[0][i] = ta; sum[1][i] = tb; }
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < K; ++j)
       if (vec(j) < nv) {
-        a[j] = s_sum[0][sub * p.groups + vec(j) / q.gv];
-        b[j] = s_sum[1][sub * p.groups + vec(j) / q.gv];
+        a[j] = sum[0][sub * p.groups + vec(j) / q.gv];
+        b[j] = sum[1][sub * p.groups + vec(j) / q.gv];
       }
   };
   constexpr bool AHEAD = !BWD || NT < 1024;                       // registers
@@ -584,14 +614,24 @@ __global__ __launch_bounds__(NT) void norm_tokens_kernel(ResidentP q) {
     }
   }
   if constexpr (BWD)
-    if (p.part)
+    if (p.part) {                                                 // the rows of a wave together first
+      const int subs = q.lanes < 64 ? 64 / q.lanes : 1;
+      for (int d = q.lanes; d < 64; d *= 2)
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            db[j][e] += __shfl_xor(db[j][e], d);
+            da[j][e] += __shfl_xor(da[j][e], d);
+          }
 #pragma unroll
       for (int j = 0; j < K; ++j)
-        if (vec(j) < nv) {
-          float* to = p.part + ((long long)blockIdx.x * rows + sub) * 2 * p.c + vec(j) * W;
+        if (vec(j) < nv && sub % subs == 0) {
+          float* to = p.part + ((long long)blockIdx.x * (rows / subs) + sub / subs) * 2 * p.c + vec(j) * W;
           store8(to, W, db[j]);
           store8(to + p.c, W, da[j]);
         }
+    }
 }
 
 // Tokens whose groups, or rows, are not of whole vectors: the channels' values go through LDS, where a team of lanes sums each group's.
@@ -885,27 +925,28 @@ __global__ __launch_bounds__(NT, sizeof(T) * K <= 8 ? 4 : 2) void norm_image_ker
   }
 }
 
-// dbeta and dgamma from the sums of all samples' chunks, in order.
-__global__ __launch_bounds__(256) void norm_weights_kernel(const float* part, long long rows, int c, float* dgamma, float* dbeta) {
-  __shared__ float sums[8][32];
+// dbeta and dgamma from the sums of all samples' chunks, in order, 32 runs of rows at a time (with 8, and a row of sums for each of a wave's rows, 32768 x 256 in one group took 39 us backward, now 19).
+constexpr int WAYS = 32;
+__global__ __launch_bounds__(32 * WAYS) void norm_weights_kernel(const float* part, long long rows, int c, float* dgamma, float* dbeta) {
+  __shared__ float sums[WAYS][32];
   const int lane = threadIdx.x & 31, way = threadIdx.x >> 5;
   const long long n = (long long)blockIdx.x * 32 + lane;          // column of 2 c
   float t = 0.f;
   if (n < 2LL * c) {
     long long i = way;
-    for (; i + 56 < rows; i += 64) {
+    for (; i + 7 * WAYS < rows; i += 8 * WAYS) {
       float v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = part[(i + 8 * u) * 2 * c + n];
+      for (int u = 0; u < 8; ++u) v[u] = part[(i + u * WAYS) * 2 * c + n];
       t += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     }
-    for (; i < rows; i += 8) t += part[i * 2 * c + n];
+    for (; i < rows; i += WAYS) t += part[i * 2 * c + n];
   }
   sums[way][lane] = t;
   __syncthreads();
   if (way != 0 || n >= 2LL * c) return;
 #pragma unroll
-  for (int w = 1; w < 8; ++w) t += sums[w][lane];
+  for (int w = 1; w < WAYS; ++w) t += sums[w][lane];
   if (n < c) { if (dbeta) dbeta[n] = t; }
   else if (dgamma) dgamma[n - c] = t;
 }
@@ -935,11 +976,13 @@ long long part_samples(const lms_group_norm_desc* d, const Split& t) {
 // How a work-group holds samples, if it does: from the sizes and the type alone.
 enum { NOT_HELD, TOKENS, TOKENS_ANY, IMAGES };
 struct Held {
-  int kind, nt, k, lanes, span, block, blocks;
-  long long grid, rows;                // rows of sums for gamma and beta
+  int kind, nt, k, lanes, span, parts, block, blocks;
+  long long grid, grid_fwd, rows;      // rows of sums for gamma and beta
   unsigned lds;
 };
-constexpr int TOKEN_GROUPS = 512;      // work-groups that go through the tokens
+// Work-groups that go through the tokens.  Forward more of them, with at least four rounds of rows each (32768 x 1024 in 8 groups 50 -> 34 us, 2048 x 4096 with one round each 15 against 12 us);
+// backward each leaves its sums for gamma and beta.
+constexpr int TOKEN_GROUPS = 512, TOKEN_GROUPS_FWD = 2048;
 Held held_of(const lms_group_norm_desc* d) {
   Held h{};
   const int cg = d->c / d->groups, nv = (d->c + W - 1) / W, gv = cg / W;
@@ -953,10 +996,16 @@ Held held_of(const lms_group_norm_desc* d) {
     else return h;
     const long long rows = h.nt / h.lanes, need = (d->n + rows - 1) / rows;
     h.kind = cg % W ? TOKENS_ANY : TOKENS;
-    h.span = cg % W ? 0 : (gv & (gv - 1)) == 0 && gv <= 64 ? gv : d->groups == 1 && h.lanes <= 64 ? h.lanes : 0;
+    for (h.span = 1; h.kind == TOKENS && h.span < 64 && gv % (2 * h.span) == 0;) h.span *= 2;
+    h.parts = h.kind == TOKENS ? gv / h.span : 0;
+    if (h.kind == TOKENS && d->groups == 1 && h.lanes <= 64) {     // the lanes behind the last vector have zeros
+      h.span = h.lanes;
+      h.parts = 1;
+    }
     h.lds = h.kind == TOKENS_ANY ? (unsigned)(h.nt * h.k * W * 8 + rows * d->groups * 8) : 0;
     h.grid = need < TOKEN_GROUPS ? need : TOKEN_GROUPS;
-    h.rows = h.grid * rows;
+    h.grid_fwd = need / 4 < TOKEN_GROUPS ? h.grid : need / 4 < TOKEN_GROUPS_FWD ? need / 4 : TOKEN_GROUPS_FWD;
+    h.rows = h.grid * (h.kind == TOKENS && h.lanes < 64 ? h.nt / 64 : rows);
     return h;
   }
   if (cg % W) return h;
@@ -976,7 +1025,7 @@ Held held_of(const lms_group_norm_desc* d) {
     h.kind = IMAGES;
     h.nt = nt;
     h.k = k <= 2 ? 2 : k <= 4 ? 4 : 8;
-    h.grid = d->n * h.blocks;
+    h.grid = h.grid_fwd = d->n * h.blocks;
     h.rows = d->n;
     return h;
   }
@@ -1013,8 +1062,8 @@ NormP params(const lms_group_norm_desc* d, const Split& t) {
 
 template <typename T, bool BWD>
 hipError_t resident(const lms_group_norm_desc* d, const Held& h, const NormP& p, hipStream_t s) {
-  ResidentP q{p, d->n, h.lanes, h.span, h.block, h.blocks, p.cg / W};
-  const dim3 grid((unsigned)h.grid);
+  ResidentP q{p, d->n, h.lanes, h.span, h.parts, h.block, h.blocks, p.cg / W};
+  const dim3 grid((unsigned)(BWD ? h.grid : h.grid_fwd));
 #define TOKEN(NT, K) if (h.kind == TOKENS && h.nt == NT && h.k == K) hipLaunchKernelGGL((norm_tokens_kernel<T, NT, K, BWD>), grid, dim3(NT), 0, s, q)
 #define IMAGE(NT, K) if (h.kind == IMAGES && h.nt == NT && h.k == K) hipLaunchKernelGGL((norm_image_kernel<T, NT, K, BWD>), grid, dim3(NT), 0, s, q)
 #define ANY(NT, K)                                                                                                                                                 \
@@ -1059,7 +1108,7 @@ hipError_t forward(const lms_group_norm_desc* d, const Split& t, NormP& p, hipSt
 }
 
 hipError_t sum_weights(const float* part, long long rows, int c, float* dgamma, float* dbeta, hipStream_t s) {
-  hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2LL * c + 31) / 32)), dim3(256), 0, s, part, rows, c, dgamma, dbeta);
+  hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((2LL * c + 31) / 32)), dim3(32 * WAYS), 0, s, part, rows, c, dgamma, dbeta);
   return hipGetLastError();
 }
 

@@ -17,7 +17,10 @@ CASES = [(1, 1, 1, 1, "none", True, "fp32", 0), (3, 1, 8, 8, "silu", True, "bf16
          # tokens whose rows are all of a group, of no power of two of vectors; groups and rows that are not of whole vectors; images of few positions
          (700, 1, 192, 1, "gelu", True, "bf16", 0), (33, 1, 440, 1, "silu", True, "fp32", 1), (1500, 1, 576, 16, "gelu", True, "bf16", 0), (90, 1, 1001, 7, "silu", True, "fp32", 3),
          (21, 1, 4100, 41, "relu", False, "bf16", 0), (19, 1, 8190, 2, "gelu_tanh", True, "bf16", 2), (5, 1, 7000, 7000, "none", True, "bf16", 0), (3000, 1, 12, 4, "silu", True, "fp32", 0),
-         (50, 2, 1024, 32, "silu", True, "bf16", 0), (33, 3, 64, 8, "relu", True, "fp32", 0), (9, 7, 8, 1, "none", True, "bf16", 0), (6, 30, 2048, 2, "gelu", True, "bf16", 8)]
+         (50, 2, 1024, 32, "silu", True, "bf16", 0), (33, 3, 64, 8, "relu", True, "fp32", 0), (9, 7, 8, 1, "none", True, "bf16", 0), (6, 30, 2048, 2, "gelu", True, "bf16", 8),
+         # parts of groups in several waves, a thread's vectors of one group, more rows than work-groups
+         (700, 1, 4096, 1, "silu", True, "bf16", 0), (40, 1, 6000, 1, "none", True, "fp32", 0), (33, 1, 8192, 2, "relu", True, "bf16", 0), (12, 1, 16384, 1, "gelu", True, "bf16", 0),
+         (9, 1, 12000, 3, "silu", True, "fp32", 0), (9000, 1, 64, 2, "silu", True, "bf16", 0), (2600, 1, 2048, 1, "none", False, "bf16", 0), (50, 1, 1000, 5, "gelu", True, "fp32", 0)]
 
 
 def ptr(t):

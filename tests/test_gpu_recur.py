@@ -149,12 +149,13 @@ def test_gates_at_their_ends():
     assert not out["dx"][:, 0].any() and torch.equal(out["dx"][:, 1], d["dy"][:, 1] + torch.nn.functional.one_hot(torch.tensor([95] * 96), 96)[0].cuda() * d["dlast"][0, 1])
 
 
-def test_a_sequence_keeps_its_nan_to_itself():
+@pytest.mark.parametrize("c", [12, 300])
+def test_a_sequence_keeps_its_nan_to_itself(c):
     import torch
     import paper_1807_02037_amd as L
     lengths = [70, 5, 64, 3, 200, 9]
-    d = make(torch, 2, 12, lengths, "silu", "fp32", 0)
-    clean = call(torch, L, d, 12, "silu", 0)
+    d = make(torch, 2, c, lengths, "silu", "fp32", 0)
+    clean = call(torch, L, d, c, "silu", 0)
     bad = dict(d)
     bad["x"], bad["dy"], bad["g"] = d["x"].clone(), d["dy"].clone(), d["g"].clone()
     off = [0] + list(np.cumsum(lengths))
@@ -162,7 +163,7 @@ def test_a_sequence_keeps_its_nan_to_itself():
         bad["x"][off[s]] = float("nan")
         bad["g"][off[s] + 1] = float("nan")
         bad["dy"][off[s + 1] - 1] = float("nan")
-    got = call(torch, L, bad, 12, "silu", 0)
+    got = call(torch, L, bad, c, "silu", 0)
     torch.cuda.synchronize()
     for s in (1, 3, 5):
         for n in ("y", "dx", "dg", "do"):
