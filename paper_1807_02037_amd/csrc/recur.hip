@@ -385,36 +385,39 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
   }
 }
 
-// The states that enter the chunks chunk0 .. chunk0 + chunks of the line from that which enters the first (backwards: r from behind, from that which enters the last): 64 channels, 16 spans of chunks.
-constexpr int JOIN_SPANS = 16;
+// The states that enter the chunks chunk0 .. chunk0 + chunks of the line from that which enters the first (backwards: r from behind, from that which enters the last): 16 channels, 64 spans of
+// chunks, which stay in registers between the two ways through them where they are eight or fewer.  Bound by the reads that follow one another, so many short spans of few channels (us, the
+// three launches backward of bf16 with a gate, for 64 channels x 16 spans / 32 x 32 / 16 x 64 / 8 x 128: 200000 x 256 339 / 276 / 269 / 278, 64571 x 640 225 / 207 / 203 / 212, 4096 x 512
+// 21.5 / 20.6 / 21.3 / 22.9).
+constexpr int JOIN_WIDTH = 16, JOIN_SPANS = 64;
 template <bool BWD>
-__global__ __launch_bounds__(64 * JOIN_SPANS) void recur_join_kernel(RecurP p) {
-  __shared__ float s_a[JOIN_SPANS][64], s_h[JOIN_SPANS][64];
-  const int lane = threadIdx.x & 63, span = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+__global__ __launch_bounds__(JOIN_WIDTH * JOIN_SPANS) void recur_join_kernel(RecurP p) {
+  __shared__ float s_a[JOIN_SPANS][JOIN_WIDTH], s_h[JOIN_SPANS][JOIN_WIDTH];
+  const int lane = threadIdx.x & (JOIN_WIDTH - 1), span = threadIdx.x / JOIN_WIDTH, c = blockIdx.x * JOIN_WIDTH + lane;
   const int per = (p.chunks + JOIN_SPANS - 1) / JOIN_SPANS, first = span * per, end = first + per < p.chunks ? first + per : p.chunks;
   const bool there = c < p.channels;
   auto index = [&](int i) { return BWD ? p.chunks - 1 - i : i; };   // i: in the order of composition
   constexpr int U = 8;
-  auto walk = [&](float& a, float& h, bool write) {
-    for (int i0 = first; i0 < end; i0 += U) {
-      float ka[U], kh[U];
+  float ka[U], kh[U];
+  auto ask = [&](int i0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float* from = p.sums + (long long)index(i0 + u < end ? i0 + u : i0) * 2 * p.channels + c;
-        ka[u] = from[0];
-        kh[u] = from[p.channels];
-      }
+    for (int u = 0; u < U; ++u) {
+      const float* from = p.sums + (long long)index(i0 + u < end ? i0 + u : i0) * 2 * p.channels + c;
+      ka[u] = from[0];
+      kh[u] = from[p.channels];
+    }
+  };
+  float a = 1.f, h = 0.f;
+  if (there)
+    for (int i0 = first; i0 < end; i0 += U) {
+      ask(i0);
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (i0 + u < end) {
           a = product(a, ka[u]);
           h = through(ka[u], h, kh[u]);
-          if (write) p.in[(long long)(p.chunk0 + (BWD ? index(i0 + u) : i0 + u + 1)) * p.channels + c] = h;
         }
     }
-  };
-  float a = 1.f, h = 0.f;
-  if (there) walk(a, h, false);
   s_a[span][lane] = a;
   s_h[span][lane] = h;
   __syncthreads();
@@ -424,7 +427,15 @@ __global__ __launch_bounds__(64 * JOIN_SPANS) void recur_join_kernel(RecurP p) {
   float in = outer ? 0.f : *edge;
   if (outer && span == 0) *edge = 0.f;
   for (int s = 0; s < span; ++s) in = through(s_a[s][lane], in, s_h[s][lane]);
-  walk(a, in, true);
+  for (int i0 = first; i0 < end; i0 += U) {
+    if (per > U) ask(i0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u < end) {
+        in = through(ka[u], in, kh[u]);
+        p.in[(long long)(p.chunk0 + (BWD ? index(i0 + u) : i0 + u + 1)) * p.channels + c] = in;
+      }
+  }
 }
 
 // ---- sequences of one length, each by work-groups that walk along it ----
@@ -761,7 +772,7 @@ hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
       if (e != hipSuccess) return e;
       p.direct = p.all_chunks <= DIRECT;
       if (p.direct) p.in = nullptr;
-      else hipLaunchKernelGGL(recur_join_kernel<BWD>, dim3((unsigned)((p.channels + 63) / 64)), dim3(64 * JOIN_SPANS), 0, s, p);
+      else hipLaunchKernelGGL(recur_join_kernel<BWD>, dim3((unsigned)((p.channels + JOIN_WIDTH - 1) / JOIN_WIDTH)), dim3(JOIN_WIDTH * JOIN_SPANS), 0, s, p);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
