@@ -48,8 +48,7 @@ struct Marks {
 // The borders are read as constants: for a whole wave by scalar loads, which do not wait for the rows that are on their way.
 typedef const __attribute__((address_space(4))) int32_t* Borders;
 // The last sequence that begins at or before the row; of several at the same place all but the last are empty.  -1: none.
-__device__ __forceinline__ int sequence_of(const RecurP& p, long long row) {
-  int lo = -1, hi = p.seqs + 1;                                   // offsets[lo] <= row < offsets[hi]
+__device__ __forceinline__ int sequence_of(const RecurP& p, long long row, int lo, int hi) {  // offsets[lo] <= row < offsets[hi]; -1 and seqs + 1: any row
   while (hi - lo > 1) {
     const int mid = lo + (hi - lo) / 2;
     if (((Borders)(uintptr_t)p.offsets)[mid] <= row) lo = mid;
@@ -57,13 +56,30 @@ __device__ __forceinline__ int sequence_of(const RecurP& p, long long row) {
   }
   return lo;
 }
-template <int ROWS>
-__device__ __forceinline__ Marks<ROWS> marks(const RecurP& p, long long r0) {
+// w0, wn: first row and number of rows of the wave.  Where it has several runs, they are looked for between the sequences of its first and its last row, which most often are one.
+template <int ROWS, bool NARROW>
+__device__ __forceinline__ Marks<ROWS> marks(const RecurP& p, long long r0, long long w0, int wn) {
   Marks<ROWS> m = {0u, 0u, 0u, {}};
-  if (r0 >= p.rows) return m;
   const Borders off = (Borders)(uintptr_t)p.offsets;
-  int s = p.offsets ? sequence_of(p, r0) : (int)(r0 / p.each);
-  long long begin = p.offsets ? (s >= 0 ? off[s] : 0) : s * p.each, next = p.offsets ? (s < p.seqs ? off[s + 1] : 0) : begin + p.each;
+  int s = 0;
+  long long begin = 0, next = 0;
+  if (p.offsets) {
+    if (w0 >= p.rows) return m;
+    s = sequence_of(p, w0, -1, p.seqs + 1);
+    begin = s >= 0 ? off[s] : 0;
+    next = s < p.seqs ? off[s + 1] : 0;
+    if (NARROW && s < p.seqs && next < w0 + wn) {
+      const int end = sequence_of(p, w0 + wn - 1, s, p.seqs + 1) + 1;
+      s = sequence_of(p, r0, s, end);
+      begin = s >= 0 ? off[s] : 0;
+      next = s < p.seqs ? off[s + 1] : 0;
+    }
+  } else {
+    s = (int)(r0 / p.each);
+    begin = s * p.each;
+    next = begin + p.each;
+  }
+  if (r0 >= p.rows) return m;
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     const long long row = r0 + r;
@@ -169,7 +185,7 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
             for (int e = 0; e < V; ++e) v[e] = through(ka[u][e], v[e], kh[u][e]);
       }
     }
-  const Marks<ROWS> m = marks<ROWS>(p, r0);
+  const Marks<ROWS> m = marks<ROWS, NARROW>(p, r0, row0 + wave * runs * ROWS, runs * ROWS);
   auto of_sequence = [&](const float* t, int r, float (&v)[V]) __attribute__((always_inline)) {  // the values of row r's sequence, zeros where there are none
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.f;
