@@ -1,12 +1,13 @@
 // Linear layer in 8-bit integers: rows of x and columns of w as whole numbers from -127 to 127 with a scale each (include/lms.h has the formulas).
 //
 // Both operands of the product lie with the reduction in rows of whole 16-byte vectors, zeros behind the last element: the weights are turned once, x as it is quantised.  In bytes the
-// product is then that of two bf16 matrices whose reductions lie in rows, and it runs on the same tiles (dense_gemm.hip).
-// us: 8192 rows, 8192 -> 4096, residual: rows 45 (201 MB at 4.4 TB/s), product 261 to 295 as the clock goes (1.9 to 2.1 P/s; operands of zeros 199); 24 rows, 2048 -> 8192: 3 and 8.
+// product is then that of two bf16 matrices whose reductions lie in rows, and it runs on the same tiles (dense_gemm.hip); up to 64 rows have kernels of their own, which read the weights in one round.
+// us: 8192 rows, 8192 -> 4096, residual: rows 45 (201 MB at 4.4 TB/s), product 261 to 295 as the clock goes (1.9 to 2.1 P/s; operands of zeros 199); 24 rows, 2048 -> 8192: 3 and 6.
 #include <hip/hip_runtime.h>
 
 #include <initializer_list>
 
+#include "conv_dma.hpp"
 #include "kernels.hpp"
 #include "rows4.hpp"
 
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(NT) void q8_rows_kernel(const T* x, long long ldx, 
 // Bound by reading the weights once.  A wave takes CW columns, its lanes consecutive 16 bytes of the reduction, and has eight loads of weights in flight before anything else happens; the rows of x lie
 // in LDS, 4-byte dot products go to whole sums of each lane, and the lanes meet by shuffles: whole numbers, in any order the same.  FUSED: every work-group quantises the rows itself,
 // while its weights are on their way, instead of waiting for another launch.  One row, 4096 -> 4096: 5.8 us in a graph, 2.9 TB/s of weights.  (Products of 32 x 32 x 32 with both operands straight from memory, for 9 to
-// 32 rows, took 10.1 us at 24 x 2048 -> 8192 and 58 at 32 x 8192 -> 16384, where the tiles take 10.8 and 32: half a line of each column a load is what the address unit is slow at.)
+// 32 rows, took 10.1 us at 24 x 2048 -> 8192 and 58 at 32 x 8192 -> 16384: half a line of each column a load is what the address unit is slow at.)
 constexpr int FT = 512, FEW_LDS = 65536 - 256;      // with what the kernel has besides, no more than any launch may have
 
 template <int ACT>
@@ -252,6 +253,117 @@ __global__ __launch_bounds__(FT) void q8_few_kernel(DenseP p, const T* x, long l
   }
 }
 
+// ---- some rows ----
+//
+// ROWS rows and C columns a work-group, its four waves in turn 128 bytes of the reduction each, a whole line of every row and column, straight to LDS.  Each wave has a ring of DEPTH such
+// stages for itself and waits for nobody: no barrier before the waves' sums meet.
+constexpr int MT = 256, LINE = 128;
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+constexpr int some_ring(int rows, int c, int depth) { return 4 * depth * (rows + c) * LINE; }
+
+template <typename T, int ROWS, int C, int DEPTH>
+__global__ __launch_bounds__(MT) void q8_some_kernel(DenseP p, int kp) {
+  constexpr int LA = ROWS / 8, LOADS = LA + C / 8, STAGE = (ROWS + C) * LINE, PITCH = C + 4;       // LA: loads of rows
+  constexpr int R = ROWS / C, STEPS = C == 32 ? 4 : 2, PARTS = 8 / STEPS;                          // products of C x C by PARTS pieces of 16 bytes
+  static_assert(some_ring(ROWS, C, DEPTH) >= 4 * ROWS * PITCH * 4 && (DEPTH - 1) * LOADS < 64, "the waves' sums take the rings' place; vmcnt has six bits");
+  typedef std::conditional_t<C == 32, i32x16, v4i> Acc;
+  constexpr int VALUES = sizeof(Acc) / 4;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char s_ring[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rows = (int)p.M, n0 = blockIdx.x * C;
+  const int lines = (kp + LINE - 1) / LINE, count = (lines + 3) / 4;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)s_ring + wave * DEPTH * STAGE);
+  const v4u rs_a = buffer_rsrc(p.a[0], 0x7fffffff), rs_b = buffer_rsrc((const signed char*)p.b[0] + (long long)n0 * kp, 0x7fffffff);
+  // eight rows of a line a load; a row's 16-byte pieces lie in an order of its own, so that the reads of many rows' same piece meet all banks
+  const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+  unsigned off[LOADS];
+#pragma unroll
+  for (int v = 0; v < LOADS; ++v) {
+    const int row = (v < LA ? v : v - LA) * 8 + (lane >> 3);
+    off[v] = row < (v < LA ? rows : p.N - n0) ? (unsigned)(row * kp + piece) : DMA_OOB;
+  }
+  auto ask = [&](int it) __attribute__((always_inline)) {
+    const unsigned at = lds0 + it % DEPTH * STAGE, k0 = (it * 4 + wave) * LINE;
+    const bool whole = (int)k0 + LINE <= kp, have = (int)k0 + piece < kp;     // beyond the end: zeros
+    if (whole) {
+#pragma unroll
+      for (int v = 0; v < LOADS; ++v) load_lds16(v < LA ? rs_a : rs_b, at + v * 1024, off[v], k0);
+    } else {
+#pragma unroll
+      for (int v = 0; v < LOADS; ++v) load_lds16(v < LA ? rs_a : rs_b, at + v * 1024, have ? off[v] : DMA_OOB, k0);
+    }
+  };
+  const int quad = tid % (C / 4) * 4, cnt = p.N - n0 - quad;
+  float sw[V], bias[V] = {};
+  load4(p.sw + n0 + quad, cnt, sw);
+  if (p.bias) load4(p.bias + n0 + quad, cnt, bias);
+#pragma unroll
+  for (int it = 0; it < DEPTH; ++it) ask(it);
+  Acc acc[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) acc[r][v] = 0;
+  int read[STEPS];
+#pragma unroll
+  for (int ks = 0; ks < STEPS; ++ks) read[ks] = wave * DEPTH * STAGE + lane % C * LINE + ((ks * PARTS + lane / C) ^ (lane & 7)) * 16;
+  for (int it = 0; it < count; ++it) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * LOADS) : "memory");
+    const unsigned char* t = s_ring + it % DEPTH * STAGE;
+    v4i a[R][STEPS], b[STEPS];
+#pragma unroll
+    for (int ks = 0; ks < STEPS; ++ks) {
+      b[ks] = *reinterpret_cast<const v4i*>(t + read[ks] + ROWS * LINE);
+#pragma unroll
+      for (int r = 0; r < R; ++r) a[r][ks] = *reinterpret_cast<const v4i*>(t + read[ks] + r * C * LINE);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // this stage's place is free
+    ask(it + DEPTH);
+#pragma unroll
+    for (int ks = 0; ks < STEPS; ++ks)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if constexpr (C == 32) acc[r] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[ks], a[r][ks], acc[r], 0, 0, 0);
+        else acc[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[ks], a[r][ks], acc[r], 0, 0, 0);
+      }
+  }
+  wait_loads();
+  __syncthreads();
+  int* const sums = reinterpret_cast<int*>(s_ring);               // [wave][row][column], from the transposed accumulators: lane l has row l % C, columns 4 (l / C) + v % 4, 8 further for each four of v
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int v = 0; v < VALUES / 4; ++v)
+      *reinterpret_cast<v4i*>(sums + (wave * ROWS + r * C + lane % C) * PITCH + 8 * v + 4 * (lane / C)) = v4i{acc[r][4 * v], acc[r][4 * v + 1], acc[r][4 * v + 2], acc[r][4 * v + 3]};
+  __syncthreads();
+  constexpr int EACH = MT / (C / 4);                              // rows at a time
+  const int n = n0 + quad;
+#pragma unroll
+  for (int i0 = 0; i0 < ROWS; i0 += EACH) {
+    const int i = i0 + tid / (C / 4);
+    if (i >= rows || i >= ROWS || cnt <= 0) continue;
+    v4i sum = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) sum += *reinterpret_cast<const v4i*>(sums + (w * ROWS + i) * PITCH + quad);
+    const float s = p.sx[i];
+    float y[V], beside[V] = {};
+    if (p.res) {
+      const Raw<T, V> q = raw<V>((const T*)p.res + i * p.ldr + n, cnt);
+#pragma unroll
+      for (int e = 0; e < V; ++e) beside[e] = q.get(e);
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[e] = (float)sum[e] * (s * sw[e]) + bias[e];
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) y[e] = act_value<decltype(act)::value>(y[e]);
+    });
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[e] += beside[e];
+    store4((T*)p.out[0] + i * p.ldo + n, cnt, y);
+  }
+}
+
 // ---- weights, laid out once ----
 //
 // Columns' largest magnitudes meet in sw as bits, by a maximum whose order does not matter; then tiles are turned through LDS; then the bits become scales.
@@ -367,8 +479,8 @@ hipError_t quantise(const lms_linear_q8_desc* d, const T* x, signed char* xq, fl
   return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
 
-// One or two rows that fit the LDS.  From three on the tiles, whose two launches then cost less than the dot products (us, few rows / tiles: 4096 -> 4096 one row 5.8 / 11.0, two 7.2 / 11.1, four 9.4 / 11.5,
-// eight 14.2 / 12.1; 2048 -> 8192 four rows 10.7 / 10.3; 8192 -> 16384 four rows 31.6 / 31.8).
+// One or two rows that fit the LDS.  From three on products of many rows, whose two launches then cost less than the dot products (us, dot products / those: 4096 -> 4096 one row 5.8 / 8, two 7.2 / 8.3,
+// four 9.4 / 8.6; 2048 -> 8192 four rows 10.7 / 7.6; 8192 -> 16384 four rows 31.6 / 31.8).
 bool few_rows(const lms_linear_q8_desc* d) { return d->m >= 1 && d->m <= 2 && d->m * pitch(d) <= FEW_LDS; }
 
 template <typename T, int R, bool FUSED>
@@ -391,10 +503,31 @@ hipError_t few_product(const lms_linear_q8_desc* d, DenseP& p, const void* x, hi
   return x ? few<T, 2, true>(d, p, t, s) : few<T, 2, false>(d, p, t, s);
 }
 
+template <typename T, int ROWS, int C, int DEPTH>
+hipError_t some(const lms_linear_q8_desc* d, DenseP& p, hipStream_t s) {
+  constexpr int ring = some_ring(ROWS, C, DEPTH);
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(q8_some_kernel<T, ROWS, C, DEPTH>), hipFuncAttributeMaxDynamicSharedMemorySize, ring);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((q8_some_kernel<T, ROWS, C, DEPTH>), dim3((unsigned)((d->n + C - 1) / C)), dim3(MT), ring, s, p, pitch(d));
+  return hipGetLastError();
+}
+// Where one round of work-groups takes all columns, and a wave has few enough stages one after the other that the tiles' splits with their join cost more.  us, tiles / this, with the rows' launch of 3:
+//   rows                       3             24            64                                    3             32            64
+//   1024 -> 1024        7.7 / 6.1     8.4 / 6.5     8.0 / 7.0      4096 -> 6000      13.4 / 9.7    14.3 / 10.3   15.3 / 12.2
+//   4096 -> 4096       11.3 / 8.4    12.4 / 9.6    13.8 / 11.6     8192 -> 8192      20.7 / 18.8   21.6 / 21.3   22.9 / 22.7
+//   2048 -> 8192       10.2 / 7.5    10.9 / 8.1    10.7 / 9.7      12000 -> 4096     19.0 / 15.5   20.7 / 18.3   21.4 / 24.5
+//   8192 -> 2048       12.7 / 10.7   13.5 / 11.3   14.8 / 14.2     16384 -> 8192     32.8 / 35.7   33.6 / 38.8   43.5 / 41.8
+bool some_rows(const lms_linear_q8_desc* d) { return d->m >= 3 && d->m <= 64 && d->n <= 256 * 32 && pitch(d) <= (d->m <= 32 ? 12288 : 8192); }
+template <typename T>
+hipError_t some_product(const lms_linear_q8_desc* d, DenseP& p, hipStream_t s) {
+  if (d->n > 256 * 16) return d->m > 32 ? some<T, 64, 32, 3>(d, p, s) : some<T, 32, 32, 4>(d, p, s);
+  return d->m > 32 ? some<T, 64, 16, 3>(d, p, s) : some<T, 32, 16, 5>(d, p, s);
+}
+
 uint64_t rows_bytes(const lms_linear_q8_desc* d) { return up256((uint64_t)d->m * pitch(d)); }
 uint64_t scale_bytes(const lms_linear_q8_desc* d) { return up256((uint64_t)d->m * 4); }
 int mode_of(const lms_linear_q8_desc* d) { return d->dtype == LMS_F32 ? DENSE_Q8_F32 : DENSE_Q8; }
-uint64_t product_bytes(const lms_linear_q8_desc* d) { return few_rows(d) ? 0 : up256(dense_bf16_ws(mode_of(d), d->m, d->n, pitch(d) / 2, 1, 1)); }
+uint64_t product_bytes(const lms_linear_q8_desc* d) { return few_rows(d) || some_rows(d) ? 0 : up256(dense_bf16_ws(mode_of(d), d->m, d->n, pitch(d) / 2, 1, 1)); }
 
 lms_status check(const char* what, const lms_linear_q8_desc* d) {
   NEED(d->m >= 0 && d->n >= 1 && d->k >= 1, "%s: rows must be >= 0, widths >= 1", what);
@@ -430,6 +563,7 @@ hipError_t product(const lms_linear_q8_desc* d, const void* x, const void* xq, c
   p.segs = 1; p.srcs = 1; p.act = d->act;
   p.part = (float*)ws;
   if (few_rows(d)) return d->dtype == LMS_F32 ? few_product<float>(d, p, x, s) : few_product<uint16_t>(d, p, x, s);
+  if (some_rows(d)) return d->dtype == LMS_F32 ? some_product<float>(d, p, s) : some_product<uint16_t>(d, p, s);
   return dense_bf16(mode_of(d), p, s);
 }
 

@@ -14,7 +14,11 @@ CASES = [(1, 1, 1, "none", False, False, "fp32", 0), (1, 16, 8, "silu", True, Tr
          (24, 2048, 4096, "gelu_tanh", True, True, "bf16", 8), (33, 520, 776, "none", True, False, "fp32", 0), (64, 8190, 256, "none", False, False, "bf16", 0),
          (100, 700, 1000, "silu", True, True, "fp32", 5), (300, 1024, 1024, "gelu", True, True, "bf16", 0), (1000, 64, 100, "none", False, False, "bf16", 0),
          (1030, 1032, 1100, "relu", True, True, "bf16", 8), (513, 2064, 4104, "none", True, True, "fp32", 0), (4100, 528, 2056, "silu", True, True, "bf16", 0),
-         (16, 40000, 70, "none", False, False, "fp32", 0), (2, 131072, 16, "none", False, False, "fp32", 0)]
+         (16, 40000, 70, "none", False, False, "fp32", 0), (2, 131072, 16, "none", False, False, "fp32", 0),
+         # up to 64 rows in one round: blocks of 16 and of 32 columns, lines and stages that end inside, one short row of weights; and what takes the tiles beside them
+         (3, 1, 1, "none", True, True, "bf16", 0), (32, 144, 4096, "silu", True, True, "bf16", 4), (17, 2064, 4097, "gelu", True, True, "fp32", 3), (32, 2032, 8190, "none", False, True, "bf16", 2),
+         (33, 3000, 4096, "relu", True, False, "fp32", 0), (64, 8192, 50, "none", True, True, "bf16", 6), (63, 530, 8192, "gelu_tanh", True, True, "bf16", 0), (40, 127, 5001, "none", False, False, "fp32", 1),
+         (7, 12288, 37, "none", True, True, "bf16", 0), (9, 12300, 300, "none", True, False, "bf16", 0), (24, 2048, 8200, "gelu", True, True, "bf16", 0), (65, 2560, 500, "silu", True, True, "bf16", 0)]
 
 
 def ptr(t):
