@@ -36,6 +36,7 @@ struct RecurP {
   int seqs, channels, act;
   int chunk0, chunks, all_chunks;      // chunks of this launch
   int direct;                  // few chunks: each composes those that come before it out of sums itself, and there is no `in`
+  int empties;                 // work-groups of a block of channels behind the chunks' that look for sequences without rows
   int lpr, subs;               // lanes of a row, a power of two; runs of rows of a wave, 64 / lpr
 };
 
@@ -83,10 +84,15 @@ __device__ __forceinline__ Marks<ROWS> marks(const RecurP& p, long long r0, long
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     const long long row = r0 + r;
-    while (s < p.seqs && next <= row) {                           // on to the sequence of this row
+    if (s < p.seqs && next <= row) {                              // on to the sequence of this row: most often the next one
       ++s;
       begin = next;
       next = p.offsets ? (s < p.seqs ? off[s + 1] : 0) : begin + p.each;
+      if (s < p.seqs && next <= row) {                            // behind any number of empty ones
+        s = sequence_of(p, row, s, p.seqs + 1);
+        begin = off[s];
+        next = s < p.seqs ? off[s + 1] : 0;
+      }
     }
     const bool live = row < p.rows && s >= 0 && s < p.seqs;
     m.live |= (unsigned)live << r;
@@ -137,6 +143,27 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
   const bool column = c0 < p.channels;
   const int cnt = WHOLE ? V : p.channels - c0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // sequences without a row keep their states: eight at a time to a wave, by work-groups behind those of the chunks
+  if constexpr (WAY == APPLY_FWD || WAY == APPLY_BWD)
+    if (chunk >= p.chunks) {
+      constexpr int EACH = 8;
+      float* to = BWD ? p.dh0 : p.last;
+      const float* from = BWD ? p.dlast : p.h0;
+      for (long long s0 = ((long long)(chunk - p.chunks) * WAVES + wave) * EACH; s0 < p.seqs; s0 += (long long)p.empties * WAVES * EACH) {
+        const int s = (int)s0 + lane;
+        const bool empty = lane < EACH && s < p.seqs && (!p.offsets || p.offsets[s] == p.offsets[s + 1]);
+        const unsigned long long found = __ballot(empty);
+        if (!column) continue;
+        float v[EACH][V] = {};
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+          if (from && (found >> i & 1)) load4(from + (s0 + i) * p.channels + c, cnt, v[i]);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+          if (found >> i & 1) store4(to + (s0 + i) * p.channels + c, cnt, v[i]);
+      }
+      return;
+    }
   const long long row0 = (long long)(p.chunk0 + chunk) * (CHUNK * runs), r0 = row0 + (wave * runs + run) * ROWS;
   const long long x0 = r0 * p.ldx, y0 = r0 * p.ldy;               // of the first row
   const bool there = column && r0 < p.rows, gated = p.o != nullptr;
@@ -296,23 +323,6 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
     return;
   }
   if constexpr (WAY == APPLY_FWD || WAY == APPLY_BWD) {
-    // sequences without a row keep their states
-    if (p.chunk0 + chunk == 0) {                                  // all lanes: they look through the sequences
-      float* to = BWD ? p.dh0 : p.last;
-      const float* from = BWD ? p.dlast : p.h0;
-      if (to && (p.offsets || p.rows == 0))
-        for (int s0 = wave * 64; s0 < p.seqs; s0 += Shape<T, WAY>::NT) {
-          const int s = s0 + (threadIdx.x & 63);
-          unsigned long long empty = __ballot(s < p.seqs && (!p.offsets || p.offsets[s] == p.offsets[s + 1]));
-          for (; empty; empty &= empty - 1) {
-            const long long entry = (long long)(s0 + __builtin_ctzll(empty)) * p.channels + c;
-            float v[V] = {};
-            if (!column) continue;
-            if (from) load4(from + entry, cnt, v);
-            store4(to + entry, cnt, v);
-          }
-        }
-    }
     if (!there) return;
     // what was computed of the inputs is computed again from here on: kept, it takes twice the registers of the inputs, and with them the second work-group of a compute unit
     auto anew = [](auto& t) __attribute__((always_inline)) {
@@ -762,7 +772,7 @@ hipError_t walk(const lms_recur_desc* d, const RecurP& p, hipStream_t s) {
 template <typename T, int WAY>
 hipError_t launch(const RecurP& p, hipStream_t s) {
   const int blocks = (p.channels + BLOCK - 1) / BLOCK;
-  const dim3 grid((unsigned)(blocks * p.chunks)), threads((Shape<T, WAY>::NT));
+  const dim3 grid((unsigned)(blocks * (p.chunks + p.empties))), threads((Shape<T, WAY>::NT));
   if (p.subs == 1) hipLaunchKernelGGL((recur_kernel<T, WAY, true, false>), grid, threads, 0, s, p);
   else if (p.channels >= V) hipLaunchKernelGGL((recur_kernel<T, WAY, true, true>), grid, threads, 0, s, p);
   else hipLaunchKernelGGL((recur_kernel<T, WAY, false, true>), grid, threads, 0, s, p);
@@ -772,6 +782,8 @@ hipError_t launch(const RecurP& p, hipStream_t s) {
 // Chunks up to which a launch for the states between them is not worth it (us, forward + backward, with it / without: 256 x 1024 in bf16 16.4 + 17.2 / 14.6 + 15.6, 512 x 960 16.9 + 18.4 / 15.1 + 17.2;
 // of 32 chunks, 1024 x 1024 backward 19.4 / 21.3).
 constexpr int DIRECT = 16;
+
+constexpr int EMPTIES = 1 << 14;       // work-groups that look for sequences without rows, at most
 
 // in: entries of the states between chunks, sums: of a part.
 template <typename T, bool BWD>
@@ -792,8 +804,12 @@ hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    e = launch<T, BWD ? APPLY_BWD : APPLY_FWD>(p, s);
+    constexpr int WAY = BWD ? APPLY_BWD : APPLY_FWD, looked = Shape<T, WAY>::WAVES * 8;
+    const int blocks = (p.channels + BLOCK - 1) / BLOCK, most = blocks < EMPTIES ? EMPTIES / blocks : 1, need = (p.seqs + looked - 1) / looked;
+    p.empties = i > 0 || !(BWD ? p.dh0 : p.last) || !(p.offsets || p.rows == 0) ? 0 : need < most ? need : most;
+    e = launch<T, WAY>(p, s);
     if (e != hipSuccess) return e;
+    p.empties = 0;
   }
   p.in = in;
   return hipSuccess;

@@ -19,7 +19,10 @@ CASES = [(1, [1], None, "fp32", 0), (4, [0, 0], "silu", "bf16", 0), (5, [3, 0, 1
          # few channels: several runs of rows in a wave, in one and in several chunks
          (1, [3000, 0, 5000, 1, 777], "silu", "bf16", 0), (2, [9001], None, "fp32", 0), (3, (4200, 6), "gelu", "bf16", 1), (16, (3 * 1300, 3), "relu", "fp32", 0), (33, (5000, 2), "silu", "bf16", 3),
          (100, ODD, "gelu_tanh", "fp32", 0), (128, ODD * 3, "silu", "bf16", 0), (64, [1] * 300 + [0] * 9 + [4] * 50, "none", "bf16", 0), (20, (50, 1), "silu", "bf16", 0), (7, [40], "silu", "fp32", 0),
-         (600, [50], "silu", "bf16", 0), (16, (64 * 128, 64), "silu", "bf16", 0)]
+         (600, [50], "silu", "bf16", 0), (16, (64 * 128, 64), "silu", "bf16", 0),
+         # many sequences without rows, before, between and behind others; nothing but them
+         (300, [0] * 2000 + [3] + [0] * 1500 + [70, 1, 1] + [0] * 700, "silu", "bf16", 0), (3, [2, 0, 0, 0, 500] + [0] * 3000 + [1], "gelu", "fp32", 1), (40, [0] * 1000, "silu", "bf16", 0),
+         (260, (0, 700), "relu", "fp32", 0), (516, [5] + [0] * 600 + [64] * 3 + [0] * 65 + [129], None, "bf16", 0)]
 
 
 def make(torch, seed, c, lengths, act, dtype, pad):
