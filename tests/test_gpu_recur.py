@@ -209,7 +209,7 @@ def test_a_line_in_several_launches():
         check(torch, one, got, oracle(one, "silu"), 1)
 
 
-@pytest.mark.parametrize("dtype,c,n,slots", [("bf16", 256, 5, 9), ("fp32", 1033, 3, 3), ("bf16", 4100, 70, 200), ("bf16", 3, 1, 1)])
+@pytest.mark.parametrize("dtype,c,n,slots", [("bf16", 256, 5, 9), ("fp32", 1033, 3, 3), ("bf16", 4100, 70, 200), ("bf16", 3, 1, 1), ("bf16", 20, 1300, 40), ("fp32", 5, 2000, 1990)])
 def test_step(dtype, c, n, slots):
     import torch
     import paper_1807_02037_amd as L
@@ -218,7 +218,7 @@ def test_step(dtype, c, n, slots):
     kind = torch.bfloat16 if dtype == "bf16" else torch.float32
     x, g, o = (torch.randn(n, c + 3, generator=gen).to(kind).cuda()[:, :c] for _ in range(3))
     state = torch.randn(slots, c, generator=gen).cuda()
-    ids = torch.randperm(slots, generator=gen)[:n].int()
+    ids = (torch.randperm(slots, generator=gen)[:n] if n <= slots else torch.randint(slots, (n,), generator=gen)).int()      # more rows than slots: positions far apart
     if n > 2:
         ids[1] = -1
     if n > 60:
