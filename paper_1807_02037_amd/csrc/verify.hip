@@ -3,8 +3,8 @@
 // Two launches.  The first sums, for each request, the chunks of the one distribution that its next token comes from, a wave a chunk; every wave finds that distribution by itself, from a few reads of the drafts.
 // The second picks the chunk in which the running sum passes the drawn share of the whole, and the class in it.  Differences and sums are fp64: the token is that of exact sums but
 // where the drawn number lies within some 2^-50 of a border, and whole numbers have no tolerance.
-// Bound by latency, then by memory: us in a graph, 1 x 32003 7.7, 8 x 128000 8.3, 128 x 50304 16.5 (51 MB; launches 10 and 5.4), 512 x 50304 42.9.  Both steps in one launch, a work-group a request, read
-// at what one compute unit gets: 10.7, 30.7, 18.6, 45.8.
+// Bound by latency, then by memory: us in a graph, 1 x 32003 8.0, 8 x 128000 8.3, 128 x 50304 16.5 (51 MB; launches 10 and 5.4), 512 x 50304 42.9.  Both steps in one launch, a work-group a request, read
+// at what one compute unit gets (10.7, 30.7, 18.6, 45.8), so only few classes go that way.
 #include <hip/hip_runtime.h>
 
 #include <initializer_list>
@@ -18,6 +18,9 @@ namespace {
 
 constexpr int NT = 256, STEP = NT * 4;  // classes of a work-group at a time, and of a chunk at least
 constexpr int MAX_CHUNKS = 256;        // of a request: four a lane
+// Few chunks of few requests: both steps by a work-group of FEW threads a request (us in a graph, two launches / one: 1 x 1000 7.1 / 5.8, 1 x 8000 7.8 / 6.4, 1 x 16000 8.0 / 8.2, 64 x 8000 8.6 / 7.1,
+// 256 x 16000 13.5 / 12.0; 1 x 32003 8.0 / 11.6, 4000 x 1000 23 / 71 with 1024 threads; call by call from Python 1 x 8000 10.1 / 7.5, 1 x 16000 9.5 / 7.3).
+constexpr int FEW = 512, ALONE_REQUESTS = 256, ALONE_CHUNKS = 16;
 
 struct VerifyP {
   const float *p, *q;
@@ -58,17 +61,10 @@ __device__ __forceinline__ void masses(const float (&a)[4], const float (&b)[4],
   }
 }
 
-__global__ __launch_bounds__(NT) void verify_sums_kernel(VerifyP p) {
-  const int lane = threadIdx.x & 63;
-  const long long job = (long long)blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (job >= (long long)p.requests * p.chunks) return;
-  const int b = (int)(job / p.chunks), chunk = (int)(job - (long long)b * p.chunks);
-  int count;
-  const int at = accepted_drafts(p, b, count);
-  const float* pr = p.p + ((long long)b * (p.drafts + 1) + at) * p.ldp;
-  const float* qr = at < count ? p.q + ((long long)b * p.drafts + at) * p.ldq : nullptr;
-  const int begin = chunk * p.chunk, end = begin + p.chunk < p.classes ? begin + p.chunk : p.classes;
-  double sr = 0.0, sp = 0.0;
+// The wave's sums over a chunk of the distribution pr, qr: in all lanes.
+__device__ __forceinline__ void chunk_sums(const VerifyP& p, const float* pr, const float* qr, int chunk, double& sr, double& sp) {
+  const int lane = threadIdx.x & 63, begin = chunk * p.chunk, end = begin + p.chunk < p.classes ? begin + p.chunk : p.classes;
+  sr = sp = 0.0;
   for (int c0 = begin; c0 < end; c0 += STEP) {
     float a[4][4], q[4][4];
 #pragma unroll
@@ -92,7 +88,17 @@ __global__ __launch_bounds__(NT) void verify_sums_kernel(VerifyP p) {
     sr += __shfl_xor(sr, d);
     sp += __shfl_xor(sp, d);
   }
-  if (lane == 0) {
+}
+
+__global__ __launch_bounds__(NT) void verify_sums_kernel(VerifyP p) {
+  const long long job = (long long)blockIdx.x * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (job >= (long long)p.requests * p.chunks) return;
+  const int b = (int)(job / p.chunks), chunk = (int)(job - (long long)b * p.chunks);
+  int count;
+  const int at = accepted_drafts(p, b, count);
+  double sr, sp;
+  chunk_sums(p, p.p + ((long long)b * (p.drafts + 1) + at) * p.ldp, at < count ? p.q + ((long long)b * p.drafts + at) * p.ldq : nullptr, chunk, sr, sp);
+  if ((threadIdx.x & 63) == 0) {
     p.sums[job * 2] = sr;
     p.sums[job * 2 + 1] = sp;
   }
@@ -109,21 +115,33 @@ __device__ __forceinline__ double running(double v) {
   return v;
 }
 
+// ALONE: the sums as well, a chunk a wave, in LDS.
+template <int NT, bool ALONE>
 __global__ __launch_bounds__(NT) void verify_pick_kernel(VerifyP p) {
-  __shared__ double lds[NT / 64];
+  constexpr int STEP = NT * 4;
+  __shared__ double lds[NT / 64], s_sums[ALONE ? ALONE_CHUNKS : 1][2];
   __shared__ int s_first[NT / 64], s_last[NT / 64];
   const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int count;
   const int at = accepted_drafts(p, b, count);
   const float* pr = p.p + ((long long)b * (p.drafts + 1) + at) * p.ldp;
   const float* qr = at < count ? p.q + ((long long)b * p.drafts + at) * p.ldq : nullptr;
+  if constexpr (ALONE) {
+    for (int chunk = wave; chunk < p.chunks; chunk += NT / 64) {
+      double sr, sp;
+      chunk_sums(p, pr, qr, chunk, sr, sp);
+      if (lane == 0) { s_sums[chunk][0] = sr; s_sums[chunk][1] = sp; }
+    }
+    __syncthreads();
+  }
   // the chunk: lane l has four, from 4 l on
   constexpr int NONE = 0x7fffffff;
   double er[4], ep[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const bool there = lane * 4 + e < p.chunks;
-    const double* from = p.sums + ((long long)b * p.chunks + lane * 4 + e) * 2;
+    const double* from = ALONE ? nullptr : p.sums + ((long long)b * p.chunks + lane * 4 + e) * 2;
+    if constexpr (ALONE) from = s_sums[there ? lane * 4 + e : 0];
     er[e] = there ? from[0] : 0.0;
     ep[e] = there ? from[1] : 0.0;
   }
@@ -245,8 +263,12 @@ lms_status verify(const lms_verify_desc* d, const float* pr, const float* q, con
   p.requests = d->requests; p.drafts = d->drafts; p.classes = d->classes;
   chunks_of(d, p.chunks, p.chunk);
   hipStream_t s = (hipStream_t)stream;
+  if (p.chunks <= ALONE_CHUNKS && d->requests <= ALONE_REQUESTS) {
+    hipLaunchKernelGGL((verify_pick_kernel<FEW, true>), dim3((unsigned)d->requests), dim3(FEW), 0, s, p);
+    return done(what, hipGetLastError());
+  }
   hipLaunchKernelGGL(verify_sums_kernel, dim3((unsigned)(((long long)d->requests * p.chunks + NT / 64 - 1) / (NT / 64))), dim3(NT), 0, s, p);
-  hipLaunchKernelGGL(verify_pick_kernel, dim3((unsigned)d->requests), dim3(NT), 0, s, p);
+  hipLaunchKernelGGL((verify_pick_kernel<NT, false>), dim3((unsigned)d->requests), dim3(NT), 0, s, p);
   return done(what, hipGetLastError());
 }
 

@@ -61,7 +61,7 @@ def make(seed, b, d, c, spread=0.5, agree=0.3):
 
 
 @pytest.mark.parametrize("b,d,c,pad", [(1, 0, 1, 0), (1, 1, 1, 0), (3, 2, 2, 1), (5, 4, 100, 0), (40, 3, 1023, 3), (2, 70, 1025, 0), (7, 5, 4097, 0), (1, 4, 32003, 5), (1, 8, 131073, 0),
-                                       (600, 2, 130, 0), (16, 6, 20000, 4)])
+                                       (600, 2, 130, 0), (16, 6, 20000, 4), (256, 3, 16384, 0), (257, 2, 16384, 0), (3, 2, 16385, 1), (9, 3, 8200, 2), (2, 1024, 1500, 0)])
 def test_against_the_rule(b, d, c, pad):
     import torch
     import paper_1807_02037_amd as L
@@ -73,7 +73,8 @@ def test_against_the_rule(b, d, c, pad):
         assert (got[0] == want[0]).all() and (got[1] == want[1]).all(), np.argwhere(got[1] != want[1])
 
 
-def test_borders():
+@pytest.mark.parametrize("times", [1, 20])
+def test_borders(times):                                           # many requests take two launches
     import torch
     import paper_1807_02037_amd as L
     nan, inf = float("nan"), float("inf")
@@ -97,6 +98,7 @@ def test_borders():
     p[11, 1, 5], p[11, 1, 2050], v[11] = 0.5, 0.5, 0.5             # half of the whole: the running sum has to be above
     p[12, 1], v[12] = 1.0 / 4096, 0.0                              # the first class
     p[13, 1, 5], v[13] = -1.0, 0.0                                 # below 0: no share
+    p, q, t, u, v = (np.tile(a, (times,) + (1,) * (a.ndim - 1)) for a in (p, q, t, u, v))
     want = rule(p.astype(float), q.astype(float), t, None, u.astype(float), v.astype(float))
     got = call(torch, L, p, q, t, None, u, v)
     assert (got[0] == want[0]).all() and (got[1] == want[1]).all(), (got, want)
