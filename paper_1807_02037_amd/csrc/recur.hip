@@ -9,6 +9,7 @@
 // parts of 96 / 192 MB / one: forward 427 / 362 / 325 us, backward 624 / 580 / 528.)
 #include <hip/hip_runtime.h>
 
+#include <cstdlib>
 #include <initializer_list>
 
 #include "dense.hpp"
@@ -416,10 +417,11 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
 // three launches backward of bf16 with a gate, for 64 channels x 16 spans / 32 x 32 / 16 x 64 / 8 x 128: 200000 x 256 339 / 276 / 269 / 278, 64571 x 640 225 / 207 / 203 / 212, 4096 x 512
 // 21.5 / 20.6 / 21.3 / 22.9).
 constexpr int JOIN_WIDTH = 16, JOIN_SPANS = 64;
+constexpr int JOIN_BLOCKS = 1 << 21;   // blocks of channels of a launch: a grid holds less than 2^32 threads
 template <bool BWD>
-__global__ __launch_bounds__(JOIN_WIDTH * JOIN_SPANS) void recur_join_kernel(RecurP p) {
+__global__ __launch_bounds__(JOIN_WIDTH * JOIN_SPANS) void recur_join_kernel(RecurP p, int block0) {
   __shared__ float s_a[JOIN_SPANS][JOIN_WIDTH], s_h[JOIN_SPANS][JOIN_WIDTH];
-  const int lane = threadIdx.x & (JOIN_WIDTH - 1), span = threadIdx.x / JOIN_WIDTH, c = blockIdx.x * JOIN_WIDTH + lane;
+  const int lane = threadIdx.x & (JOIN_WIDTH - 1), span = threadIdx.x / JOIN_WIDTH, c = (block0 + (int)blockIdx.x) * JOIN_WIDTH + lane;
   const int per = (p.chunks + JOIN_SPANS - 1) / JOIN_SPANS, first = span * per, end = first + per < p.chunks ? first + per : p.chunks;
   const bool there = c < p.channels;
   auto index = [&](int i) { return BWD ? p.chunks - 1 - i : i; };   // i: in the order of composition
@@ -733,12 +735,18 @@ int lanes_of(int channels) {
 int chunk_of(const lms_recur_desc* d, bool bwd) { return (bwd ? CHUNK_BWD : CHUNK_FWD) * (64 / lanes_of(d->channels)); }
 long long chunks_of(long long rows, int chunk) { return rows <= chunk ? 1 : (rows + chunk - 1) / chunk; }
 // Chunks of one launch: 2^21 work-groups of up to 1024 threads are a grid.
-long long part_chunks(const lms_recur_desc* d) {
+long long most_chunks(const lms_recur_desc* d) {
   const long long most = (1LL << 21) / ((d->channels + BLOCK - 1) / BLOCK);
   return most < 1 ? 1 : most;
 }
+// Tuning aid: LMS_RECUR_CHUNKS, fewer of them in a launch.  The workspace is that of the most.
+long long part_chunks(const lms_recur_desc* d) {
+  const char* fewer = getenv("LMS_RECUR_CHUNKS");
+  const long long most = most_chunks(d), want = fewer ? atoll(fewer) : 0;
+  return want > 0 && want < most ? want : most;
+}
 uint64_t sums_bytes(const lms_recur_desc* d, int chunk) {
-  const long long part = part_chunks(d), all = chunks_of(d->rows, chunk);
+  const long long part = most_chunks(d), all = chunks_of(d->rows, chunk);
   return up256((uint64_t)(part < all ? part : all) * 2 * d->channels * 4);
 }
 uint64_t in_bytes(const lms_recur_desc* d, int chunk) { return up256((uint64_t)(chunks_of(d->rows, chunk) + 1) * d->channels * 4); }
@@ -834,9 +842,11 @@ hipError_t line(RecurP& p, bool alone, long long part, hipStream_t s) {
     if (!alone) {
       e = launch<T, BWD ? SUM_BWD : SUM_FWD>(p, s);
       if (e != hipSuccess) return e;
-      p.direct = p.all_chunks <= DIRECT;
+      p.direct = parts == 1 && p.all_chunks <= DIRECT;               // of several parts, the sums are only this one's
       if (p.direct) p.in = nullptr;
-      else hipLaunchKernelGGL(recur_join_kernel<BWD>, dim3((unsigned)((p.channels + JOIN_WIDTH - 1) / JOIN_WIDTH)), dim3(JOIN_WIDTH * JOIN_SPANS), 0, s, p);
+      else
+        for (int b = 0, all = (p.channels + JOIN_WIDTH - 1) / JOIN_WIDTH; b < all; b += JOIN_BLOCKS)
+          hipLaunchKernelGGL(recur_join_kernel<BWD>, dim3((unsigned)(all - b < JOIN_BLOCKS ? all - b : JOIN_BLOCKS)), dim3(JOIN_WIDTH * JOIN_SPANS), 0, s, p, b);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
