@@ -104,14 +104,17 @@ __device__ __forceinline__ Marks<ROWS> marks(const RecurP& p, long long r0, long
   return m;
 }
 
-// 1 - a for a = sigmoid(g), without its cancellation: the exponential that a has below its line, times a.  Beyond 2^100 it is cut: a is then nothing against any state, and the rest 1.
-__device__ __forceinline__ float rest_of(float g, float a) {
-  const float e = __builtin_amdgcn_exp2f(g * -1.44269504f);
-  return e >= 0x1p100f ? 1.f : e * a;
+// Of a = sigmoid(g) and 1 - a the smaller one, e / (1 + e) with e = exp(-|g|), and the sign of g: where that is negative it is a, else 1 - a.  The other is one minus it, so both are there to their own
+// precision (a difference from an a that is rounded already is off by 1 % at g = 12 and by all at 18), and a gate at its end keeps or replaces all, bit for bit.
+__device__ __forceinline__ float share(float g) {
+  const float e = __builtin_amdgcn_exp2f(__builtin_fabsf(g) * -1.44269504f);
+  return __builtin_copysignf(e * __builtin_amdgcn_rcpf(1.f + e), g);
 }
+__device__ __forceinline__ float kept_of(float share) { return __builtin_signbitf(share) ? -share : 1.f - share; }     // a
+__device__ __forceinline__ float rest_of(float share) { return __builtin_signbitf(share) ? 1.f + share : share; }      // 1 - a
 
-// a h + (1 - a) x: a difference that is exact from a = 1/2 on, so that a state no gate touches stays what it is.
-__device__ __forceinline__ float mix(float a, float h, float x) { return __builtin_fmaf(a, h, (1.f - a) * x); }
+// a h + (1 - a) x
+__device__ __forceinline__ float mix(float share, float h, float x) { return __builtin_fmaf(kept_of(share), h, rest_of(share) * x); }
 
 // What leaves a span (a, h) that v enters, and the a of two spans, the one of `second` behind.
 __device__ __forceinline__ float through(float a, float v, float h) { return __builtin_signbitf(a) ? h : __builtin_fmaf(a, v, h); }
@@ -221,7 +224,7 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
   };
 
   // ---- the wave's spans ----
-  float a[ROWS][V], err[BWD ? ROWS : 1][V];                       // err: e = dy act(o)
+  float a[ROWS][V], err[BWD ? ROWS : 1][V];                       // a: the gates' shares; err: e = dy act(o)
   if constexpr (BWD) {
     if (gated && there) with_act(p.act, [&](auto act) {
 #pragma unroll
@@ -251,9 +254,9 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
     }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      a[r][e] = sigmoid(there ? g[r].get(e) : 0.f);
+      a[r][e] = share(there ? g[r].get(e) : 0.f);
       if constexpr (STATE) {
-        A[e] *= a[r][e];
+        A[e] *= kept_of(a[r][e]);
         H[e] = mix(a[r][e], H[e], there ? x[r].get(e) : 0.f);
       }
     }
@@ -264,7 +267,7 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
         if (end) of_sequence(p.dlast, r, d);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          B[e] *= a[r][e];
+          B[e] *= kept_of(a[r][e]);
           R[e] = __builtin_fmaf(B[e], err[r][e] + d[e], R[e]);
           if (end) B[e] = -0.f;
         }
@@ -388,9 +391,9 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
           if (first) of_sequence(p.h0, r, before);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
-            const float dh = err[r][e] + behind[e], rest = rest_of(g[r].get(e), a[r][e]);
+            const float dh = err[r][e] + behind[e], rest = rest_of(a[r][e]);
             dx[e] = rest * dh;
-            behind[e] = a[r][e] * dh;
+            behind[e] = kept_of(a[r][e]) * dh;
             dg[e] = behind[e] * rest * (before[e] - x[r].get(e));
             if constexpr (decltype(with_gate)::value) {
               float value, slope;
@@ -526,7 +529,7 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
     }
     entry = next_entry;
     if (i + 1 < steps) ask(BWD ? step - 1 : step + 1);
-    float a[WROWS][WV], err[BWD ? WROWS : 1][WV];
+    float a[WROWS][WV], err[BWD ? WROWS : 1][WV];                  // a: the gates' shares
     if constexpr (BWD) {
       if (gated) with_act(p.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
@@ -550,13 +553,13 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
       const bool live = at0 + r < each;
 #pragma unroll
       for (int e = 0; e < WV; ++e) {
-        a[r][e] = sigmoid(g[r].get(e));
+        a[r][e] = share(g[r].get(e));
         if constexpr (BWD) {
-          a[r][e] = live ? a[r][e] : 1.f;
+          a[r][e] = live ? a[r][e] : 0.f;
           err[r][e] = live ? err[r][e] : 0.f;
         }
       }
-      A = make_float2(A.x * a[r][0], A.y * a[r][1]);
+      A = make_float2(A.x * kept_of(a[r][0]), A.y * kept_of(a[r][1]));
       H = make_float2(mix(a[r][0], H.x, x[r].get(0)), mix(a[r][1], H.y, x[r].get(1)));
       if constexpr (BWD) R = make_float2(__builtin_fmaf(A.x, err[r][0], R.x), __builtin_fmaf(A.y, err[r][1], R.y));
     }
@@ -625,9 +628,9 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
           float dx[WV], dg[WV], dout[WV], back[WV];
 #pragma unroll
           for (int e = 0; e < WV; ++e) {
-            const float dh = err[r][e] + get(behind, e), rest = rest_of(g[r].get(e), a[r][e]);
+            const float dh = err[r][e] + get(behind, e), rest = rest_of(a[r][e]);
             dx[e] = rest * dh;
-            back[e] = a[r][e] * dh;
+            back[e] = kept_of(a[r][e]) * dh;
             dg[e] = back[e] * rest * (get(before, e) - x[r].get(e));
             if constexpr (decltype(with_gate)::value) {
               float value, slope;
@@ -670,7 +673,7 @@ __global__ __launch_bounds__(256) void recur_step_kernel(RecurP p, const int32_t
     float y[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      y[e] = h[e] = mix(sigmoid(g.get(e)), h[e], x.get(e));
+      y[e] = h[e] = mix(share(g.get(e)), h[e], x.get(e));
     }
     if (p.o) with_act(p.act, [&](auto act) {
 #pragma unroll
