@@ -217,7 +217,13 @@ template <int MODE>
 __device__ __forceinline__ void dense_bias8(const DenseP& p, int n, int cnt, float (&b)[8]) {
   if ((MODE == DENSE_FWD || dense_q8(MODE)) && p.bias) load8(p.bias + n, cnt, b);
 }
-// Sums of 8-bit integers into what they stand for; s = sx of the row.  Rounded to 24 bits before the product, once.
+// A sum of 8-bit integers into what it stands for: it is rounded to 24 bits, once, then multiplied by both scales' product.  That goes as significands and exponents: the scales' product, or the sum's
+// with one of them, may be beyond the type's ends where the result is not.
+__device__ __forceinline__ float q8_scaled(int sum, float s, float w) {
+  const float m = __builtin_amdgcn_frexp_mantf(s) * __builtin_amdgcn_frexp_mantf(w);
+  return __builtin_amdgcn_ldexpf((float)sum * m, __builtin_amdgcn_frexp_expf(s) + __builtin_amdgcn_frexp_expf(w));
+}
+// s = sx of the row
 template <int MODE>
 __device__ __forceinline__ void dense_scales8(const DenseP& p, int n, int cnt, float (&w)[8]) {
   if constexpr (dense_q8(MODE)) load8(p.sw + n, cnt, w);
@@ -231,7 +237,7 @@ template <int MODE>
 __device__ __forceinline__ void dense_scaled8(float s, const float (&w)[8], float (&v)[8]) {
   if constexpr (dense_q8(MODE))
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)__float_as_int(v[e]) * (s * w[e]);
+    for (int e = 0; e < 8; ++e) v[e] = q8_scaled(__float_as_int(v[e]), s, w[e]);
 }
 
 // What is done with eight sums (DENSE_GATED: of g and of u) at row i, columns n .. n+7 (cnt of them exist).  T: storage type.

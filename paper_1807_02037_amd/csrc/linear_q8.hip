@@ -239,7 +239,7 @@ __global__ __launch_bounds__(FT) void q8_few_kernel(DenseP p, const T* x, long l
       float s = sx[0];
 #pragma unroll
       for (int i = 1; i < R; ++i) s = r == i ? sx[i] : s;
-      float v = (float)mine * (s * p.sw[n]);
+      float v = q8_scaled(mine, s, p.sw[n]);
       if (p.bias) v += p.bias[n];
       with_act(p.act, [&](auto act) { v = act_value<decltype(act)::value>(v); });
       if constexpr (sizeof(T) == 2) {
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(MT) void q8_some_kernel(DenseP p, int kp) {
       for (int e = 0; e < V; ++e) beside[e] = q.get(e);
     }
 #pragma unroll
-    for (int e = 0; e < V; ++e) y[e] = (float)sum[e] * (s * sw[e]) + bias[e];
+    for (int e = 0; e < V; ++e) y[e] = q8_scaled(sum[e], s, sw[e]) + bias[e];
     with_act(p.act, [&](auto act) {
 #pragma unroll
       for (int e = 0; e < V; ++e) y[e] = act_value<decltype(act)::value>(y[e]);
