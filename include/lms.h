@@ -542,7 +542,9 @@ lms_status lms_recur_bwd(const lms_recur_desc* d, const void* dy, const void* x,
 lms_status lms_recur_step(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* slots, const float* state, float* next, void* y, void* stream);
 
 /* Group normalisation with an activation, channels last: n samples of s positions (n * s rows of c channels), `groups` groups of c / groups neighbouring channels.  Over a sample's positions and
- * a group's channels xhat = (x - mean) / sqrt(variance + eps), variance = mean of the squared deviations; y = act(gamma xhat + beta).  s = 1: each token by itself; groups = 1: all its channels. */
+ * a group's channels xhat = (x - mean) / sqrt(variance + eps), variance = mean of the squared deviations; y = act(gamma xhat + beta).  s = 1: each token by itself; groups = 1: all its channels.
+ * Where one value of a group is not finite, the sample's whole group is NaN before the activation (ReLU makes 0 of that).  Sums, of squared deviations too, are
+ * fp32 and have to be finite there: values of 1e19 and more from their mean are beyond it. */
 typedef struct {
   int64_t n, s;             /* samples, >= 0; positions of a sample, >= 1 */
   int32_t c, groups;        /* channels, a multiple of the groups, at most 2^20 */
@@ -560,7 +562,8 @@ lms_status lms_group_norm_bwd(const lms_group_norm_desc* d, const void* dy, cons
                               float* dgamma, float* dbeta, void* workspace, void* stream);
 
 /* Linear layer in 8-bit integers, for serving: y = act((xq wq) sx sw + bias) + res, where a row of x stands as xq = 127 x / max |x| rounded to the nearest whole number, ties to even, times
- * sx = max |x| / 127, and each column of w alike with sw; sums are exact.  A row or column of zeros has the scale 0; one that is not finite everywhere has the scale NaN, and so have the results. */
+ * sx = max |x| / 127, and each column of w alike with sw; sums are exact.  A row or column of zeros has the scale 0; one that is not finite everywhere has the scale NaN, and its sums are NaN before
+ * the activation, which makes 0 of that if it is ReLU. */
 typedef struct {
   int64_t m;                /* rows (tokens), >= 0 */
   int32_t n, k;             /* outputs; inputs, at most 2^17 */
