@@ -155,16 +155,18 @@ class SequenceStudent:
 
     def draft(self, tokens, count, u):
         """For every slot: `count` tokens behind `tokens`, drawn with the random numbers u (slots x count), and the probabilities that they were drawn from.  The states stay as they are."""
-        slots = torch.arange(self.slots, dtype=torch.int32, device="cuda")
+        slots = torch.arange(self.slots, dtype=torch.int32, device=self.state.device)
         old, drafted, probs = self.state, [], []
         self.state = old.clone()
-        for i in range(count):
-            q = torch.softmax(self.read(tokens, slots).float(), dim=1)
-            run = q.double().cumsum(1)
-            tokens = (run > u[:, i:i + 1] * run[:, -1:]).long().argmax(1)
-            drafted.append(tokens)
-            probs.append(q)
-        self.state = old
+        try:
+            for i in range(count):
+                q = torch.softmax(self.read(tokens, slots).float(), dim=1)
+                run = q.double().cumsum(1)
+                tokens = (run > u[:, i:i + 1] * run[:, -1:]).long().argmax(1)
+                drafted.append(tokens)
+                probs.append(q)
+        finally:
+            self.state = old
         return torch.stack(drafted, 1), torch.stack(probs, 1).contiguous()
 
 

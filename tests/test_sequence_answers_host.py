@@ -1,0 +1,37 @@
+"""Drafting and answering of the sequence student on the host, with its reads replaced (no GPU)."""
+import pytest
+import torch
+
+from paper_1807_02037_amd.sequence_student import SequenceStudent
+
+
+class Reads(SequenceStudent):
+    """A student whose read adds 1 to the states and prefers the class behind the token's; the read number `fails` does not come back."""
+
+    def __init__(self, slots=2, classes=7, fails=None):
+        self.slots, self.classes, self.width, self.fails, self.reads = slots, classes, 4, fails, 0
+        self.state = torch.zeros(slots, 4)
+
+    def read(self, tokens, slots, into=None):
+        self.reads += 1
+        if self.reads == self.fails:
+            raise RuntimeError("no answer")
+        into = self.state if into is None else into
+        into += 1
+        return torch.nn.functional.one_hot((tokens + 1) % self.classes, self.classes) * 50.0
+
+
+def test_drafting_leaves_the_states():
+    s = Reads()
+    state = s.state
+    drafted, probs = s.draft(torch.tensor([0, 5]), 3, torch.full((2, 3), 0.5))
+    assert drafted.tolist() == [[1, 2, 3], [6, 0, 1]] and probs.shape == (2, 3, 7)
+    assert s.state is state and not state.any()
+
+
+def test_drafting_leaves_the_states_after_an_error():
+    s = Reads(fails=2)
+    state = s.state
+    with pytest.raises(RuntimeError, match="no answer"):
+        s.draft(torch.tensor([0, 5]), 3, torch.full((2, 3), 0.5))
+    assert s.state is state and not state.any()
