@@ -170,18 +170,20 @@ class SequenceStudent:
         return torch.stack(drafted, 1), torch.stack(probs, 1).contiguous()
 
 
-def verify(p, q, drafted, u, v):
-    """The accepted counts and the tokens of lms_verify; p: (requests, drafts + 1, classes), q: (requests, drafts, classes)."""
+def verify(p, q, drafted, u, v, counts=None):
+    """The accepted counts and the tokens of lms_verify; p: (requests, drafts + 1, classes), q: (requests, drafts, classes).  counts: drafts that each request has, or None for all."""
     b, d, c = q.shape
     _expect("p", p, (b, d + 1, c), torch.float32)
     _expect("q", q, (b, d, c), torch.float32)
     _expect("drafted", drafted, (b, d), torch.int32)
     _expect("u", u, (b, d), torch.float32)
     _expect("v", v, (b,), torch.float32)
+    if counts is not None:
+        _expect("counts", counts, (b,), torch.int32)
     desc = L.verify_desc(b, d, c)
     ws = torch.empty(L.verify_workspace_bytes(desc) + 16, dtype=torch.uint8, device="cuda")
     accepted, tokens = torch.empty(b, dtype=torch.int32, device="cuda"), torch.empty(b, d + 1, dtype=torch.int32, device="cuda")
-    L.verify(desc, _ptr(p), _ptr(q), _ptr(drafted), None, _ptr(u), _ptr(v), _ptr(accepted), _ptr(tokens), _ptr(ws), _stream())
+    L.verify(desc, _ptr(p), _ptr(q), _ptr(drafted), _ptr(counts), _ptr(u), _ptr(v), _ptr(accepted), _ptr(tokens), _ptr(ws), _stream())
     return accepted, tokens
 
 

@@ -1,0 +1,18 @@
+"""The sequence student's verification with fewer drafts of some requests, and its answers at their ends, on the GPU."""
+import pytest
+
+import test_gpu_verify as V
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("b,d,c", [(6, 4, 300), (300, 3, 20000)])
+def test_requests_with_fewer_drafts(b, d, c):
+    import torch
+    from paper_1807_02037_amd.sequence_student import verify
+    p, q, t, n, u, v = V.make(3, b, d, c)
+    args = [torch.as_tensor(x).cuda() for x in (p, q, t.astype("int32"), u, v)]
+    for counts in (None, torch.as_tensor(n, dtype=torch.int32).cuda()):
+        got = verify(*args, counts)
+        want = V.rule(p.astype(float), q.astype(float), t, None if counts is None else n, u.astype(float), v.astype(float))
+        assert (got[0].cpu().numpy() == want[0]).all() and (got[1].cpu().numpy() == want[1]).all()

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_1807_02037_amd.sequence_student import SequenceStudent
+from paper_1807_02037_amd.sequence_student import SequenceStudent, verify
 
 
 class Reads(SequenceStudent):
@@ -35,3 +35,10 @@ def test_drafting_leaves_the_states_after_an_error():
     with pytest.raises(RuntimeError, match="no answer"):
         s.draft(torch.tensor([0, 5]), 3, torch.full((2, 3), 0.5))
     assert s.state is state and not state.any()
+
+
+@pytest.mark.parametrize("shape,dtype", [((3,), torch.int32), ((2,), torch.int64), ((2, 1), torch.int32)])
+def test_verify_refuses_counts(shape, dtype, monkeypatch):
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
+    with pytest.raises(ValueError, match="counts:"):
+        verify(torch.zeros(2, 4, 9), torch.zeros(2, 3, 9), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3), torch.zeros(2), torch.zeros(*shape, dtype=dtype))
