@@ -167,6 +167,8 @@ class SequenceStudent:
                 probs.append(q)
         finally:
             self.state = old
+        if count == 0:
+            return tokens.new_empty(self.slots, 0), old.new_empty(self.slots, 0, self.classes)
         return torch.stack(drafted, 1), torch.stack(probs, 1).contiguous()
 
 
@@ -202,15 +204,16 @@ def answer(student, teacher, tokens, length, drafts, gen):
         z = teacher.read(run.reshape(-1).contiguous(), slots.reshape(-1).contiguous(), into=trial)
         p = torch.softmax(z.float(), dim=1).reshape(b, drafts + 1, -1)
         accepted, got = verify(p, q, drafted.int().contiguous(), u, v)
+        runs = [t[:n + 1] for n, t in zip(accepted.tolist(), got.tolist())]
         # the token before the drafts and the accepted ones go into the states; the next token will with the next run
         keep = torch.where(at[None, :] <= accepted[:, None], slots, torch.full_like(slots, -1)).reshape(-1).contiguous()
         for m in (student, teacher):
             m.read(run.reshape(-1).contiguous(), keep)
         tokens = got.gather(1, accepted.long()[:, None])[:, 0].long()
-        counts.append(accepted.float().mean().item())
-        for i, (n, t) in enumerate(zip(accepted.tolist(), got.tolist())):
-            answers[i] += t[:n + 1]
-    return answers, sum(counts) / len(counts)
+        counts.append(sum(map(len, runs)) / b - 1)
+        for a, r in zip(answers, runs):
+            a += r
+    return answers, sum(counts) / max(1, len(counts))
 
 
 def batches(teacher, rows, seqs, classes, top, gen, sharp=3.0):

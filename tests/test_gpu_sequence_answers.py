@@ -16,3 +16,19 @@ def test_requests_with_fewer_drafts(b, d, c):
         got = verify(*args, counts)
         want = V.rule(p.astype(float), q.astype(float), t, None if counts is None else n, u.astype(float), v.astype(float))
         assert (got[0].cpu().numpy() == want[0]).all() and (got[1].cpu().numpy() == want[1]).all()
+
+
+def models(torch, b=3):
+    from paper_1807_02037_amd.sequence_student import SequenceStudent
+    return [SequenceStudent(32, 1, 64, 120, 4, slots=b, seed=1) for _ in range(2)], torch.Generator(device="cuda").manual_seed(3)
+
+
+def test_answers_without_drafts_and_without_length():
+    import torch
+    from paper_1807_02037_amd.sequence_student import answer
+    (student, teacher), gen = models(torch)
+    first = torch.randint(120, (3,), generator=gen, device="cuda")
+    answers, accepted = answer(student, teacher, first, 5, 0, gen)
+    assert [len(a) for a in answers] == [5, 5, 5] and accepted == 0 and all(0 <= t < 120 for a in answers for t in a)
+    assert torch.equal(student.state, teacher.state) and student.state.any()
+    assert answer(student, teacher, first, 0, 4, gen) == ([[], [], []], 0)

@@ -42,3 +42,8 @@ def test_verify_refuses_counts(shape, dtype, monkeypatch):
     monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
     with pytest.raises(ValueError, match="counts:"):
         verify(torch.zeros(2, 4, 9), torch.zeros(2, 3, 9), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3), torch.zeros(2), torch.zeros(*shape, dtype=dtype))
+
+
+def test_no_drafts():
+    drafted, probs = Reads().draft(torch.tensor([0, 5]), 0, torch.empty(2, 0))
+    assert drafted.shape == (2, 0) and drafted.dtype == torch.int64 and probs.shape == (2, 0, 7) and probs.dtype == torch.float32
