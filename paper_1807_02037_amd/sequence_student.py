@@ -191,7 +191,7 @@ def verify(p, q, drafted, u, v, counts=None):
 
 def answer(student, teacher, tokens, length, drafts, gen):
     """Tokens of every slot behind `tokens`, at least `length` of each, distributed as the teacher's: the student drafts, the teacher reads each run of drafts in one call.  Returns a list of lists and
-    the mean of accepted drafts."""
+    the mean of accepted drafts.  ValueError where the teacher's probabilities leave no class to take."""
     b = teacher.slots
     answers, counts = [[] for _ in range(b)], []
     at = torch.arange(drafts + 1, device="cuda")
@@ -205,6 +205,8 @@ def answer(student, teacher, tokens, length, drafts, gen):
         p = torch.softmax(z.float(), dim=1).reshape(b, drafts + 1, -1)
         accepted, got = verify(p, q, drafted.int().contiguous(), u, v)
         runs = [t[:n + 1] for n, t in zip(accepted.tolist(), got.tolist())]
+        if min(r[-1] for r in runs) < 0:
+            raise ValueError("the teacher gives no class a probability: its logits are not finite")
         # the token before the drafts and the accepted ones go into the states; the next token will with the next run
         keep = torch.where(at[None, :] <= accepted[:, None], slots, torch.full_like(slots, -1)).reshape(-1).contiguous()
         for m in (student, teacher):

@@ -32,3 +32,13 @@ def test_answers_without_drafts_and_without_length():
     assert [len(a) for a in answers] == [5, 5, 5] and accepted == 0 and all(0 <= t < 120 for a in answers for t in a)
     assert torch.equal(student.state, teacher.state) and student.state.any()
     assert answer(student, teacher, first, 0, 4, gen) == ([[], [], []], 0)
+
+
+def test_no_class_to_take():
+    """Logits that are not finite: an error, not tokens that are no class."""
+    import torch
+    from paper_1807_02037_amd.sequence_student import answer
+    (student, teacher), gen = models(torch)
+    teacher.weights["wh"][3] = float("nan")
+    with pytest.raises(ValueError, match="no class"):
+        answer(student, teacher, torch.randint(120, (3,), generator=gen, device="cuda"), 5, 2, gen)
