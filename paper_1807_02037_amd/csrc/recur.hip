@@ -337,6 +337,11 @@ __global__ __launch_bounds__((Shape<T, WAY>::NT), 4) void recur_kernel(RecurP p)
     };
     anew(x);
     if constexpr (BWD) { anew(g); anew(o); }
+    if constexpr (NARROW)                                         // there a and 1 - a as well (146338 x 64 forward 78 -> 63 us, backward 107 -> 100; 64571 x 640 124 and 126)
+#pragma unroll
+      for (auto& row : a)
+#pragma unroll
+        for (float& v : row) asm volatile("" : "+v"(v));
     for (int w = 0; w < wave; ++w) compose(s_a[w], s_h[w], state);
     if constexpr (NARROW)
 #pragma unroll
@@ -547,7 +552,7 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
 #pragma unroll
           for (int e = 0; e < WV; ++e) err[r][e] = dy[r].get(e);
     }
-    float2 A = {1.f, 1.f}, H = {0.f, 0.f}, R = {0.f, 0.f};
+    float2 A = {1.f, 1.f}, H = {0.f, 0.f}, R = {0.f, 0.f}, upto_a[BWD ? 1 : WROWS], upto_h[BWD ? 1 : WROWS];      // upto: A and H of the rows up to each
 #pragma unroll
     for (int r = 0; r < WROWS; ++r) {
       const bool live = at0 + r < each;
@@ -562,6 +567,7 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
       A = make_float2(A.x * kept_of(a[r][0]), A.y * kept_of(a[r][1]));
       H = make_float2(mix(a[r][0], H.x, x[r].get(0)), mix(a[r][1], H.y, x[r].get(1)));
       if constexpr (BWD) R = make_float2(__builtin_fmaf(A.x, err[r][0], R.x), __builtin_fmaf(A.y, err[r][1], R.y));
+      else { upto_a[r] = A; upto_h[r] = H; }
     }
     s_a[half][wave][lane] = A;
     s_h[half][wave][lane] = H;
@@ -589,7 +595,7 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
 #pragma unroll
         for (unsigned& w : v.q) asm volatile("" : "+v"(w));
     };
-    anew(x);
+    if constexpr (BWD) anew(x);
     if (!column) continue;
     if constexpr (!BWD) {
       if (p.kept && at0 % KEEP == 0 && at0 < each) __builtin_memcpy(p.kept + ((long long)seq * keeps + at0 / KEEP) * p.channels + c, &state, 8);
@@ -597,10 +603,10 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
 #pragma unroll
         for (int r = 0; r < WROWS; ++r) {
           float y[WV];
-          state = make_float2(mix(a[r][0], state.x, x[r].get(0)), mix(a[r][1], state.y, x[r].get(1)));
+          const float2 h = pass(upto_a[r], state, upto_h[r]);
 #pragma unroll
           for (int e = 0; e < WV; ++e) {
-            y[e] = get(state, e);
+            y[e] = get(h, e);
             if constexpr (decltype(with_gate)::value) {
               float value, slope;
               act_one<decltype(act)::value>(o[r].get(e), value, slope);
@@ -609,7 +615,7 @@ __global__ __launch_bounds__(512, 2) void recur_walk_kernel(RecurP p) {
           }
           if (at0 + r >= each) continue;
           put((T*)p.y, (row0 + at0 + r) * p.ldy, y);
-          if (at0 + r == each - 1 && p.last) __builtin_memcpy(p.last + (long long)seq * p.channels + c, &state, 8);
+          if (at0 + r == each - 1 && p.last) __builtin_memcpy(p.last + (long long)seq * p.channels + c, &h, 8);
         }
       };
       if (gated) with_act(p.act, [&](auto act) __attribute__((always_inline)) { finish(act, std::true_type{}); });
