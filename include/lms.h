@@ -534,7 +534,8 @@ lms_status lms_recur_kept_bytes(const lms_recur_desc* d, uint64_t* bytes);
 lms_status lms_recur_fwd(const lms_recur_desc* d, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, void* y, float* last, void* kept,
                          void* workspace, void* stream);
 /* dlast: gradient of last, or NULL for zeros.  With e = dy act(o): dh_t = e_t + a_{t+1} dh_{t+1}, at a sequence's end e_t + dlast; dx = (1 - a) dh, dg = dh (h_{t-1} - x) a (1 - a),
- * dout = dy h act'(o), dh0 = a dh of the first position.  h is computed again from kept.  dx, dg, dout and dh0 may each be NULL.  Deterministic. */
+ * dout = dy h act'(o), dh0 = a dh of the first position.  h is computed again from kept, as a forward call with the same descriptor left it,
+ * with offsets in both calls or in neither.  dx, dg, dout and dh0 may each be NULL.  Deterministic. */
 lms_status lms_recur_bwd(const lms_recur_desc* d, const void* dy, const void* x, const void* g, const void* o, const int32_t* offsets, const float* h0, const void* kept,
                          const float* dlast, void* dx, void* dg, void* dout, float* dh0, void* workspace, void* stream);
 /* One position of each of `rows` requests (at most 65536): row i goes on from state[slots[i]] and leaves next[slots[i]]; state and next: seqs x channels fp32, the same or apart.
@@ -562,7 +563,7 @@ lms_status lms_group_norm_bwd(const lms_group_norm_desc* d, const void* dy, cons
                               float* dgamma, float* dbeta, void* workspace, void* stream);
 
 /* Linear layer in 8-bit integers, for serving: y = act((xq wq) sx sw + bias) + res, where a row of x stands as xq = 127 x / max |x| rounded to the nearest whole number, ties to even, times
- * sx = max |x| / 127, and each column of w alike with sw; sums are exact.  A row or column of zeros has the scale 0; one that is not finite everywhere has the scale NaN, and its sums are NaN before
+ * sx = max |x| / 127 (fp32, with fewer digits below 2^-126), and each column of w alike with sw; sums are exact.  A row or column of zeros has the scale 0; one that is not finite everywhere has the scale NaN, and its sums are NaN before
  * the activation, which makes 0 of that if it is ReLU. */
 typedef struct {
   int64_t m;                /* rows (tokens), >= 0 */

@@ -2,7 +2,7 @@
 //
 // Both operands of the product lie with the reduction in rows of whole 16-byte vectors, zeros behind the last element: the weights are turned once, x as it is quantised.  In bytes the
 // product is then that of two bf16 matrices whose reductions lie in rows, and it runs on the same tiles (dense_gemm.hip); up to 64 rows have kernels of their own, which read the weights in one round.
-// us: 8192 rows, 8192 -> 4096, residual: rows 45 (201 MB at 4.4 TB/s), product 261 to 295 as the clock goes (1.9 to 2.1 P/s; operands of zeros 199); 24 rows, 2048 -> 8192: 3 and 6.
+// us: 8192 rows, 8192 -> 4096, residual: rows 45 (201 MB at 4.4 TB/s), product 265 to 300 as the clock goes (1.8 to 2.1 P/s; operands of zeros 199); 24 rows, 2048 -> 8192: 3 and 6.
 #include <hip/hip_runtime.h>
 
 #include <initializer_list>
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(NT) void q8_rows_kernel(const T* x, long long ldx, 
 //
 // Bound by reading the weights once.  A wave takes CW columns, its lanes consecutive 16 bytes of the reduction, and has eight loads of weights in flight before anything else happens; the rows of x lie
 // in LDS, 4-byte dot products go to whole sums of each lane, and the lanes meet by shuffles: whole numbers, in any order the same.  FUSED: every work-group quantises the rows itself,
-// while its weights are on their way, instead of waiting for another launch.  One row, 4096 -> 4096: 5.8 us in a graph, 2.9 TB/s of weights.  (Products of 32 x 32 x 32 with both operands straight from memory, for 9 to
+// while its weights are on their way, instead of waiting for another launch.  One row, 4096 -> 4096, us in a graph: 5.5 with the same weights again, 7.0 with two sets by turns, 8.4 with weights from memory (2.0 TB/s).  (Products of 32 x 32 x 32 with both operands straight from memory, for 9 to
 // 32 rows, took 10.1 us at 24 x 2048 -> 8192 and 58 at 32 x 8192 -> 16384: half a line of each column a load is what the address unit is slow at.)
 constexpr int FT = 512, FEW_LDS = 65536 - 256;      // with what the kernel has besides, no more than any launch may have
 
@@ -479,7 +479,7 @@ hipError_t quantise(const lms_linear_q8_desc* d, const T* x, signed char* xq, fl
   return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
 
-// One or two rows that fit the LDS.  From three on products of many rows, whose two launches then cost less than the dot products (us, dot products / those: 4096 -> 4096 one row 5.8 / 8, two 7.2 / 8.3,
+// One or two rows that fit the LDS.  From three on products of many rows, whose two launches then cost less than the dot products (us, the same weights again, dot products / those: 4096 -> 4096 one row 5.8 / 8, two 7.2 / 8.3,
 // four 9.4 / 8.6; 2048 -> 8192 four rows 10.7 / 7.6; 8192 -> 16384 four rows 31.6 / 31.8).
 bool few_rows(const lms_linear_q8_desc* d) { return d->m >= 1 && d->m <= 2 && d->m * pitch(d) <= FEW_LDS; }
 

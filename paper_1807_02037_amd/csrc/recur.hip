@@ -478,8 +478,8 @@ __global__ __launch_bounds__(JOIN_WIDTH * JOIN_SPANS) void recur_join_kernel(Rec
 //
 // Where there are enough of them for the chip, every tensor is read once: a work-group takes two channels a lane of one sequence and goes through it 64 rows at a time, eight waves of eight rows, the next rows' loads out
 // before these are worked on.  The waves' spans meet in LDS, every wave composes all of them, and so each knows the state that the next 64 rows begin with: one barrier a step.  Rows
-// beyond a sequence's end pass r on as it is (a = 1, e = 0), so that the gradient of the last state enters there.  32768 x 4096 in bf16 of 8 sequences, with a gate: forward 198 us (5.4 TB/s), backward
-// 392 us (4.8 TB/s); a copy of 1 GiB reaches 5.05 TB/s.
+// beyond a sequence's end pass r on as it is (a = 1, e = 0), so that the gradient of the last state enters there.  32768 x 4096 in bf16 of 8 sequences, with a gate: forward 199 us (5.4 TB/s), backward
+// 386 us (4.9 TB/s); a copy of 1 GiB reaches 5.05 TB/s.
 constexpr int WV = 2, WBLOCK = 64 * WV, WROWS = 8, WSTEP = 8 * WROWS;
 
 template <typename T, bool BWD>
@@ -805,8 +805,8 @@ bool alone(const lms_recur_desc* d, int chunk, const int32_t* offsets) { return 
 // Whether work-groups walk along sequences of one length, for both directions together, since they share what is kept: by what both are estimated to take.  A step of 64 rows takes
 // 8.5 us there and back, on each compute unit one at a time, or as long as the eleven tensors take; the line reads five of them twice and has two more launches each way.
 // us, bf16 with a gate, forward + backward, walk / line:
-//   sequences x rows x channels   8 x 4096 x 4096  222 + 412 / 325 + 528     4 x 4096 x 4096  176 + 352 / 184 + 287     8 x 2048 x 2048  93 + 184 / 94 + 158
-//   32 x 512 x 512  23 + 42 / 30 + 54     16 x 128 x 1024  9 + 15 / 17 + 20     4 x 1024 x 2048  41 + 79 / 28 + 44     1 x 8192 x 4096  331 + 636 / 95 + 156
+//   sequences x rows x channels   8 x 4096 x 4096  209 + 385 / 336 + 529     4 x 4096 x 4096  175 + 338 / 186 + 276     8 x 2048 x 2048  92 + 177 / 95 + 150
+//   32 x 512 x 512  24 + 47 / 32 + 48     16 x 128 x 1024  9 + 14 / 21 + 22     4 x 1024 x 2048  43 + 83 / 32 + 46     1 x 8192 x 4096  331 + 613 / 102 + 149
 bool walks(const lms_recur_desc* d, const int32_t* offsets) {
   const long long each = d->rows / d->seqs, groups = (long long)d->seqs * ((d->channels + WBLOCK - 1) / WBLOCK);
   if (offsets || each <= CHUNK_FWD || d->channels < WV || groups >= 1 << 22) return false;
