@@ -155,6 +155,8 @@ class SequenceStudent:
 
     def draft(self, tokens, count, u):
         """For every slot: `count` tokens behind `tokens`, drawn with the random numbers u (slots x count), and the probabilities that they were drawn from.  The states stay as they are."""
+        if tuple(u.shape) != (self.slots, count):
+            raise ValueError(f"u: a tensor of {(self.slots, count)} is needed, not {tuple(u.shape)}")
         slots = torch.arange(self.slots, dtype=torch.int32, device=self.state.device)
         old, drafted, probs = self.state, [], []
         self.state = old.clone()

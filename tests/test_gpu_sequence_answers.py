@@ -42,3 +42,12 @@ def test_no_class_to_take():
     teacher.weights["wh"][3] = float("nan")
     with pytest.raises(ValueError, match="no class"):
         answer(student, teacher, torch.randint(120, (3,), generator=gen, device="cuda"), 5, 2, gen)
+
+
+def test_no_tokens():
+    import torch
+    (student, _), _ = models(torch)
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    for _ in range(2):
+        assert student.read(none, none.int()).shape == (0, 120) and not student.state.any()
+        student.quantise()

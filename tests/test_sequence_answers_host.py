@@ -47,3 +47,10 @@ def test_verify_refuses_counts(shape, dtype, monkeypatch):
 def test_no_drafts():
     drafted, probs = Reads().draft(torch.tensor([0, 5]), 0, torch.empty(2, 0))
     assert drafted.shape == (2, 0) and drafted.dtype == torch.int64 and probs.shape == (2, 0, 7) and probs.dtype == torch.float32
+
+
+@pytest.mark.parametrize("shape", [(1, 3), (2, 2), (2, 4), (3, 3)])
+def test_random_numbers_of_another_size(shape):
+    """One row would be the same numbers for every request."""
+    with pytest.raises(ValueError, match="u:"):
+        Reads().draft(torch.tensor([0, 5]), 3, torch.full(shape, 0.5))
